@@ -273,6 +273,70 @@ pc_status percache_attention_reuse(percache_ctx *ctx, int32_t layer, const void 
                                    int32_t max_chunks, int32_t n_splits, void *attn_out_dev,
                                    void *workspace_dev, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------- drafted tokens
+ * Decoding several guesses at once (Sec. 2.2: decoding one token at a time dominates server-side inference): each query brings a TREE of
+ * t_draft drafted tokens, all of them go through a layer in one pass, and the accepted path is kept.
+ *
+ * A tree, on the host: parents_host[b*t_draft + i] is the node in front of node i -- an earlier node, -1 for a node that hangs on the last
+ * token before the tree, or -2 for padding (nobody's parent; a query with fewer nodes).  Node i sees every cached token, its ancestors
+ * and itself; padding sees nothing.  parents_host == NULL: each node's parent is the one before it (a plain sequence, any length);
+ * trees have at most 256 nodes (PC_ESHAPE).
+ * A path, on the host: n_path_host[b] nodes path_host[b*max_path + j], 1 <= max_path <= t_draft.
+ *
+ * percache_qkv_rope_draft: steps 1-2 of percache_prefill_reuse for the nodes, node i at position pos0_host[b] + depth(i) (roots: depth 0; padding
+ *   too).  The positions are the caller's: behind slots from which tokens were evicted (percache_kv_keep) the cached length is not
+ *   the position any more.  x_dev [batch, t_draft, hidden]; q_out_dev [batch, Hq, t_draft, D], k_out_dev, v_out_dev [batch, Hkv, t_draft, D], bf16.
+ * percache_attention_draft: step 3.  attn_out_dev [batch, t_draft, Hq * D] bf16, zero for padding.  lse_out_dev (may be NULL): float
+ *   [batch, Hq, t_draft], the log-sum-exp of the scores q.k / sqrt(D) that a row sees, -infinity for padding.  What a row does not see takes no part,
+ *   infinities and NaN included.  n_splits as in percache_attention_reuse.  L_pre is not checked against max_pos - t_draft here.
+ * percache_attention_weights: what the rows pay to each key, from the log-sum-exp of the same rows,
+ *     w(key) = sum over the queries that use it, the query heads of its kv head and their rows that count, of exp(q.k / sqrt(D) - lse),
+ *   rows with lse -infinity none.  path_host == NULL: every row counts; else the nodes of each query's path (after verification: the
+ *   accepted ones; a node named twice counts twice).
+ *     weights_out[slot, kv head, token] = weights_in[...] + w   for the used tokens of the slots in the chunk list, nothing else is written.
+ *   weights_in_dev, weights_out_dev: float [n_slots, Hkv, slot_capacity] of this layer, the caller's; the same array adds in place, weights_in_dev
+ *   NULL starts from zero.  A slot that several queries use gets the sum over all of them.  draft_weights_out_dev (may be NULL; else
+ *   k_draft_dev is needed): float [batch, Hkv, t_draft], written with the weights of the draft keys.  The sums are fp32, in a fixed order.
+ * percache_kv_append_path: token start_host[b] + j of slot append_slots_host[b] (negative: skipped) becomes row path[j] of k_dev, v_dev
+ *   [batch, Hkv, t_draft, D]; tokens that the slot held from start on are dropped (start_host NULL: behind its last token, nothing is dropped).
+ *   With draft_weights_dev and weights_dev (both or neither) the nodes' weights go along: weights[slot, kv head, start + j].  In an 8-bit slot
+ *   everything from the block of token start on is quantised afresh, as by percache_kv_append.  A slot may appear once.
+ * Workspace of the first three: percache_draft_workspace_bytes (max_chunks 0 for the projection), 256-byte aligned.  The calls bring their
+ * lists to the device as the calls with host chunk lists do. */
+size_t percache_draft_workspace_bytes(const percache_ctx *ctx, int32_t batch, int32_t t_draft, int32_t max_chunks);
+pc_status percache_qkv_rope_draft(percache_ctx *ctx, const void *x_dev, const void *wqkv_dev, int32_t batch, int32_t t_draft,
+                                  const int32_t *parents_host, const int32_t *pos0_host, void *q_out_dev, void *k_out_dev,
+                                  void *v_out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+pc_status percache_attention_draft(percache_ctx *ctx, int32_t layer, const void *q_dev, const void *k_draft_dev,
+                                   const void *v_draft_dev, int32_t batch, int32_t t_draft, const int32_t *slot_ids_host,
+                                   const int32_t *used_len_host, const int32_t *n_chunks_host, int32_t max_chunks,
+                                   const int32_t *parents_host, int32_t n_splits, void *attn_out_dev, float *lse_out_dev,
+                                   void *workspace_dev, size_t workspace_bytes, void *stream);
+pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer, const void *q_dev, const void *k_draft_dev,
+                                     const float *lse_dev, int32_t batch, int32_t t_draft, const int32_t *slot_ids_host,
+                                     const int32_t *used_len_host, const int32_t *n_chunks_host, int32_t max_chunks,
+                                     const int32_t *parents_host, const int32_t *path_host, const int32_t *n_path_host,
+                                     int32_t max_path, const float *weights_in_dev, float *weights_out_dev,
+                                     float *draft_weights_out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+pc_status percache_kv_append_path(percache_ctx *ctx, int32_t layer, const void *k_dev, const void *v_dev, int32_t batch,
+                                  int32_t t_draft, const int32_t *path_host, const int32_t *n_path_host, int32_t max_path,
+                                  const int32_t *append_slots_host, const int32_t *start_host, const float *draft_weights_dev,
+                                  float *weights_dev, void *stream);
+
+/* Eviction inside a slot (Sec. 4.1.1 evicts whole entries by use; Sec. 7 looks ahead to finer organisations): slot slots_host[i] with more than
+ * keep_host[i] tokens is cut to keep_host[i], by every kv head for itself: the first n_first, the last n_last and, of those between, the tokens
+ * of the largest weights (weights_dev as kept by percache_attention_weights; equal weights: the earlier token, NaN below everything).  The
+ * kept tokens stay in order and close up, their weights with them; a slot with no more than keep_host[i] tokens keeps all of them.
+ * Needs n_first + n_last <= keep_host[i].  dst_slots_host NULL: in place; else the kept tokens (and weights) go to slot dst_slots_host[i], of either
+ * format, and the source stays as it is (dst == source: in place).  No slot may appear twice otherwise.  An 8-bit destination is quantised
+ * afresh from the values the source reads back.
+ *   idx_out_dev (may be NULL): int32 [n, Hkv, largest keep], the token each kept one was, -1 behind them.
+ *   workspace_dev >= percache_kv_keep_workspace_bytes(ctx, n, largest keep), 256-byte aligned. */
+size_t percache_kv_keep_workspace_bytes(const percache_ctx *ctx, int32_t n, int32_t max_keep);
+pc_status percache_kv_keep(percache_ctx *ctx, int32_t layer, const int32_t *slots_host, const int32_t *dst_slots_host, int32_t n,
+                           const int32_t *keep_host, int32_t n_first, int32_t n_last, float *weights_dev, int32_t *idx_out_dev,
+                           void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- cache index (Sec. 4.1.1, Sec. 4.2.2, App. B.2)
  * Host-side prefix tree over knowledge chunks that hands out slot ids of the K/V store; no device work.  A node is
  * one chunk (keyed by its text), a path from the root the chunk list of one query.  The same slot id is meant to

@@ -32,6 +32,8 @@ EXPORTS = [
     "percache_prefill_workspace_bytes", "percache_prefill_reuse", "percache_qkv_rope", "percache_attention_reuse",
     "percache_chunk_table_bytes", "percache_chunk_table_put", "percache_chunk_table_drop",
     "percache_prefill_reuse_table", "percache_stack_reuse_table",
+    "percache_draft_workspace_bytes", "percache_qkv_rope_draft", "percache_attention_draft", "percache_attention_weights",
+    "percache_kv_append_path", "percache_kv_keep_workspace_bytes", "percache_kv_keep",
     "percache_profile_enable", "percache_profile_read",
     "percache_peak_scratch_bytes", "percache_peak_mfma_bf16", "percache_peak_stream_read", "percache_peak_attention_tile_loop",
 ]
@@ -103,6 +105,14 @@ def load_library() -> ctypes.CDLL:
         "percache_prefill_reuse_table": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
         "percache_stack_reuse_table": (_i32, [_vp, ctypes.POINTER(BlockWeights), _i32, _i32, ctypes.c_float, _vp, _i32, _i32,
                                               _vp, _vp, _vp, _sz, _vp]),
+        "percache_draft_workspace_bytes": (_sz, [_vp, _i32, _i32, _i32]),
+        "percache_qkv_rope_draft": (_i32, [_vp, _vp, _vp, _i32, _i32, _pi32, _pi32, _vp, _vp, _vp, _vp, _sz, _vp]),
+        "percache_attention_draft": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _pi32, _pi32, _pi32, _i32, _pi32, _i32, _vp, _vp, _vp, _sz, _vp]),
+        "percache_attention_weights": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _pi32, _pi32, _pi32, _i32, _pi32, _pi32, _pi32, _i32, _vp, _vp, _vp,
+                                              _vp, _sz, _vp]),
+        "percache_kv_append_path": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, _pi32, _pi32, _i32, _pi32, _pi32, _vp, _vp, _vp]),
+        "percache_kv_keep_workspace_bytes": (_sz, [_vp, _i32, _i32]),
+        "percache_kv_keep": (_i32, [_vp, _i32, _pi32, _pi32, _i32, _pi32, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
         "percache_kv_slice": (_i32, [_vp, _i32, _vp, _vp, _i32, _pi32, _pi32, _i32, _vp]),
         "percache_kv_append": (_i32, [_vp, _i32, _i32, _vp, _vp, _i32, _vp]),
         "percache_stack_decode": (_i32, [_vp, ctypes.POINTER(BlockWeights), _i32, _i32, ctypes.c_float, _vp, _i32, _i32,
@@ -180,6 +190,7 @@ class Percache:
         self._step_ws = None
         self._lookup_ws = None
         self._topk_ws = None
+        self._draft_ws = None
 
     # ------------------------------------------------------------------ helpers
     def _check(self, st: int):
@@ -472,6 +483,133 @@ class Percache:
                                                       t_fresh, ids_p, ul_p, nc_p, max_chunks, n_splits, _ptr(attn_out),
                                                       ws, need, _stream()))
         return attn_out
+
+    # ------------------------------------------------------------------ drafted tokens, eviction inside a slot
+    def _draft_workspace(self, nbytes: int):
+        import torch
+        if self._draft_ws is None or self._draft_ws.numel() < nbytes + 256:
+            self._draft_ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        return (self._draft_ws.data_ptr() + 255) // 256 * 256
+
+    def _want(self, name, t, shape, dtype):
+        """The kernels read dense rows: a tensor of another shape, type or stride order is refused, not reinterpreted."""
+        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device.type != self.device.type):
+            raise ValueError(f"{name}: a contiguous {dtype} tensor {shape} on {self.device.type} is wanted, got {t.dtype} {tuple(t.shape)} "
+                             f"{'' if t.is_contiguous() else 'not contiguous '}on {t.device}")
+
+    def _want_weights(self, *named):
+        import torch
+        c = self.cfg
+        for name, t in named:
+            self._want(name, t, (c.n_slots, c.n_kv_heads, c.slot_capacity), torch.float32)
+
+    def _want_draft(self, batch, t_draft, q=None, k=None, v=None):
+        import torch
+        c = self.cfg
+        self._want("q", q, (batch, c.n_q_heads, t_draft, c.head_dim), torch.bfloat16)
+        self._want("k", k, (batch, c.n_kv_heads, t_draft, c.head_dim), torch.bfloat16)
+        self._want("v", v, (batch, c.n_kv_heads, t_draft, c.head_dim), torch.bfloat16)
+
+    @staticmethod
+    def _path_args(path, n_path, batch):
+        if path is None:
+            return None, None, None, 0
+        path, path_p = _host_i32(path)
+        path = path.reshape(batch, -1)
+        n_path, n_path_p = _host_i32(np.full(batch, path.shape[1], np.int32) if n_path is None else n_path, (batch,))
+        return (path, n_path), path_p, n_path_p, path.shape[1]
+
+    def percache_qkv_rope_draft(self, x, wqkv, pos0, parents=None, q_out=None, k_out=None, v_out=None):
+        """x [B, T, hidden]; parents [B, T] (-1: behind the tokens before the tree, -2: padding) or None for a sequence; pos0 [B]."""
+        import torch
+        batch, t_draft, _ = x.shape
+        par, par_p = _host_i32(parents, (batch, t_draft))
+        p0, p0_p = _host_i32(pos0, (batch,))
+        c = self.cfg
+        if q_out is None:
+            q_out = torch.empty((batch, c.n_q_heads, t_draft, c.head_dim), dtype=torch.bfloat16, device=self.device)
+            k_out = torch.empty((batch, c.n_kv_heads, t_draft, c.head_dim), dtype=torch.bfloat16, device=self.device)
+            v_out = torch.empty_like(k_out)
+        self._want("x", x, (batch, t_draft, c.hidden), torch.bfloat16)
+        self._want("wqkv", wqkv, ((c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, c.hidden), torch.bfloat16)
+        self._want_draft(batch, t_draft, q_out, k_out, v_out)
+        need = self.lib.percache_draft_workspace_bytes(self.ctx, batch, t_draft, 0)
+        ws = self._draft_workspace(need)
+        self._check(self.lib.percache_qkv_rope_draft(self.ctx, _ptr(x), _ptr(wqkv), batch, t_draft, par_p, p0_p, _ptr(q_out), _ptr(k_out), _ptr(v_out),
+                                                     ws, need, _stream()))
+        return q_out, k_out, v_out
+
+    def percache_attention_draft(self, layer, q, k_draft, v_draft, slot_ids=None, used_len=None, n_chunks=None, parents=None, n_splits: int = 0,
+                                 attn_out=None, lse_out=None):
+        """(attn_out [B, T, Hq * D], lse [B, Hq, T] or None).  lse_out: a float32 tensor, True for a new one, None for none."""
+        import torch
+        batch, _, t_draft, _ = q.shape
+        keep, ids_p, ul_p, nc_p, max_chunks = self._chunk_args(batch, slot_ids, used_len, n_chunks)
+        par, par_p = _host_i32(parents, (batch, t_draft))
+        c = self.cfg
+        if attn_out is None:
+            attn_out = torch.empty((batch, t_draft, c.n_q_heads * c.head_dim), dtype=torch.bfloat16, device=self.device)
+        if lse_out is True:
+            lse_out = torch.empty((batch, c.n_q_heads, t_draft), dtype=torch.float32, device=self.device)
+        self._want_draft(batch, t_draft, q, k_draft, v_draft)
+        self._want("attn_out", attn_out, (batch, t_draft, c.n_q_heads * c.head_dim), torch.bfloat16)
+        self._want("lse_out", lse_out, (batch, c.n_q_heads, t_draft), torch.float32)
+        need = self.lib.percache_draft_workspace_bytes(self.ctx, batch, t_draft, max_chunks)
+        ws = self._draft_workspace(need)
+        self._check(self.lib.percache_attention_draft(self.ctx, layer, _ptr(q), _ptr(k_draft), _ptr(v_draft), batch, t_draft, ids_p, ul_p, nc_p, max_chunks,
+                                                      par_p, n_splits, _ptr(attn_out), _ptr(lse_out), ws, need, _stream()))
+        return attn_out, lse_out
+
+    def percache_attention_weights(self, layer, q, k_draft, lse, weights_in, weights_out, slot_ids=None, used_len=None, n_chunks=None, parents=None,
+                                   path=None, n_path=None, draft_weights=None):
+        """Adds what the rows (or the nodes of the paths) pay to the cached keys to weights_in [n_slots, Hkv, slot_capacity] (None: zero), into
+        weights_out; returns the weights of the draft keys [B, Hkv, T] (None where k_draft is None)."""
+        import torch
+        batch, _, t_draft, _ = q.shape
+        keep, ids_p, ul_p, nc_p, max_chunks = self._chunk_args(batch, slot_ids, used_len, n_chunks)
+        par, par_p = _host_i32(parents, (batch, t_draft))
+        paths, path_p, n_path_p, max_path = self._path_args(path, n_path, batch)
+        if draft_weights is None and k_draft is not None:
+            draft_weights = torch.empty((batch, self.cfg.n_kv_heads, t_draft), dtype=torch.float32, device=self.device)
+        self._want_draft(batch, t_draft, q, k_draft)
+        self._want("lse", lse, (batch, self.cfg.n_q_heads, t_draft), torch.float32)
+        self._want("draft_weights", draft_weights, (batch, self.cfg.n_kv_heads, t_draft), torch.float32)
+        self._want_weights(("weights_in", weights_in), ("weights_out", weights_out))
+        need = self.lib.percache_draft_workspace_bytes(self.ctx, batch, t_draft, max_chunks)
+        ws = self._draft_workspace(need)
+        self._check(self.lib.percache_attention_weights(self.ctx, layer, _ptr(q), _ptr(k_draft), _ptr(lse), batch, t_draft, ids_p, ul_p, nc_p, max_chunks,
+                                                        par_p, path_p, n_path_p, max_path, _ptr(weights_in), _ptr(weights_out), _ptr(draft_weights),
+                                                        ws, need, _stream()))
+        return draft_weights
+
+    def percache_kv_append_path(self, layer, k, v, append_slots, path, n_path=None, start=None, weights=None, draft_weights=None):
+        """k, v [B, Hkv, T, D]: the nodes of each query's path behind token start[b] (None: the last one) of slot append_slots[b] (< 0: skipped)."""
+        import torch
+        batch, _, t_draft, _ = k.shape
+        self._want_draft(batch, t_draft, None, k, v)
+        self._want("draft_weights", draft_weights, (batch, self.cfg.n_kv_heads, t_draft), torch.float32)
+        self._want_weights(("weights", weights))
+        paths, path_p, n_path_p, max_path = self._path_args(path, n_path, batch)
+        sl, sl_p = _host_i32(append_slots, (batch,))
+        st, st_p = _host_i32(start, (batch,))
+        self._check(self.lib.percache_kv_append_path(self.ctx, layer, _ptr(k), _ptr(v), batch, t_draft, path_p, n_path_p, max_path, sl_p, st_p,
+                                                     _ptr(draft_weights), _ptr(weights), _stream()))
+
+    def percache_kv_keep(self, layer, slots, keep, weights, n_first: int = 0, n_last: int = 0, dst_slots=None, idx_out=None):
+        """Cuts each slot to keep (an int or one per slot) tokens per kv head, by weight; returns the kept tokens' indexes [n, Hkv, max keep]."""
+        import torch
+        sl, sl_p = _host_i32(slots)
+        dst, dst_p = _host_i32(dst_slots, (len(sl),))
+        kp, kp_p = _host_i32(np.broadcast_to(np.asarray(keep, np.int32), (len(sl),)))
+        most = int(kp.max()) if len(kp) else 0
+        if idx_out is None:
+            idx_out = torch.empty((len(sl), self.cfg.n_kv_heads, max(most, 0)), dtype=torch.int32, device=self.device)
+        self._want_weights(("weights", weights))
+        self._want("idx_out", idx_out, (len(sl), self.cfg.n_kv_heads, max(most, 0)), torch.int32)
+        need = self.lib.percache_kv_keep_workspace_bytes(self.ctx, len(sl), most)
+        ws = self._draft_workspace(need)
+        self._check(self.lib.percache_kv_keep(self.ctx, layer, sl_p, dst_p, len(sl), kp_p, n_first, n_last, _ptr(weights), _ptr(idx_out), ws, need, _stream()))
+        return idx_out
 
     # ------------------------------------------------------------------ stack of layers on the retained rows
     def percache_stack_workspace_bytes(self, batch, t_fresh, max_chunks, ffn) -> int:

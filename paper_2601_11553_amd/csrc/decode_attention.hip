@@ -52,12 +52,13 @@ struct Lds {
 // writes: dense (k_out, v_out) and, where the query has a bf16 slot to append to, behind the tokens that slot holds.  The
 // keys of that slot read by this launch, for this query or another, are the older ones: lengths come from the chunk list, K rows
 // past the end are not read and V positions past it are cleared after the read (compute), which may see the new ones.
-template <int D, int FMT, int NR, bool RAW, bool TWO>
+// DRAFT: the fresh keys are nodes of a tree (pc::DraftView), of which a row sees its ancestors.
+template <int D, int FMT, int NR, bool RAW, bool TWO, bool DRAFT = false>
 __global__ __launch_bounds__(256, (FMT == 1 && (NR == 1 || !RAW)) || TWO ? 2 : 1) void decode_attention_kernel(
     const __bf16 *__restrict__ Q, const __bf16 *__restrict__ Kf, const __bf16 *__restrict__ Vf, pc::RawQkv raw, const __bf16 *k16,
     const __bf16 *v16, const uint8_t *__restrict__ k8, const uint8_t *__restrict__ v8, const float *__restrict__ k_scale,
     const float *__restrict__ v_scale, int n_slots16, const int32_t *__restrict__ table, int tbl_stride, int T, int Hq, int Hkv, int C,
-    int n_splits, float scale_log2e, __bf16 *__restrict__ out, float *__restrict__ part_o, float *__restrict__ part_ml) {
+    int n_splits, float scale_log2e, __bf16 *__restrict__ out, float *__restrict__ part_o, float *__restrict__ part_ml, pc::DraftView draft) {
   using L = Lds<D, FMT, NR, TWO>;
   constexpr int KS = D / 32, DB = D / 16, NSTG = L::NSTG;
   __shared__ __align__(16) char lds[L::BYTES];
@@ -84,6 +85,7 @@ __global__ __launch_bounds__(256, (FMT == 1 && (NR == 1 || !RAW)) || TWO ? 2 : 1
   const int F = (Hq + 2 * Hkv) * D;   // (RAW) width of a row of sums: q heads, k heads, v heads
   const bool fresh_mine = with_fresh && wave * 16 < T;
   int my_i[NR];
+  unsigned sees[NR];   // (DRAFT: the nodes that the row looks at; at most 32 nodes here)
   bf16x8 q[NR][KS], kf[KS];
   RawRow<D> rq[TWO ? 1 : NR], rk;   // (TWO: one row block at a time, the others behind the first tiles: half the registers)
   f32x4 rv[2];       // (RAW) sums and bias of 8 elements of a fresh V row: the first of this thread's units (row, 8 elements)
@@ -104,6 +106,7 @@ __global__ __launch_bounds__(256, (FMT == 1 && (NR == 1 || !RAW)) || TWO ? 2 : 1
   for (int r = 0; r < NR; ++r) {
     const int row = min(r * 16 + l16, R - 1), hg = row / T, head = gkv * G + hg;
     my_i[r] = row - hg * T;
+    if constexpr (DRAFT) sees[r] = (unsigned)pc::draft_row(draft, b, T, my_i[r], 0);
     if constexpr (RAW) {
       if (!TWO || r == 0) load_q(rq[TWO ? 0 : r], r);
     } else {
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(256, (FMT == 1 && (NR == 1 || !RAW)) || TWO ? 2 : 1
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks], q[r][ks], s, 0, 0, 0);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = wave * 16 + g * 4 + e <= my_i[r] ? s[e] : -INFINITY;
+      for (int e = 0; e < 4; ++e) s[e] = (DRAFT ? (sees[r] >> (wave * 16 + g * 4 + e) & 1) != 0 : wave * 16 + g * 4 + e <= my_i[r]) ? s[e] : -INFINITY;
       pf[r] = soften(s, r);
     }
   }
@@ -485,13 +488,24 @@ __global__ __launch_bounds__(256, (FMT == 1 && (NR == 1 || !RAW)) || TWO ? 2 : 1
       for (int e = 0; e < 4; ++e) { acc[e] += lo[e] * a[w]; acc[4 + e] += hi[e] * a[w]; }
     }
     const int hg = row / T, i = row - hg * T;
+    const unsigned seen = DRAFT ? (unsigned)pc::draft_row(draft, b, T, i, 0) : 0u;
     if (with_fresh) {
       for (int t = 0; t <= i; ++t) {
+        if (DRAFT && !(seen >> t & 1)) continue;
         const float p = pl[row * 32 + t] * (t < 16 ? a[0] : a[1]);
         const bf16x8 v = *(const bf16x8 *)(vl + t * D + dv * 8);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] += p * (float)v[e];
       }
+    }
+    if constexpr (DRAFT) {
+      if (!seen) {   // (padding)
+        l = 0.f;
+        m = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+      }
+      if (n_splits == 1 && draft.lse && dv == 0) draft.lse[((size_t)b * Hq + gkv * G + hg) * T + i] = pc::lse_of(m, l);
     }
     const float inv = l > 0.f ? 1.0f / l : 0.f;
 #pragma unroll
@@ -535,7 +549,7 @@ static int decode_splits(int n_cu, int slots, long base_wgs, int tiles, int cap,
 
 pc_status launch_decode_attention(percache_ctx *ctx, int layer, const __bf16 *q, const __bf16 *kf, const __bf16 *vf, const RawQkv *raw, int batch, int t_fresh,
                                   const int32_t *table_dev, int tbl_stride, int tiles, int &n_splits, int merge_limit, __bf16 *out, float *part_o,
-                                  float *part_ml, hipStream_t stream, int formats) {
+                                  float *part_ml, hipStream_t stream, int formats, const DraftView *draft) {
   const percache_config &c = ctx->cfg;
   const int R = c.n_q_heads / c.n_kv_heads * t_fresh;
   const int fmt = !((formats & 1) && ctx->n_slots8 > 0) ? 0 : (formats & 2) ? 2 : 1;
@@ -559,7 +573,16 @@ pc_status launch_decode_attention(percache_ctx *ctx, int layer, const __bf16 *q,
 #define PC_DEC(DD, FF, RR, WW, TT)                                                                                                      \
   hipLaunchKernelGGL((decode_attention_kernel<DD, FF, RR, WW, TT>), grid, dim3(64 * NW), 0, stream, q, kf, vf, rq, k16, v16, k8, v8, ctx->k_scale + sc, \
                      ctx->v_scale + sc, ctx->n_slots16, table_dev, tbl_stride, t_fresh, c.n_q_heads, c.n_kv_heads, c.slot_capacity, n_splits,        \
-                     scale_log2e, out, part_o, part_ml)
+                     scale_log2e, out, part_o, part_ml, DraftView{})
+#define PC_DEC_DRAFT(DD, FF, RR, TT)                                                                                                     \
+  hipLaunchKernelGGL((decode_attention_kernel<DD, FF, RR, false, TT, true>), grid, dim3(64 * NW), 0, stream, q, kf, vf, rq, k16, v16, k8, v8, ctx->k_scale + sc, \
+                     ctx->v_scale + sc, ctx->n_slots16, table_dev, tbl_stride, t_fresh, c.n_q_heads, c.n_kv_heads, c.slot_capacity, n_splits,        \
+                     scale_log2e, out, part_o, part_ml, *draft)
+#define PC_DEC_DRAFT_R(DD, RR)                                                                                                           \
+  do {                                                                                                                                   \
+    if constexpr (DD == 128) { if (two && fmt == 2) { PC_DEC_DRAFT(DD, 2, RR, true); break; } }                                           \
+    if (fmt == 0) PC_DEC_DRAFT(DD, 0, RR, false); else if (fmt == 1) PC_DEC_DRAFT(DD, 1, RR, false); else PC_DEC_DRAFT(DD, 2, RR, false);     \
+  } while (0)
 #define PC_DEC_F(DD, RR, WW)                                                                                                             \
   do {                                                                                                                                   \
     if constexpr (DD == 128) {                                                                                                            \
@@ -573,7 +596,17 @@ pc_status launch_decode_attention(percache_ctx *ctx, int layer, const __bf16 *q,
     if (raw) { if (R <= 16) PC_DEC_F(DD, 1, true); else PC_DEC_F(DD, 2, true); }                     \
     else { if (R <= 16) PC_DEC_F(DD, 1, false); else PC_DEC_F(DD, 2, false); }                       \
   } while (0)
-  if (c.head_dim == 128) PC_DEC_D(128); else PC_DEC_D(64);
+  if (draft) {
+    if (c.head_dim == 128) { if (R <= 16) PC_DEC_DRAFT_R(128, 1); else PC_DEC_DRAFT_R(128, 2); }
+    else if (R <= 16) PC_DEC_DRAFT_R(64, 1);
+    else PC_DEC_DRAFT_R(64, 2);
+  } else if (c.head_dim == 128) {
+    PC_DEC_D(128);
+  } else {
+    PC_DEC_D(64);
+  }
+#undef PC_DEC_DRAFT_R
+#undef PC_DEC_DRAFT
 #undef PC_DEC_D
 #undef PC_DEC_F
 #undef PC_DEC

@@ -190,9 +190,10 @@ struct Store8 {
   float *k_scale, *v_scale;
   long slot_stride, scale_stride;
 };
-template <int D>
+// row_of: the dense row (of the entry's range) that holds new token i.
+template <int D, class RowOf>
 __device__ __forceinline__ void quant_block(const Store8 &st, const __bf16 *__restrict__ dense_k, const __bf16 *__restrict__ dense_v, int C, const Entry &ent,
-                                            int slot, int g, int head_rows) {
+                                            int slot, int g, int head_rows, RowOf row_of) {
   constexpr int HALF = D / 64;  // wavefronts of each kind
   __shared__ float red[2 * HALF];
   uint8_t *const __restrict__ slot_k = st.k, *const __restrict__ slot_v = st.v;
@@ -211,7 +212,7 @@ __device__ __forceinline__ void quant_block(const Store8 &st, const __bf16 *__re
   auto token = [&](int j) __attribute__((always_inline)) { return is_v ? chunk_key<true>(lo) + in_chunk(j) : hi + 8 * j; };  // inside the block
   pc::bf16x8 x[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = *(const pc::bf16x8 *)(src + (size_t)min(max(t0 + token(j) - off, 0), n_new - 1) * D);
+  for (int j = 0; j < 8; ++j) x[j] = *(const pc::bf16x8 *)(src + (size_t)row_of(min(max(t0 + token(j) - off, 0), n_new - 1)) * D);
   uint8_t *const kc = slot_k + slot_at + d, *const vc = slot_v + slot_at + (size_t)d * kKvTile + lo * 8;
   if (t0 < off) {  // (only the first block of an append) what the stored codes read back as, exact in bf16
     const float scale = (is_v ? scale_v : scale_k)[sc];
@@ -275,11 +276,49 @@ __device__ __forceinline__ void quant_block(const Store8 &st, const __bf16 *__re
   }
 }
 
+struct SameRow {
+  __device__ __forceinline__ int operator()(int i) const { return i; }
+};
+
 template <int D, class List>
 __global__ __launch_bounds__(2 * D) void kv_quant_kernel(Store8 st, const __bf16 *__restrict__ dense_k, const __bf16 *__restrict__ dense_v, int C, List list,
                                                          int head_rows) {
   const Entry e = list.at(blockIdx.z);
-  quant_block<D>(st, dense_k, dense_v, C, e, e.slot, blockIdx.y, head_rows);
+  quant_block<D>(st, dense_k, dense_v, C, e, e.slot, blockIdx.y, head_rows, SameRow{});
+}
+
+// The accepted nodes of a tree of drafted tokens into the slots of their sequences, in the order of the path: token start + j of query z's slot is
+// row path[j] of its dense tensors [Hkv][T][D]; what the slot held from token start on goes.  One workgroup a (query, kv head, 64-token block),
+// bf16 and 8-bit slots in one launch.  The lists travel as a launch argument, so a call is one launch: a few kilobytes a head, bound by its latency.
+struct PathWeights {
+  const float *draft;   // [B][Hkv][T]
+  float *out;           // [slots][Hkv][C], null: no weights
+};
+template <int D>
+__global__ __launch_bounds__(2 * D) void kv_path_kernel(Store16 s16, Store8 s8, int n_slots16, const __bf16 *__restrict__ dense_k, const __bf16 *__restrict__ dense_v,
+                                                        PathWeights w, int C, int T, const pc::ListWords lists, int record) {
+  const int z = blockIdx.z, g = blockIdx.y, Hkv = gridDim.y, tid = threadIdx.x;
+  const int32_t *rec = lists.v + z * record, *path = rec + 3;   // slot, start, number of nodes, the nodes
+  const int slot = rec[0], start = rec[1], n = rec[2], end = start + n;
+  const int blk = start / kKvTile + blockIdx.x, t0 = blk * kKvTile;
+  if (slot < 0 || t0 >= end) return;
+  const size_t row0 = ((size_t)z * Hkv + g) * T;
+  if (w.out && tid < kKvTile && t0 + tid >= start && t0 + tid < end)
+    w.out[((size_t)slot * Hkv + g) * C + t0 + tid] = w.draft[row0 + path[t0 + tid - start]];
+  if (slot >= n_slots16) {
+    const Entry e = {slot - n_slots16, z * Hkv * T, n, start};
+    quant_block<D>(s8, dense_k, dense_v, C, e, e.slot, g, T, [&](int i) { return n ? path[max(i, 0)] : 0; });
+    return;
+  }
+  const size_t head = (size_t)slot * s16.slot_stride + (size_t)g * C * D;
+  for (int e = tid; e < kKvTile * (D / 8); e += 2 * D) {
+    const int t = t0 + e / (D / 8), d = e % (D / 8) * 8;
+    if (t >= start && t < end) *(pc::u32x4 *)(s16.k + head + (size_t)t * D + d) = *(const pc::u32x4 *)(dense_k + (row0 + path[t - start]) * D + d);
+  }
+  for (int e = tid; e < kKvTile * D; e += 2 * D) {   // (zeros behind the last token: the padding stays finite)
+    const int p = e % kKvTile, d = e / kKvTile, t = t0 + (p & ~15) + pc::blocked_key(p & 15);
+    if (t >= start) s16.v[head + (size_t)t0 * D + e] = t < end ? dense_v[(row0 + path[t - start]) * D + d] : (__bf16)0.f;
+  }
 }
 
 // The values an 8-bit slot holds, as dense bf16 [kv head][token][head_dim]: code * 2^e (exact).  Work split as in
@@ -351,7 +390,7 @@ __global__ __launch_bounds__(2 * D) void kv_mixed_kernel(Store16 s16, Store8 s8,
   const Entry e = list.at(blockIdx.z);
   const int unit = blockIdx.x * (2 * D / 64) + (threadIdx.x >> 6);
   if (e.slot < n_slots16) copy_unit<D, kToStore>(s16, dense_k, dense_v, C, e, e.slot, blockIdx.y, unit, head_rows);
-  else if (kToStore) quant_block<D>(s8, dense_k, dense_v, C, e, e.slot - n_slots16, blockIdx.y, head_rows);
+  else if (kToStore) quant_block<D>(s8, dense_k, dense_v, C, e, e.slot - n_slots16, blockIdx.y, head_rows, SameRow{});
   else dequant_unit<D>(s8, dense_k, dense_v, C, e, e.slot - n_slots16, blockIdx.y, unit, head_rows);
 }
 
@@ -476,6 +515,22 @@ pc_status launch_kv_slices(percache_ctx *ctx, int layer, const int32_t *slots, c
     }
   return flush();
 }
+pc_status launch_kv_put_rows(percache_ctx *ctx, int layer, const int32_t *slots, const int32_t *lengths, int n, const __bf16 *k, const __bf16 *v, int rows,
+                             hipStream_t stream) {
+  const size_t per_slot = (size_t)ctx->cfg.n_kv_heads * rows * ctx->cfg.head_dim;
+  PieceList<kListMax> l;
+  for (int i0 = 0; i0 < n; i0 += kListMax) {
+    const int cnt = n - i0 < kListMax ? n - i0 : kListMax;
+    int longest = 0;
+    for (int i = 0; i < cnt; ++i) {
+      l.entry[i] = {slots[i0 + i], i * ctx->cfg.n_kv_heads * rows, lengths[i0 + i], 0};
+      if (lengths[i0 + i] > longest) longest = lengths[i0 + i];
+    }
+    const pc_status st = launch_copy<true>(ctx, layer, l, cnt, longest, (void *)(k + i0 * per_slot), (void *)(v + i0 * per_slot), rows, stream);
+    if (st != PC_OK) return st;
+  }
+  return PC_OK;
+}
 pc_status launch_kv_append(percache_ctx *ctx, int layer, const int32_t *slot_list, int n, bool only_8bit, const __bf16 *k, const __bf16 *v,
                            int n_tokens, hipStream_t stream) {
   const size_t per_slot = (size_t)ctx->cfg.n_kv_heads * n_tokens * ctx->cfg.head_dim;
@@ -504,6 +559,68 @@ pc_status percache_kv_append(percache_ctx *ctx, int32_t layer, int32_t slot, con
   st = pc::launch_kv_append(ctx, layer, &slot, 1, false, (const __bf16 *)k_dev, (const __bf16 *)v_dev, n_tokens, (hipStream_t)stream);
   if (st != PC_OK) return st;
   ctx->slot_len[(size_t)layer * c.n_slots + slot] = have + n_tokens;
+  return PC_OK;
+}
+
+pc_status percache_kv_append_path(percache_ctx *ctx, int32_t layer, const void *k_dev, const void *v_dev, int32_t batch, int32_t t_draft,
+                                  const int32_t *path_host, const int32_t *n_path_host, int32_t max_path, const int32_t *append_slots_host,
+                                  const int32_t *start_host, const float *draft_weights_dev, float *weights_dev, void *stream) {
+  if (!ctx) return PC_EINVAL;
+  const percache_config &c = ctx->cfg;
+  if (!k_dev || !v_dev) return pc::fail(ctx, PC_EINVAL, "k_dev / v_dev is NULL");
+  if (((uintptr_t)k_dev | (uintptr_t)v_dev) % 16) return pc::fail(ctx, PC_EINVAL, "k_dev / v_dev must be 16-byte aligned");
+  if (!draft_weights_dev != !weights_dev) return pc::fail(ctx, PC_EINVAL, "draft_weights_dev and weights_dev: both or neither");
+  if (((uintptr_t)draft_weights_dev | (uintptr_t)weights_dev) % sizeof(float)) return pc::fail(ctx, PC_EINVAL, "weights must be 4-byte aligned");
+  if (batch < 1 || t_draft < 1) return pc::fail(ctx, PC_EINVAL, "batch and t_draft must be positive");
+  if (!path_host || !append_slots_host) return pc::fail(ctx, PC_EINVAL, "path_host or append_slots_host is NULL");
+  if (layer < 0 || layer >= c.n_layers) return pc::fail(ctx, PC_ESLOT, "layer %d out of range [0,%d)", layer, c.n_layers);
+  pc_status st = pc::check_paths(ctx, batch, t_draft, path_host, n_path_host, max_path);
+  if (st != PC_OK) return st;
+  if ((long)batch * c.n_kv_heads * t_draft >= (1L << 31)) return pc::fail(ctx, PC_ESHAPE, "more than 2^31 rows");
+  std::vector<char> named(c.n_slots, 0);
+  std::vector<int32_t> start(batch, 0);
+  int longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int slot = append_slots_host[b];
+    if (slot < 0) continue;
+    if (slot >= c.n_slots) return pc::fail(ctx, PC_ESLOT, "slot %d out of range [0,%d)", slot, c.n_slots);
+    if (named[slot]++) return pc::fail(ctx, PC_EINVAL, "slot %d appears twice in the batch", slot);
+    const int have = ctx->slot_len[(size_t)layer * c.n_slots + slot];
+    start[b] = start_host ? start_host[b] : have;
+    if (start[b] < 0 || start[b] > have) return pc::fail(ctx, PC_ELEN, "query %d: start %d outside [0,%d]", b, start[b], have);
+    if ((long)start[b] + n_path_host[b] > c.slot_capacity)
+      return pc::fail(ctx, PC_ELEN, "slot %d: %d tokens behind %d do not fit the capacity %d", slot, n_path_host[b], start[b], c.slot_capacity);
+    if (n_path_host[b] > longest) longest = n_path_host[b];
+  }
+  const int record = longest + 3;
+  if (record > pc::kListWords) return pc::fail(ctx, PC_ESHAPE, "a path of %d nodes, at most %d are supported", longest, pc::kListWords - 3);
+  for (int b0 = 0, cnt; b0 < batch; b0 += cnt) {
+    cnt = pc::kListWords / record < batch - b0 ? pc::kListWords / record : batch - b0;
+    pc::ListWords lists;
+    int blocks = 0;
+    for (int z = 0; z < cnt; ++z) {
+      const int b = b0 + z, n = n_path_host[b], end = start[b] + n;
+      int32_t *rec = lists.v + z * record;
+      rec[0] = append_slots_host[b];
+      rec[1] = start[b];
+      rec[2] = n;
+      for (int j = 0; j < n && j < longest; ++j) rec[3 + j] = path_host[(size_t)b * max_path + j];
+      const int touched = rec[0] < 0 ? 0 : (end + kKvTile - 1) / kKvTile - start[b] / kKvTile;
+      if (touched > blocks) blocks = touched;
+    }
+    if (blocks == 0) continue;
+    const size_t at = (size_t)b0 * c.n_kv_heads * t_draft;
+    const __bf16 *k = (const __bf16 *)k_dev + at * c.head_dim, *v = (const __bf16 *)v_dev + at * c.head_dim;
+    const PathWeights w = {draft_weights_dev ? draft_weights_dev + at : nullptr, weights_dev};
+    const dim3 grid(blocks, c.n_kv_heads, cnt);
+    if (c.head_dim == 128)
+      hipLaunchKernelGGL(kv_path_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, store16(ctx, layer), store8(ctx, layer), ctx->n_slots16, k, v, w, c.slot_capacity, t_draft, lists, record);
+    else
+      hipLaunchKernelGGL(kv_path_kernel<64>, grid, dim3(128), 0, (hipStream_t)stream, store16(ctx, layer), store8(ctx, layer), ctx->n_slots16, k, v, w, c.slot_capacity, t_draft, lists, record);
+    PC_HIP(ctx, hipGetLastError());
+  }
+  for (int b = 0; b < batch; ++b)
+    if (append_slots_host[b] >= 0) ctx->slot_len[(size_t)layer * c.n_slots + append_slots_host[b]] = start[b] + n_path_host[b];
   return PC_OK;
 }
 

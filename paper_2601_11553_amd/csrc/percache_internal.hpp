@@ -59,6 +59,27 @@ struct ListWords {
   int32_t v[kListWords];
 };
 
+// Attention of drafted tokens: the fresh rows of a query are the nodes of a tree in which a node comes behind its parent.
+constexpr int kMaxNodes = 256;
+struct DraftView {
+  const uint2 *sees = nullptr;   // per node ceil(T / 64) words of 64 bits: the nodes it looks at, itself and its ancestors (none: it is padding);
+                                 // null: node i looks at nodes 0 .. i
+  float *lse = nullptr;          // [B][Hq][T] log-sum-exp of the scores a row looks at, -infinity if it looks at none; may be null
+};
+// the 64 nodes from t0 on (a multiple of 64) that node i of query b looks at
+__device__ __forceinline__ unsigned long long draft_row(const DraftView &d, int b, int T, int i, int t0) {
+  if (d.sees) {
+    const uint2 w = d.sees[((size_t)b * T + i) * ((T + 63) / 64) + t0 / 64];
+    return ((unsigned long long)w.y << 32) | w.x;
+  }
+  const int n = i - t0 + 1;
+  return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+}
+// a node's own bit: not set for padding
+__device__ __forceinline__ bool draft_live(const DraftView &d, int b, int T, int i) { return draft_row(d, b, T, i, i & ~63) >> (i & 63) & 1; }
+// log-sum-exp from a reference exponent m (log2) and the sum l of 2^(score - m)
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f; }
+
 // Size of the file-scope scratch array behind the entry points that allocate nothing.
 constexpr size_t kStaticScratchBytes = 1u << 20;
 
@@ -183,11 +204,13 @@ struct RawQkv {
 bool few_rows_qkv(const percache_ctx *ctx, long M, bool head_norm);
 pc_status launch_qkv_raw(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, int M, const QkvExtras &extras, float *sums, hipStream_t stream);
 // v_blk / v_blk_done: if given, the launch may also write V as the 64-key blocks of launch_v_repack and says so.
+// The position of token i of query b is table[b * tbl_stride + 1 + i * node_stride] + i: 0 for the cached length of a chunk table, 1 for
+// a table of the nodes' own positions (less i).
 // extras.pre_norm only where few_rows_qkv; raw: workspace of that case (M rows of fp32 sums) for a head norm.
 pc_status launch_qkv_rope(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, int batch, int t_fresh,
                           const int32_t *table_dev, int tbl_stride, __bf16 *q, __bf16 *k, __bf16 *v,
                           hipStream_t stream, const QkvExtras &extras = QkvExtras(), __bf16 *v_blk = nullptr,
-                          bool *v_blk_done = nullptr, float *raw = nullptr);
+                          bool *v_blk_done = nullptr, float *raw = nullptr, int node_stride = 0);
 
 pc_status launch_v_repack(percache_ctx *ctx, const __bf16 *vf, __bf16 *vf_blk, int batch, int t_fresh, hipStream_t stream);
 // Whether a call's attention takes the kernel for very few rows per kv head (decode_attention.hip), which reads the fresh V
@@ -198,15 +221,33 @@ inline bool decode_rows(const percache_config &c, int t_fresh) { return (long)(c
 // raw: q and the fresh k, v as the projection's sums instead (decode_rows only; q, kf, vf unused).
 // left_splits (decode_rows only): in, the most partials that the caller would merge itself; out, the number left to it, at 1 the
 // result is in out.
+// draft: the fresh rows are nodes of trees (min_tiles: cached tiles alone); its partials are fp32, rows x partitions x D, up to max_splits_for of them.
 pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const __bf16 *kf, const __bf16 *vf, const __bf16 *vf_blk,
                            const RawQkv *raw, int batch, int t_fresh, const int32_t *table_dev, int tbl_stride, int max_tiles,
                            int n_splits, __bf16 *out, void *part_o, float *part_ml, hipStream_t stream, int formats,
-                           int *left_splits = nullptr);
+                           int *left_splits = nullptr, const DraftView *draft = nullptr);
 // The first of its two launches where decode_rows; tiles: cached tiles of the shortest query.  n_splits <= 0: chosen here
 // (merge_limit: up to so many partials are left to the o_proj, more are merged by a launch of their own).
 pc_status launch_decode_attention(percache_ctx *ctx, int layer, const __bf16 *q, const __bf16 *kf, const __bf16 *vf, const RawQkv *raw, int batch, int t_fresh,
                                   const int32_t *table_dev, int tbl_stride, int tiles, int &n_splits, int merge_limit, __bf16 *out, float *part_o,
-                                  float *part_ml, hipStream_t stream, int formats);
+                                  float *part_ml, hipStream_t stream, int formats, const DraftView *draft = nullptr);
+// Validates the parents of a batch of trees (null: every node's parent is the node before it) and, if given, the paths through them.
+pc_status check_trees(percache_ctx *ctx, int32_t batch, int32_t t_draft, const int32_t *parents);
+pc_status check_paths(percache_ctx *ctx, int32_t batch, int32_t t_draft, const int32_t *path, const int32_t *n_path, int32_t max_path);
+// Workspace of the calls on drafted tokens.
+struct DraftWs {
+  int32_t *words;   // the lists of a call: see draft.hip, attention_weights.hip
+  uint2 *sees;      // DraftView::sees (trees only)
+  float *part_o, *part_ml;
+  size_t total;
+};
+DraftWs carve_draft_ws(const percache_config &cfg, int n_cu, void *base, int32_t batch, int32_t t_draft, int32_t max_chunks);
+// Brings the words of a call to the device and, if there are parents, makes the trees' DraftView::sees.
+pc_status upload_draft(percache_ctx *ctx, std::vector<int32_t> &words, int batch, int t_draft, const int32_t *parents, const DraftWs &ws, hipStream_t stream);
+
+// Merges the fp32 partials of the cached keys (n_splits of them a row; 0: none) and, where q is given, the nodes that each row looks at.
+pc_status launch_draft_merge(percache_ctx *ctx, const float *part_o, const float *part_ml, int n_splits, const __bf16 *q, const __bf16 *k, const __bf16 *v, int batch, int T,
+                             const DraftView &draft, __bf16 *out, hipStream_t stream);
 // Number of key-axis partitions that fills `slots` resident workgroups best (at least 4 tiles in each).
 int choose_splits(int slots, long base_wgs, int min_tiles, int cap);
 inline int table_formats(const std::vector<int32_t> &rows, int stride, int batch) {
@@ -219,6 +260,10 @@ inline int table_formats(const std::vector<int32_t> &rows, int stride, int batch
 // in slot slots[b * n_pieces + j] (negative: skipped), one launch per 64 pieces (no validation, no slot-table update).
 pc_status launch_kv_slices(percache_ctx *ctx, int layer, const int32_t *slots, const int32_t *bounds, int n_pieces, int batch, const __bf16 *k,
                            const __bf16 *v, int seq_len, hipStream_t stream);
+
+// Stores the first lengths[i] tokens of dense tensor i of [n][Hkv][rows][D] in slot slots[i] (no validation, no slot-table update).
+pc_status launch_kv_put_rows(percache_ctx *ctx, int layer, const int32_t *slots, const int32_t *lengths, int n, const __bf16 *k, const __bf16 *v, int rows,
+                             hipStream_t stream);
 
 // Appends n_tokens tokens of every dense tensor of [n][Hkv][n_tokens][D] behind the tokens that the slot of the same place
 // in the list holds (by the slot table; no validation, no slot-table update).  Negative entries are skipped, and with

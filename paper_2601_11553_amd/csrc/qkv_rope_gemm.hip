@@ -23,7 +23,7 @@ using pc::gemm::pack4;
 template <int D, int NTB, bool EXTRA, bool WIDE = false>
 __global__ __launch_bounds__(WIDE ? 512 : 256, WIDE ? 1 : 2) void qkv_rope_kernel(const __bf16 *__restrict__ X, const __bf16 *__restrict__ W, int M,
                                                           int H, int t_fresh, int Hq, int Hkv,
-                                                          const int32_t *__restrict__ table, int tbl_stride,
+                                                          const int32_t *__restrict__ table, int tbl_stride, int node_stride,
                                                           const float2 *__restrict__ rope, __bf16 *__restrict__ Q,
                                                           __bf16 *__restrict__ K, __bf16 *__restrict__ V, pc::QkvExtras ex,
                                                           __bf16 *__restrict__ V_blk) {
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, WIDE ? 1 : 2) void qkv_rope_kerne
     const bool m_ok = m_raw < M;
     const int m = m_ok ? m_raw : M - 1;
     const int b = m / t_fresh, i = m - b * t_fresh;
-    const int pos = table[(size_t)b * tbl_stride + 1] + i;
+    const int pos = table[(size_t)b * tbl_stride + 1 + i * node_stride] + i;
     __bf16 *row = dst + (((size_t)b * n_heads + hh) * t_fresh + i) * D;
     // all sixteen (cos, sin) pairs of this lane's token first (eight 16-byte loads in flight), then the math
     float4 cs[4][2];
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, WIDE ? 1 : 2) void qkv_rope_kerne
 template <int D, int NF, int NT, bool NORM>
 __global__ __launch_bounds__((64 * pc::few::Form<NF, NT>::WV)) void qkv_rope_few_kernel(
     const __bf16 *__restrict__ X, const __bf16 *__restrict__ W, int M, int H, int t_fresh, int Hq, int Hkv, const int32_t *__restrict__ table,
-    int tbl_stride, const float2 *__restrict__ rope, __bf16 *__restrict__ Q, __bf16 *__restrict__ K, __bf16 *__restrict__ V, pc::QkvExtras ex,
+    int tbl_stride, int node_stride, const float2 *__restrict__ rope, __bf16 *__restrict__ Q, __bf16 *__restrict__ K, __bf16 *__restrict__ V, pc::QkvExtras ex,
     __bf16 *__restrict__ V_blk, int n_wt, int n_tt) {
   constexpr int WV = pc::few::Form<NF, NT>::WV, NSTG = pc::few::Form<NF, NT>::NSTG;
   constexpr int PAIRS = NF == 1 ? 8 : 8 * NF, TPH = D / 2 / PAIRS, NFP = NF == 1 ? 1 : NF / 2, PER = (NFP * NT + WV - 1) / WV;
@@ -204,7 +204,7 @@ __global__ __launch_bounds__((64 * pc::few::Form<NF, NT>::WV)) void qkv_rope_few
     q_b[j] = m / t_fresh;
     q_i[j] = m - q_b[j] * t_fresh;
     first[j] = sub * PAIRS + (NF == 1 ? 4 * (g & 1) : b / NT * 16 + 4 * g);  // first of this lane's 4 consecutive pairs
-    l_pre[j] = rotate ? table[(size_t)q_b[j] * tbl_stride + 1] : 0;
+    l_pre[j] = rotate ? table[(size_t)q_b[j] * tbl_stride + 1 + q_i[j] * node_stride] : 0;
   }
   f32x4 acc[NF][NT];
   float ss[NT];
@@ -306,7 +306,7 @@ __global__ __launch_bounds__((64 * pc::few::Form<NF, NT>::WV)) void qkv_rope_few
 // 264 rows of 16 heads).
 template <int D>
 __global__ __launch_bounds__(256) void finish_rope_kernel(const float *__restrict__ sums, int batch, int t_fresh, int rows, int Hq, int Hkv,
-                                                          const int32_t *__restrict__ table, int tbl_stride, const float2 *__restrict__ rope,
+                                                          const int32_t *__restrict__ table, int tbl_stride, int node_stride, const float2 *__restrict__ rope,
                                                           __bf16 *__restrict__ Q, __bf16 *__restrict__ K, __bf16 *__restrict__ V, pc::QkvExtras ex,
                                                           __bf16 *__restrict__ V_blk) {
   constexpr int QUADS = D / 8;
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(256) void finish_rope_kernel(const float *__restric
     }
   }
   if (rotate) {
-    const f32x4 *p = (const f32x4 *)(rope + (size_t)(table[(size_t)b * tbl_stride + 1] + i) * (D / 2) + mm);
+    const f32x4 *p = (const f32x4 *)(rope + (size_t)(table[(size_t)b * tbl_stride + 1 + i * node_stride] + i) * (D / 2) + mm);
     const f32x4 c01 = p[0], c23 = p[1];  // (cos, sin) of pairs mm, mm+1 and mm+2, mm+3
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -437,7 +437,7 @@ pc_status launch_qkv_raw(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, in
 
 pc_status launch_qkv_rope(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, int batch, int t_fresh,
                           const int32_t *table_dev, int tbl_stride, __bf16 *q, __bf16 *k, __bf16 *v,
-                          hipStream_t stream, const QkvExtras &extras, __bf16 *v_blk, bool *v_blk_done, float *raw) {
+                          hipStream_t stream, const QkvExtras &extras, __bf16 *v_blk, bool *v_blk_done, float *raw, int node_stride) {
   if (v_blk_done) *v_blk_done = false;
   const percache_config &c = ctx->cfg;
   const int M = batch * t_fresh;
@@ -457,7 +457,7 @@ pc_status launch_qkv_rope(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, i
       const long threads = (long)batch * rows * (c.n_q_heads + 2 * c.n_kv_heads) * (c.head_dim / 8);
 #define PC_FINISH(DD)                                                                                                                   \
   hipLaunchKernelGGL(finish_rope_kernel<DD>, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, stream, raw, batch, t_fresh, rows, c.n_q_heads, \
-                     c.n_kv_heads, table_dev, tbl_stride, rope, q, k, v, extras, vb)
+                     c.n_kv_heads, table_dev, tbl_stride, node_stride, rope, q, k, v, extras, vb)
       if (c.head_dim == 128) PC_FINISH(128); else PC_FINISH(64);
 #undef PC_FINISH
       prof_end(ctx, PC_KERNEL_QKV_ROPE, stream);
@@ -469,7 +469,7 @@ pc_status launch_qkv_rope(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, i
     prof_begin(ctx, PC_KERNEL_QKV_ROPE, stream);
 #define PC_FEW_K(DD, NF, NT, NN)                                                                                                \
   hipLaunchKernelGGL((qkv_rope_few_kernel<DD, NF, NT, NN>), dim3(few::grid_of(n_wt, n_tt)), dim3(64 * few::Form<NF, NT>::WV), 0, stream, x, w, \
-                     M, c.hidden, t_fresh, c.n_q_heads, c.n_kv_heads, table_dev, tbl_stride, rope, q, k, v, extras, vb, n_wt, n_tt)
+                     M, c.hidden, t_fresh, c.n_q_heads, c.n_kv_heads, table_dev, tbl_stride, node_stride, rope, q, k, v, extras, vb, n_wt, n_tt)
 #define PC_FEW(DD, NF, NT)                                                                          \
   if (ch.nf == NF && ch.nt == NT) {                                                                 \
     if (extras.pre_norm) PC_FEW_K(DD, NF, NT, true); else PC_FEW_K(DD, NF, NT, false);               \
@@ -522,7 +522,7 @@ pc_status launch_qkv_rope(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, i
     PC_HIP(ctx, hipFuncSetAttribute((const void *)qkv_rope_kernel<128, NN, false, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes));      \
     prof_begin(ctx, PC_KERNEL_QKV_ROPE, stream);                                                                                                     \
     hipLaunchKernelGGL((qkv_rope_kernel<128, NN, false, true>), dim3(n_heads_all / 2, (M + 64 * NN - 1) / (64 * NN)), dim3(512), lds_bytes, stream, x, w, \
-                       M, c.hidden, t_fresh, c.n_q_heads, c.n_kv_heads, table_dev, tbl_stride, rope, q, k, v, extras, vb_large);                       \
+                       M, c.hidden, t_fresh, c.n_q_heads, c.n_kv_heads, table_dev, tbl_stride, node_stride, rope, q, k, v, extras, vb_large);                       \
   } while (0)
     if (wide == 3) PC_WIDE(3); else if (wide == 4) PC_WIDE(4); else PC_WIDE(5);
 #undef PC_WIDE
@@ -537,7 +537,7 @@ pc_status launch_qkv_rope(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, i
     if (lds_bytes > 64 * 1024) /* above the default limit: opt in */                                                  \
       PC_HIP(ctx, hipFuncSetAttribute((const void *)qkv_rope_kernel<DD, NN, EE>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes)); \
     hipLaunchKernelGGL((qkv_rope_kernel<DD, NN, EE>), grid, dim3(256), lds_bytes, stream, x, w, M, c.hidden, t_fresh,  \
-                       c.n_q_heads, c.n_kv_heads, table_dev, tbl_stride, rope, q, k, v, extras, vb_large);            \
+                       c.n_q_heads, c.n_kv_heads, table_dev, tbl_stride, node_stride, rope, q, k, v, extras, vb_large);            \
   } while (0)
 #define PC_LAUNCH(DD, NN)                                                                                             \
   do {                                                                                                                \
