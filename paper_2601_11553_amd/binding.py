@@ -106,13 +106,13 @@ def load_library() -> ctypes.CDLL:
         "percache_stack_reuse_table": (_i32, [_vp, ctypes.POINTER(BlockWeights), _i32, _i32, ctypes.c_float, _vp, _i32, _i32,
                                               _vp, _vp, _vp, _sz, _vp]),
         "percache_draft_workspace_bytes": (_sz, [_vp, _i32, _i32, _i32]),
-        "percache_qkv_rope_draft": (_i32, [_vp, _vp, _vp, _i32, _i32, _pi32, _pi32, _vp, _vp, _vp, _vp, _sz, _vp]),
-        "percache_attention_draft": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _pi32, _pi32, _pi32, _i32, _pi32, _i32, _vp, _vp, _vp, _sz, _vp]),
-        "percache_attention_weights": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _pi32, _pi32, _pi32, _i32, _pi32, _pi32, _pi32, _i32, _vp, _vp, _vp,
-                                              _vp, _sz, _vp]),
-        "percache_kv_append_path": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, _pi32, _pi32, _i32, _pi32, _pi32, _vp, _vp, _vp]),
+        # (their host lists as plain addresses: a pointer object costs a microsecond or two, of a call of about twenty)
+        "percache_qkv_rope_draft": (_i32, [_vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+        "percache_attention_draft": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _sz, _vp]),
+        "percache_attention_weights": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
+        "percache_kv_append_path": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
         "percache_kv_keep_workspace_bytes": (_sz, [_vp, _i32, _i32]),
-        "percache_kv_keep": (_i32, [_vp, _i32, _pi32, _pi32, _i32, _pi32, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
+        "percache_kv_keep": (_i32, [_vp, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
         "percache_kv_slice": (_i32, [_vp, _i32, _vp, _vp, _i32, _pi32, _pi32, _i32, _vp]),
         "percache_kv_append": (_i32, [_vp, _i32, _i32, _vp, _vp, _i32, _vp]),
         "percache_stack_decode": (_i32, [_vp, ctypes.POINTER(BlockWeights), _i32, _i32, ctypes.c_float, _vp, _i32, _i32,
@@ -160,6 +160,16 @@ def _host_i32(a, shape=None):
     return arr, arr.ctypes.data_as(_pi32)
 
 
+def _i32_list(a, shape=None):
+    """A host list as a contiguous int32 array (of the shape) and its address; (None, None) for None."""
+    if a is None:
+        return None, None
+    arr = a if type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous else np.ascontiguousarray(a, dtype=np.int32)
+    if shape is not None and arr.shape != shape:
+        arr = arr.reshape(shape)
+    return arr, arr.__array_interface__["data"][0]
+
+
 class Percache:
     """One context = one arena (a torch uint8 CUDA tensor) + host bookkeeping.  Methods mirror the C calls."""
 
@@ -191,6 +201,7 @@ class Percache:
         self._lookup_ws = None
         self._topk_ws = None
         self._draft_ws = None
+        self._draft_bytes = {}
 
     # ------------------------------------------------------------------ helpers
     def _check(self, st: int):
@@ -491,73 +502,95 @@ class Percache:
             self._draft_ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         return (self._draft_ws.data_ptr() + 255) // 256 * 256
 
+    def _draft_need(self, batch, t_draft, max_chunks) -> int:
+        key = (batch, t_draft, max_chunks)
+        if key not in self._draft_bytes:
+            self._draft_bytes[key] = self.lib.percache_draft_workspace_bytes(self.ctx, *key)
+        return self._draft_bytes[key]
+
+    def _raw_stream(self):
+        import torch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+
     def _want(self, name, t, shape, dtype):
         """The kernels read dense rows: a tensor of another shape, type or stride order is refused, not reinterpreted."""
-        if t is not None and (t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device.type != self.device.type):
-            raise ValueError(f"{name}: a contiguous {dtype} tensor {shape} on {self.device.type} is wanted, got {t.dtype} {tuple(t.shape)} "
+        if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda):
+            raise ValueError(f"{name}: a contiguous {dtype} tensor {shape} on the GPU is wanted, got {t.dtype} {tuple(t.shape)} "
                              f"{'' if t.is_contiguous() else 'not contiguous '}on {t.device}")
 
-    def _want_weights(self, *named):
-        import torch
-        c = self.cfg
-        for name, t in named:
-            self._want(name, t, (c.n_slots, c.n_kv_heads, c.slot_capacity), torch.float32)
-
-    def _want_draft(self, batch, t_draft, q=None, k=None, v=None):
-        import torch
-        c = self.cfg
-        self._want("q", q, (batch, c.n_q_heads, t_draft, c.head_dim), torch.bfloat16)
-        self._want("k", k, (batch, c.n_kv_heads, t_draft, c.head_dim), torch.bfloat16)
-        self._want("v", v, (batch, c.n_kv_heads, t_draft, c.head_dim), torch.bfloat16)
+    def _draft_chunks(self, batch, slot_ids, used_len, n_chunks):
+        if slot_ids is None:
+            ids, ids_p, max_chunks = None, None, 0
+        else:
+            ids, ids_p = _i32_list(slot_ids)
+            max_chunks = ids.size // batch if batch > 0 else 0
+            if ids.size != batch * max_chunks:
+                raise ValueError(f"slot_ids: {ids.size} entries for {batch} queries")
+        ul, ul_p = _i32_list(used_len, (batch, max_chunks))
+        nc, nc_p = _i32_list(n_chunks if n_chunks is not None else np.full(batch, max_chunks, np.int32), (batch,))
+        return (ids, ul, nc), ids_p, ul_p, nc_p, max_chunks
 
     @staticmethod
     def _path_args(path, n_path, batch):
         if path is None:
             return None, None, None, 0
-        path, path_p = _host_i32(path)
-        path = path.reshape(batch, -1)
-        n_path, n_path_p = _host_i32(np.full(batch, path.shape[1], np.int32) if n_path is None else n_path, (batch,))
-        return (path, n_path), path_p, n_path_p, path.shape[1]
+        path, path_p = _i32_list(path)
+        max_path = path.size // batch if batch > 0 else 0
+        if path.size != batch * max_path:
+            raise ValueError(f"path: {path.size} entries for {batch} queries")
+        n_path, n_path_p = _i32_list(np.full(batch, max_path, np.int32) if n_path is None else n_path, (batch,))
+        return (path, n_path), path_p, n_path_p, max_path
 
     def percache_qkv_rope_draft(self, x, wqkv, pos0, parents=None, q_out=None, k_out=None, v_out=None):
         """x [B, T, hidden]; parents [B, T] (-1: behind the tokens before the tree, -2: padding) or None for a sequence; pos0 [B]."""
         import torch
+        bf16 = torch.bfloat16
         batch, t_draft, _ = x.shape
-        par, par_p = _host_i32(parents, (batch, t_draft))
-        p0, p0_p = _host_i32(pos0, (batch,))
+        par, par_p = _i32_list(parents, (batch, t_draft))
+        p0, p0_p = _i32_list(pos0, (batch,))
         c = self.cfg
+        Hq, Hkv, D, H = c.n_q_heads, c.n_kv_heads, c.head_dim, c.hidden
+        self._want("x", x, (batch, t_draft, H), bf16)
+        self._want("wqkv", wqkv, ((Hq + 2 * Hkv) * D, H), bf16)
         if q_out is None:
-            q_out = torch.empty((batch, c.n_q_heads, t_draft, c.head_dim), dtype=torch.bfloat16, device=self.device)
-            k_out = torch.empty((batch, c.n_kv_heads, t_draft, c.head_dim), dtype=torch.bfloat16, device=self.device)
-            v_out = torch.empty_like(k_out)
-        self._want("x", x, (batch, t_draft, c.hidden), torch.bfloat16)
-        self._want("wqkv", wqkv, ((c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, c.hidden), torch.bfloat16)
-        self._want_draft(batch, t_draft, q_out, k_out, v_out)
-        need = self.lib.percache_draft_workspace_bytes(self.ctx, batch, t_draft, 0)
-        ws = self._draft_workspace(need)
-        self._check(self.lib.percache_qkv_rope_draft(self.ctx, _ptr(x), _ptr(wqkv), batch, t_draft, par_p, p0_p, _ptr(q_out), _ptr(k_out), _ptr(v_out),
-                                                     ws, need, _stream()))
+            q_out = torch.empty((batch, Hq, t_draft, D), dtype=bf16, device=self.device)
+            k_out = torch.empty((batch, Hkv, t_draft, D), dtype=bf16, device=self.device)
+            v_out = torch.empty((batch, Hkv, t_draft, D), dtype=bf16, device=self.device)
+        else:
+            self._want("q_out", q_out, (batch, Hq, t_draft, D), bf16)
+            self._want("k_out", k_out, (batch, Hkv, t_draft, D), bf16)
+            self._want("v_out", v_out, (batch, Hkv, t_draft, D), bf16)
+        need = self._draft_need(batch, t_draft, 0)
+        st = self.lib.percache_qkv_rope_draft(self.ctx, x.data_ptr(), wqkv.data_ptr(), batch, t_draft, par_p, p0_p, q_out.data_ptr(), _ptr(k_out), _ptr(v_out),
+                                              self._draft_workspace(need), need, self._raw_stream())
+        self._check(st)
         return q_out, k_out, v_out
 
     def percache_attention_draft(self, layer, q, k_draft, v_draft, slot_ids=None, used_len=None, n_chunks=None, parents=None, n_splits: int = 0,
                                  attn_out=None, lse_out=None):
         """(attn_out [B, T, Hq * D], lse [B, Hq, T] or None).  lse_out: a float32 tensor, True for a new one, None for none."""
         import torch
+        bf16 = torch.bfloat16
         batch, _, t_draft, _ = q.shape
-        keep, ids_p, ul_p, nc_p, max_chunks = self._chunk_args(batch, slot_ids, used_len, n_chunks)
-        par, par_p = _host_i32(parents, (batch, t_draft))
         c = self.cfg
+        Hq, Hkv, D = c.n_q_heads, c.n_kv_heads, c.head_dim
+        self._want("q", q, (batch, Hq, t_draft, D), bf16)
+        self._want("k", k_draft, (batch, Hkv, t_draft, D), bf16)
+        self._want("v", v_draft, (batch, Hkv, t_draft, D), bf16)
+        keep, ids_p, ul_p, nc_p, max_chunks = self._draft_chunks(batch, slot_ids, used_len, n_chunks)
+        par, par_p = _i32_list(parents, (batch, t_draft))
         if attn_out is None:
-            attn_out = torch.empty((batch, t_draft, c.n_q_heads * c.head_dim), dtype=torch.bfloat16, device=self.device)
+            attn_out = torch.empty((batch, t_draft, Hq * D), dtype=bf16, device=self.device)
+        else:
+            self._want("attn_out", attn_out, (batch, t_draft, Hq * D), bf16)
         if lse_out is True:
-            lse_out = torch.empty((batch, c.n_q_heads, t_draft), dtype=torch.float32, device=self.device)
-        self._want_draft(batch, t_draft, q, k_draft, v_draft)
-        self._want("attn_out", attn_out, (batch, t_draft, c.n_q_heads * c.head_dim), torch.bfloat16)
-        self._want("lse_out", lse_out, (batch, c.n_q_heads, t_draft), torch.float32)
-        need = self.lib.percache_draft_workspace_bytes(self.ctx, batch, t_draft, max_chunks)
-        ws = self._draft_workspace(need)
-        self._check(self.lib.percache_attention_draft(self.ctx, layer, _ptr(q), _ptr(k_draft), _ptr(v_draft), batch, t_draft, ids_p, ul_p, nc_p, max_chunks,
-                                                      par_p, n_splits, _ptr(attn_out), _ptr(lse_out), ws, need, _stream()))
+            lse_out = torch.empty((batch, Hq, t_draft), dtype=torch.float32, device=self.device)
+        else:
+            self._want("lse_out", lse_out, (batch, Hq, t_draft), torch.float32)
+        need = self._draft_need(batch, t_draft, max_chunks)
+        st = self.lib.percache_attention_draft(self.ctx, layer, q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(), batch, t_draft, ids_p, ul_p, nc_p, max_chunks,
+                                               par_p, n_splits, attn_out.data_ptr(), _ptr(lse_out), self._draft_workspace(need), need, self._raw_stream())
+        self._check(st)
         return attn_out, lse_out
 
     def percache_attention_weights(self, layer, q, k_draft, lse, weights_in, weights_out, slot_ids=None, used_len=None, n_chunks=None, parents=None,
@@ -566,49 +599,60 @@ class Percache:
         weights_out; returns the weights of the draft keys [B, Hkv, T] (None where k_draft is None)."""
         import torch
         batch, _, t_draft, _ = q.shape
-        keep, ids_p, ul_p, nc_p, max_chunks = self._chunk_args(batch, slot_ids, used_len, n_chunks)
-        par, par_p = _host_i32(parents, (batch, t_draft))
+        c = self.cfg
+        Hq, Hkv, D = c.n_q_heads, c.n_kv_heads, c.head_dim
+        self._want("q", q, (batch, Hq, t_draft, D), torch.bfloat16)
+        self._want("k", k_draft, (batch, Hkv, t_draft, D), torch.bfloat16)
+        self._want("lse", lse, (batch, Hq, t_draft), torch.float32)
+        self._want("weights_in", weights_in, (c.n_slots, Hkv, c.slot_capacity), torch.float32)
+        self._want("weights_out", weights_out, (c.n_slots, Hkv, c.slot_capacity), torch.float32)
+        keep, ids_p, ul_p, nc_p, max_chunks = self._draft_chunks(batch, slot_ids, used_len, n_chunks)
+        par, par_p = _i32_list(parents, (batch, t_draft))
         paths, path_p, n_path_p, max_path = self._path_args(path, n_path, batch)
-        if draft_weights is None and k_draft is not None:
-            draft_weights = torch.empty((batch, self.cfg.n_kv_heads, t_draft), dtype=torch.float32, device=self.device)
-        self._want_draft(batch, t_draft, q, k_draft)
-        self._want("lse", lse, (batch, self.cfg.n_q_heads, t_draft), torch.float32)
-        self._want("draft_weights", draft_weights, (batch, self.cfg.n_kv_heads, t_draft), torch.float32)
-        self._want_weights(("weights_in", weights_in), ("weights_out", weights_out))
-        need = self.lib.percache_draft_workspace_bytes(self.ctx, batch, t_draft, max_chunks)
-        ws = self._draft_workspace(need)
-        self._check(self.lib.percache_attention_weights(self.ctx, layer, _ptr(q), _ptr(k_draft), _ptr(lse), batch, t_draft, ids_p, ul_p, nc_p, max_chunks,
-                                                        par_p, path_p, n_path_p, max_path, _ptr(weights_in), _ptr(weights_out), _ptr(draft_weights),
-                                                        ws, need, _stream()))
+        if draft_weights is not None:
+            self._want("draft_weights", draft_weights, (batch, Hkv, t_draft), torch.float32)
+        elif k_draft is not None:
+            draft_weights = torch.empty((batch, Hkv, t_draft), dtype=torch.float32, device=self.device)
+        need = self._draft_need(batch, t_draft, max_chunks)
+        st = self.lib.percache_attention_weights(self.ctx, layer, q.data_ptr(), _ptr(k_draft), _ptr(lse), batch, t_draft, ids_p, ul_p, nc_p, max_chunks, par_p,
+                                                 path_p, n_path_p, max_path, _ptr(weights_in), _ptr(weights_out), _ptr(draft_weights),
+                                                 self._draft_workspace(need), need, self._raw_stream())
+        self._check(st)
         return draft_weights
 
     def percache_kv_append_path(self, layer, k, v, append_slots, path, n_path=None, start=None, weights=None, draft_weights=None):
         """k, v [B, Hkv, T, D]: the nodes of each query's path behind token start[b] (None: the last one) of slot append_slots[b] (< 0: skipped)."""
         import torch
         batch, _, t_draft, _ = k.shape
-        self._want_draft(batch, t_draft, None, k, v)
-        self._want("draft_weights", draft_weights, (batch, self.cfg.n_kv_heads, t_draft), torch.float32)
-        self._want_weights(("weights", weights))
+        c = self.cfg
+        for name, t in (("k", k), ("v", v)):
+            self._want(name, t, (batch, c.n_kv_heads, t_draft, c.head_dim), torch.bfloat16)
+        self._want("draft_weights", draft_weights, (batch, c.n_kv_heads, t_draft), torch.float32)
+        self._want("weights", weights, (c.n_slots, c.n_kv_heads, c.slot_capacity), torch.float32)
         paths, path_p, n_path_p, max_path = self._path_args(path, n_path, batch)
-        sl, sl_p = _host_i32(append_slots, (batch,))
-        st, st_p = _host_i32(start, (batch,))
-        self._check(self.lib.percache_kv_append_path(self.ctx, layer, _ptr(k), _ptr(v), batch, t_draft, path_p, n_path_p, max_path, sl_p, st_p,
-                                                     _ptr(draft_weights), _ptr(weights), _stream()))
+        sl, sl_p = _i32_list(append_slots, (batch,))
+        st, st_p = _i32_list(start, (batch,))
+        self._check(self.lib.percache_kv_append_path(self.ctx, layer, k.data_ptr(), v.data_ptr(), batch, t_draft, path_p, n_path_p, max_path, sl_p, st_p,
+                                                     _ptr(draft_weights), _ptr(weights), self._raw_stream()))
 
     def percache_kv_keep(self, layer, slots, keep, weights, n_first: int = 0, n_last: int = 0, dst_slots=None, idx_out=None):
         """Cuts each slot to keep (an int or one per slot) tokens per kv head, by weight; returns the kept tokens' indexes [n, Hkv, max keep]."""
         import torch
-        sl, sl_p = _host_i32(slots)
-        dst, dst_p = _host_i32(dst_slots, (len(sl),))
-        kp, kp_p = _host_i32(np.broadcast_to(np.asarray(keep, np.int32), (len(sl),)))
-        most = int(kp.max()) if len(kp) else 0
+        sl, sl_p = _i32_list(slots)
+        n = sl.size
+        dst, dst_p = _i32_list(dst_slots, (n,))
+        kp, kp_p = _i32_list(np.full(n, keep, np.int32) if np.ndim(keep) == 0 else keep, (n,))
+        most = int(kp.max()) if n else 0
+        c = self.cfg
+        self._want("weights", weights, (c.n_slots, c.n_kv_heads, c.slot_capacity), torch.float32)
         if idx_out is None:
-            idx_out = torch.empty((len(sl), self.cfg.n_kv_heads, max(most, 0)), dtype=torch.int32, device=self.device)
-        self._want_weights(("weights", weights))
-        self._want("idx_out", idx_out, (len(sl), self.cfg.n_kv_heads, max(most, 0)), torch.int32)
-        need = self.lib.percache_kv_keep_workspace_bytes(self.ctx, len(sl), most)
-        ws = self._draft_workspace(need)
-        self._check(self.lib.percache_kv_keep(self.ctx, layer, sl_p, dst_p, len(sl), kp_p, n_first, n_last, _ptr(weights), _ptr(idx_out), ws, need, _stream()))
+            idx_out = torch.empty((n, c.n_kv_heads, max(most, 0)), dtype=torch.int32, device=self.device)
+        else:
+            self._want("idx_out", idx_out, (n, c.n_kv_heads, max(most, 0)), torch.int32)
+        need = self.lib.percache_kv_keep_workspace_bytes(self.ctx, n, most)
+        st = self.lib.percache_kv_keep(self.ctx, layer, sl_p, dst_p, n, kp_p, n_first, n_last, _ptr(weights), idx_out.data_ptr(), self._draft_workspace(need), need,
+                                       self._raw_stream())
+        self._check(st)
         return idx_out
 
     # ------------------------------------------------------------------ stack of layers on the retained rows

@@ -4,7 +4,7 @@
 // Selection is integer work on the order-preserving bits of the weights, so it is exact and the same on every run: a radix search for the
 // smallest kept weight, 8 bits a pass over an LDS histogram, then one pass in the order of the tokens that takes everything above it and, of
 // those equal to it, the first ones.
-#include "percache_internal.hpp"
+#include "fp8_codes.hpp"
 
 namespace {
 using pc::kKvTile;
@@ -21,12 +21,15 @@ __device__ __forceinline__ unsigned key_of(float w) {
   return (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-constexpr int kSelThreads = 256;
+constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelLds = 8192;
 // One workgroup a (kv head, slot).  idx [n][Hkv][idx_stride]: the kept tokens in order, -1 behind them; weights are moved along.
+// Four passes over a few thousand keys and one over the tokens, each a few LDS accesses and barriers: a chain of latencies, so the keys are read from memory
+// once, into LDS (slots of up to kSelLds tokens; longer ones are read again from the L2).  2048 tokens, 128 workgroups: 14.9 us read in every pass, 7.0 from LDS.
 __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights, const Moves mv, int Hkv, int C, int n_first, int n_last, int32_t *idx, int idx_stride) {
+  __shared__ unsigned keys[kSelLds];
   __shared__ unsigned hist[256];
   __shared__ unsigned found[2];                         // the digit, and how many tokens have a larger one
-  __shared__ int wave_n[kSelThreads / 64][2];
+  __shared__ int wave_n[kSelWaves][2];
   const int g = blockIdx.x, z = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int have = mv.have[z], keep = mv.keep[z];
   int32_t *out = idx + ((size_t)z * Hkv + g) * idx_stride;
@@ -35,12 +38,17 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
   const int lo = n_first, hi = have - n_last;           // the tokens that compete (keep < have: n_first + n_last <= keep < have)
   int need = keep >= have ? 0 : keep - n_first - n_last;
   unsigned top = 0, mask = 0;                           // the digits found so far
+  const bool in_lds = have <= kSelLds;
+  auto key_at = [&](int t) __attribute__((always_inline)) { return in_lds ? keys[t] : key_of(w_src[t]); };
+  if (need > 0 && in_lds)
+#pragma unroll 4
+    for (int t = tid; t < have; t += kSelThreads) keys[t] = key_of(w_src[t]);
   if (keep < have) {
     for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-      hist[tid] = 0;
+      if (tid < 256) hist[tid] = 0;
       __syncthreads();
       for (int t = lo + tid; t < hi; t += kSelThreads) {
-        const unsigned k = key_of(w_src[t]);
+        const unsigned k = key_at(t);
         if ((k & mask) == top) atomicAdd(&hist[k >> shift & 255], 1u);
       }
       __syncthreads();
@@ -68,8 +76,7 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
       __syncthreads();
       top |= found[0] << shift;
       mask |= 255u << shift;
-      need -= found[1];
-      __syncthreads();
+      need -= found[1];   // (hist and found are written again behind the next barriers only)
     }
   }
   // `need` tokens with the key `top` are kept, the first ones, and all with a larger key (keep >= have: every token)
@@ -90,7 +97,7 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
     __syncthreads();
     int tie_at = ties;
 #pragma unroll
-    for (int v = 0; v < kSelThreads / 64; ++v) {
+    for (int v = 0; v < kSelWaves; ++v) {
       if (v < wave) tie_at += wave_n[v][0];
       ties += wave_n[v][0];
     }
@@ -101,7 +108,7 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
     __syncthreads();
     int pos = at + __popcll(in_b & below);
 #pragma unroll
-    for (int v = 0; v < kSelThreads / 64; ++v) {
+    for (int v = 0; v < kSelWaves; ++v) {
       if (v < wave) pos += wave_n[v][1];
       at += wave_n[v][1];
     }
@@ -114,34 +121,157 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
   for (int t = at + tid; t < idx_stride; t += kSelThreads) out[t] = -1;
 }
 
+// The slots of both formats (layouts: kvstore.hip).
 struct Store {
-  const __bf16 *k16, *v16;
-  const uint8_t *k8, *v8;
-  const float *k_scale, *v_scale;
+  __bf16 *k16, *v16;
+  uint8_t *k8, *v8;
+  float *k_scale, *v_scale;
   int n_slots16;
 };
-// The kept tokens of every (slot, kv head) as dense rows [n][Hkv][rows][D]: what their slot reads back as (bf16, or code * 2^e).
+// A 64-token block of a slot as it lies in memory: bytes of K and V, then (8-bit) their scales.  In place the blocks go through the workspace: one
+// that is written early holds tokens that another one, written late, still has to read.
 template <int D>
-__global__ __launch_bounds__(256) void keep_gather_kernel(Store st, const Moves mv, const int32_t *idx, int idx_stride, int Hkv, int C, __bf16 *dense_k, __bf16 *dense_v,
-                                                          int rows) {
-  const int z = blockIdx.z, g = blockIdx.y, slot = mv.src[z], n = min(mv.keep[z], mv.have[z]);
-  const int32_t *list = idx + ((size_t)z * Hkv + g) * idx_stride;
-  const bool is8 = slot >= st.n_slots16;
-  const size_t head = (size_t)(is8 ? slot - st.n_slots16 : slot) * Hkv + g;
-  const size_t drow = ((size_t)z * Hkv + g) * rows;
-  for (int e = blockIdx.x * 256 + threadIdx.x; e < n * D; e += gridDim.x * 256) {
-    const int j = e / D, d = e - j * D, t = list[j], blk = t / kKvTile, in = t % kKvTile;
-    const size_t row = head * C + t, block = (head * C + (size_t)blk * kKvTile) * D;
-    if (is8) {
-      const size_t sc = head * (C / kKvTile) + blk;
-      dense_k[(drow + j) * D + d] = (__bf16)(__builtin_amdgcn_cvt_f32_fp8(st.k8[row * D + d], 0) * st.k_scale[sc]);
-      dense_v[(drow + j) * D + d] = (__bf16)(__builtin_amdgcn_cvt_f32_fp8(st.v8[block + (size_t)d * kKvTile + pc::blocked_pos8(in)], 0) * st.v_scale[sc]);
-    } else {
-      dense_k[(drow + j) * D + d] = st.k16[row * D + d];
-      dense_v[(drow + j) * D + d] = st.v16[block + (size_t)d * kKvTile + (in & ~15) + pc::blocked_key(in & 15)];
+struct Image {
+  static constexpr int HALF = kKvTile * D * 2, BYTES = 2 * HALF + 256;
+};
+
+// One workgroup a (slot, kv head, 64 kept tokens): the tokens' K rows and V columns are gathered into LDS as a bf16 block (8-bit slots: code * 2^e, exact), and
+// written in the destination's format, an 8-bit block quantised afresh.  K: 16-byte pieces of the tokens' rows.  V: a token is one element in each of the D rows of
+// its block, so a lane takes two neighbouring places of the new block and goes down the rows: two 2-byte loads from the few lines that hold 64 kept tokens, one
+// 4-byte LDS store.
+template <int D>
+__global__ __launch_bounds__(256) void keep_move_kernel(Store st, const Moves mv, const int32_t *__restrict__ idx, int idx_stride, int Hkv, int C, char *__restrict__ images,
+                                                        int tiles) {
+  constexpr int KP = D / 8, V_ROW = kKvTile + 8;     // 16-byte pieces of a K row; elements of a V row in LDS (padded)
+  __shared__ __align__(16) __bf16 lk[kKvTile * D], lv[D * V_ROW];
+  __shared__ int32_t list[kKvTile];
+  __shared__ float red[4][2];
+  const int z = blockIdx.z, g = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int src = mv.src[z], dst = mv.dst[z], n = min(mv.keep[z], mv.have[z]) - tile * kKvTile;   // kept tokens from this block on
+  if (n <= 0) return;
+  const bool src8 = src >= st.n_slots16, dst8 = dst >= st.n_slots16;
+  const size_t sh = (size_t)(src8 ? src - st.n_slots16 : src) * Hkv + g, dh = (size_t)(dst8 ? dst - st.n_slots16 : dst) * Hkv + g;
+  if (tid < kKvTile) list[tid] = tid < n ? idx[((size_t)z * Hkv + g) * idx_stride + tile * kKvTile + tid] : -1;
+  __syncthreads();
+  const int bpc = C / kKvTile;
+#pragma unroll
+  for (int r = 0; r < kKvTile * KP / 256; ++r) {
+    const int e = tid + r * 256, t = list[e / KP], c = e % KP;
+    pc::u32x4 w = {0, 0, 0, 0};
+    if (t >= 0) {
+      if (src8) {
+        const uint2 q = *(const uint2 *)(st.k8 + (sh * C + t) * D + c * 8);
+        const float s = st.k_scale[sh * bpc + t / kKvTile];
+        pc::bf16x8 v;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = (__bf16)(__builtin_amdgcn_cvt_f32_fp8((int)((x < 4 ? q.x : q.y) >> (8 * (x & 3))), 0) * s);
+        w = __builtin_bit_cast(pc::u32x4, v);
+      } else {
+        w = *(const pc::u32x4 *)(st.k16 + (sh * C + t) * D + c * 8);
+      }
+    }
+    *(pc::u32x4 *)(lk + e * 8) = w;
+  }
+  {
+    const int p = 2 * (lane & 31);   // (p and p + 1 hold neighbouring keys)
+    const int key = (p & ~15) + pc::blocked_key(p & 15), t[2] = {list[key], list[key + 1]};
+    size_t at[2];
+    float s[2] = {1.f, 1.f};
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int tc = max(t[x], 0), in = tc % kKvTile;
+      at[x] = (sh * C + (tc - in)) * D + (src8 ? pc::blocked_pos8(in) : (in & ~15) + pc::blocked_key(in & 15));
+      if (src8) s[x] = st.v_scale[sh * bpc + tc / kKvTile];
+    }
+#pragma unroll 8
+    for (int r = 0; r < D / 8; ++r) {
+      const int d = r * 8 + wave * 2 + (lane >> 5);
+      unsigned w = 0;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        __bf16 v;
+        if (src8) v = (__bf16)(__builtin_amdgcn_cvt_f32_fp8((int)st.v8[at[x] + (size_t)d * kKvTile], 0) * s[x]);
+        else v = st.v16[at[x] + (size_t)d * kKvTile];
+        w |= (t[x] >= 0 ? (unsigned)__builtin_bit_cast(unsigned short, v) : 0u) << (16 * x);
+      }
+      *(unsigned *)(lv + d * V_ROW + p) = w;
     }
   }
+  __syncthreads();
+  char *const image = images ? images + (((size_t)z * Hkv + g) * tiles + tile) * Image<D>::BYTES : nullptr;
+  const bool through = src == dst;   // (in place: the block's image)
+  if (!dst8) {
+    char *const ko = through ? image : (char *)(st.k16 + (dh * C + (size_t)tile * kKvTile) * D), *const vo = through ? image + Image<D>::HALF : (char *)(st.v16 + (dh * C + (size_t)tile * kKvTile) * D);
+#pragma unroll
+    for (int r = 0; r < kKvTile * KP / 256; ++r) {
+      const int e = tid + r * 256;
+      if (e / KP < n) *(pc::u32x4 *)(ko + e * 16) = *(const pc::u32x4 *)(lk + e * 8);
+      *(pc::u32x4 *)(vo + e * 16) = *(const pc::u32x4 *)(lv + e / 8 * V_ROW + e % 8 * 8);
+    }
+    return;
+  }
+  float amax[2] = {0.f, 0.f};
+#pragma unroll
+  for (int r = 0; r < kKvTile * KP / 256; ++r) {
+    const int e = tid + r * 256;
+    const pc::bf16x8 k = *(const pc::bf16x8 *)(lk + e * 8), v = *(const pc::bf16x8 *)(lv + e / 8 * V_ROW + e % 8 * 8);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      amax[0] = fmaxf(amax[0], fabsf((float)k[x]));
+      amax[1] = fmaxf(amax[1], fabsf((float)v[x]));
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) amax[x] = fmaxf(amax[x], __shfl_xor(amax[x], o, 64));
+    if (lane == 0) red[wave][x] = amax[x];
+  }
+  __syncthreads();
+  int ex[2];
+#pragma unroll
+  for (int x = 0; x < 2; ++x) ex[x] = pc::fp8::block_exponent(fmaxf(fmaxf(red[0][x], red[1][x]), fmaxf(red[2][x], red[3][x])));
+  char *const ko = through ? image : (char *)(st.k8 + (dh * C + (size_t)tile * kKvTile) * D), *const vo = through ? image + Image<D>::HALF : (char *)(st.v8 + (dh * C + (size_t)tile * kKvTile) * D);
+  if (tid < 2) {
+    const float s = pc::fp8::pow2f(ex[tid]);
+    if (through) ((float *)(image + 2 * Image<D>::HALF))[tid] = s;
+    else (tid ? st.v_scale : st.k_scale)[dh * bpc + tile] = s;
+  }
+  auto codes = [&](const __bf16 *x, float inv) __attribute__((always_inline)) {
+    const pc::bf16x8 v = *(const pc::bf16x8 *)x;
+    return make_uint2(pc::fp8::encode4((float)v[0] * inv, (float)v[1] * inv, (float)v[2] * inv, (float)v[3] * inv),
+                      pc::fp8::encode4((float)v[4] * inv, (float)v[5] * inv, (float)v[6] * inv, (float)v[7] * inv));
+  };
+  const float ki = pc::fp8::pow2f(-ex[0]), vi = pc::fp8::pow2f(-ex[1]);
+#pragma unroll
+  for (int r = 0; r < kKvTile * KP / 256; ++r) {
+    const int e = tid + r * 256;
+    if (e / KP < n) *(uint2 *)(ko + e * 8) = codes(lk + e * 8, ki);
+    // bytes 8 c .. of a V row are the bf16 block's elements 8 c' .., c' = c with its two low bits exchanged (blocked_key8, blocked_key)
+    const int c = e % 8, from = (c & 4) | (c & 1) << 1 | (c & 2) >> 1;
+    *(uint2 *)(vo + e * 8) = codes(lv + e / 8 * V_ROW + from * 8, vi);
+  }
 }
+
+// The images of slots that are cut in place to where they belong.
+template <int D>
+__global__ __launch_bounds__(256) void keep_place_kernel(Store st, const Moves mv, int Hkv, int C, const char *__restrict__ images, int tiles) {
+  const int z = blockIdx.z, g = blockIdx.y, tile = blockIdx.x, slot = mv.dst[z], n = min(mv.keep[z], mv.have[z]) - tile * kKvTile;
+  if (n <= 0 || mv.src[z] != slot) return;
+  const bool is8 = slot >= st.n_slots16;
+  const size_t head = (size_t)(is8 ? slot - st.n_slots16 : slot) * Hkv + g, at = (head * C + (size_t)tile * kKvTile) * D;
+  const char *image = images + (((size_t)z * Hkv + g) * tiles + tile) * Image<D>::BYTES;
+  const int row = is8 ? D : 2 * D, half = kKvTile * row;
+  char *const ko = is8 ? (char *)(st.k8 + at) : (char *)(st.k16 + at), *const vo = is8 ? (char *)(st.v8 + at) : (char *)(st.v16 + at);
+  for (int e = threadIdx.x * 16; e < half; e += 4096) {
+    const pc::u32x4 k = *(const pc::u32x4 *)(image + e), v = *(const pc::u32x4 *)(image + Image<D>::HALF + e);
+    if (e / row < n) *(pc::u32x4 *)(ko + e) = k;
+    *(pc::u32x4 *)(vo + e) = v;
+  }
+  if (is8 && threadIdx.x < 2) (threadIdx.x ? st.v_scale : st.k_scale)[head * (C / kKvTile) + tile] = ((const float *)(image + 2 * Image<D>::HALF))[threadIdx.x];
+}
+
+size_t image_bytes(int head_dim) { return head_dim == 128 ? Image<128>::BYTES : Image<64>::BYTES; }
 
 }  // namespace
 
@@ -150,7 +280,7 @@ extern "C" {
 size_t percache_kv_keep_workspace_bytes(const percache_ctx *ctx, int32_t n, int32_t max_keep) {
   if (!ctx || n < 1 || max_keep < 1) return 0;
   const percache_config &c = ctx->cfg;
-  return pc::align_up((size_t)n * c.n_kv_heads * max_keep * sizeof(int32_t)) + 2 * pc::align_up((size_t)n * c.n_kv_heads * max_keep * c.head_dim * 2);
+  return pc::align_up((size_t)n * c.n_kv_heads * max_keep * sizeof(int32_t)) + (size_t)n * c.n_kv_heads * ((max_keep + kKvTile - 1) / kKvTile) * image_bytes(c.head_dim);
 }
 
 pc_status percache_kv_keep(percache_ctx *ctx, int32_t layer, const int32_t *slots_host, const int32_t *dst_slots_host, int32_t n, const int32_t *keep_host,
@@ -184,36 +314,39 @@ pc_status percache_kv_keep(percache_ctx *ctx, int32_t layer, const int32_t *slot
   if (!workspace_dev || workspace_bytes < need) return pc::fail(ctx, PC_ENOMEM, "workspace has %zu bytes, need %zu", workspace_bytes, need);
   if ((uintptr_t)workspace_dev % pc::kAlign) return pc::fail(ctx, PC_EINVAL, "workspace must be 256-byte aligned");
   char *p = (char *)workspace_dev;
-  const size_t list = (size_t)n * c.n_kv_heads * max_keep, dense = list * c.head_dim;
   int32_t *idx = idx_out_dev ? idx_out_dev : (int32_t *)p;
-  p += pc::align_up(list * sizeof(int32_t));
-  __bf16 *dk = (__bf16 *)p, *dv = (__bf16 *)(p + pc::align_up(dense * 2));
+  char *const images = p + pc::align_up((size_t)n * c.n_kv_heads * max_keep * sizeof(int32_t));
+  const int tiles = (max_keep + kKvTile - 1) / kKvTile;
   hipStream_t s = (hipStream_t)stream;
   const size_t at16 = (size_t)layer * ctx->layer_stride, at8 = (size_t)layer * ctx->layer_stride8, sc = (size_t)layer * ctx->n_slots8 * c.n_kv_heads * (c.slot_capacity / kKvTile);
   const Store st = {ctx->k_store + at16, ctx->v_store + at16, ctx->k8_store + at8, ctx->v8_store + at8, ctx->k_scale + sc, ctx->v_scale + sc, ctx->n_slots16};
-  std::vector<int32_t> bounds(n), left(n);
+  std::vector<int32_t> left(n);
   for (int i0 = 0; i0 < n; i0 += kMaxMoves) {
     const int cnt = n - i0 < kMaxMoves ? n - i0 : kMaxMoves;
     Moves mv;
+    bool in_place = false;
     for (int i = 0; i < cnt; ++i) {
       mv.src[i] = slots_host[i0 + i];
       mv.dst[i] = dst[i0 + i];
       mv.have[i] = ctx->slot_len[(size_t)layer * c.n_slots + mv.src[i]];
       mv.keep[i] = keep_host[i0 + i];
+      in_place |= mv.src[i] == mv.dst[i];
       left[i0 + i] = mv.have[i] < mv.keep[i] ? mv.have[i] : mv.keep[i];
     }
     const size_t first = (size_t)i0 * c.n_kv_heads * max_keep;
     hipLaunchKernelGGL(keep_select_kernel, dim3(c.n_kv_heads, cnt), dim3(kSelThreads), 0, s, weights_dev, mv, c.n_kv_heads, c.slot_capacity, n_first, n_last, idx + first, max_keep);
     PC_HIP(ctx, hipGetLastError());
-    const dim3 grid((max_keep * c.head_dim + 2047) / 2048, c.n_kv_heads, cnt);
-    if (c.head_dim == 128)
-      hipLaunchKernelGGL(keep_gather_kernel<128>, grid, dim3(256), 0, s, st, mv, idx + first, max_keep, c.n_kv_heads, c.slot_capacity, dk + first * c.head_dim, dv + first * c.head_dim, max_keep);
-    else
-      hipLaunchKernelGGL(keep_gather_kernel<64>, grid, dim3(256), 0, s, st, mv, idx + first, max_keep, c.n_kv_heads, c.slot_capacity, dk + first * c.head_dim, dv + first * c.head_dim, max_keep);
+    const dim3 grid(tiles, c.n_kv_heads, cnt);
+    char *const im = images + (size_t)i0 * c.n_kv_heads * tiles * image_bytes(c.head_dim);
+#define PC_KEEP(DD)                                                                                                                                        \
+  do {                                                                                                                                                     \
+    hipLaunchKernelGGL(keep_move_kernel<DD>, grid, dim3(256), 0, s, st, mv, idx + first, max_keep, c.n_kv_heads, c.slot_capacity, im, tiles);                \
+    if (in_place) hipLaunchKernelGGL(keep_place_kernel<DD>, grid, dim3(256), 0, s, st, mv, c.n_kv_heads, c.slot_capacity, im, tiles);                       \
+  } while (0)
+    if (c.head_dim == 128) PC_KEEP(128); else PC_KEEP(64);
+#undef PC_KEEP
     PC_HIP(ctx, hipGetLastError());
   }
-  const pc_status put = pc::launch_kv_put_rows(ctx, layer, dst, left.data(), n, dk, dv, max_keep, s);
-  if (put != PC_OK) return put;
   for (int i = 0; i < n; ++i) ctx->slot_len[(size_t)layer * c.n_slots + dst[i]] = left[i];
   return PC_OK;
 }

@@ -7,10 +7,13 @@
 //      contiguous run; inside each group of 16 keys the order is pc::blocked_key (see percache_internal.hpp);
 //      keys past the stored count are zero in the last block.
 // percache_kv_put / percache_kv_get convert from / to the caller's dense [kv head][token][head_dim] tensors.
-#include "percache_internal.hpp"
+#include "fp8_codes.hpp"
 
 namespace {
 using pc::kKvTile;
+using pc::fp8::block_exponent;
+using pc::fp8::encode4;
+using pc::fp8::pow2f;
 
 // One launch serves a list of (slot, dense block) pairs.  A dense block is a token range of a dense tensor: head g's token t
 // is row  row0 + g * head_rows + t  of D elements.  Only as many entries are filled in as the launch has (grid z).  The lists are
@@ -156,26 +159,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(__bf16 *__restrict__ k_s
 // key order pc::blocked_key8 inside a block, zero codes past the stored count;  one scale 2^e per 64-token block
 // for K and one for V.  One workgroup per (chunk, kv head, 64-token block).
 // ---------------------------------------------------------------------------------------------------
-// 2^e with e the smallest integer such that amax <= 448 * 2^e, e kept in [-110, 127] (0 for amax == 0).
-// 448 = 1.75 * 2^8: with amax = 1.f * 2^k the answer is k - 8 when 1.f <= 1.75, else k - 7.
-__device__ __forceinline__ int block_exponent(float amax) {
-  if (amax == 0.f) return 0;
-  const unsigned bits = __float_as_uint(amax);
-  const int field = (int)((bits >> 23) & 0xff);
-  if (field == 0) return -110;  // below 2^-126
-  const int k = field - 127;
-  const int e = (bits & 0x7fffffu) <= 0x600000u ? k - 8 : k - 7;
-  return e < -110 ? -110 : (e > 127 ? 127 : e);
-}
-__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }  // e in [-126, 127]
-
-// four E4M3 codes of four floats already divided by the scale (round to nearest even in hardware; |y| <= 448)
-__device__ __forceinline__ unsigned encode4(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_fmed3f(a, -448.f, 448.f), __builtin_amdgcn_fmed3f(b, -448.f, 448.f), 0, false);
-  w = __builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_fmed3f(c, -448.f, 448.f), __builtin_amdgcn_fmed3f(d, -448.f, 448.f), w, true);
-  return (unsigned)w;
-}
-
 // Entry::off: the slot already holds that many tokens and the dense tensors are the tokens that follow them (0: a put).  The
 // block that was partly filled is then quantised afresh from the values its old tokens read back as plus the new
 // tokens (its exponent is recomputed over all of them; old codes are re-rounded only if the exponent moves); the
@@ -297,9 +280,13 @@ struct PathWeights {
 template <int D>
 __global__ __launch_bounds__(2 * D) void kv_path_kernel(Store16 s16, Store8 s8, int n_slots16, const __bf16 *__restrict__ dense_k, const __bf16 *__restrict__ dense_v,
                                                         PathWeights w, int C, int T, const pc::ListWords lists, int record) {
+  // The nodes go through LDS: indexed by a lane, the launch's arguments are host memory, a microsecond and more a look (10.1 us a call so, one query; now 3.6).
+  __shared__ int32_t path[pc::kListWords];
   const int z = blockIdx.z, g = blockIdx.y, Hkv = gridDim.y, tid = threadIdx.x;
-  const int32_t *rec = lists.v + z * record, *path = rec + 3;   // slot, start, number of nodes, the nodes
+  const int32_t *rec = lists.v + z * record;   // slot, start, number of nodes, the nodes
   const int slot = rec[0], start = rec[1], n = rec[2], end = start + n;
+  for (int j = tid; j < n; j += 2 * D) path[j] = rec[3 + j];
+  __syncthreads();
   const int blk = start / kKvTile + blockIdx.x, t0 = blk * kKvTile;
   if (slot < 0 || t0 >= end) return;
   const size_t row0 = ((size_t)z * Hkv + g) * T;
@@ -311,14 +298,21 @@ __global__ __launch_bounds__(2 * D) void kv_path_kernel(Store16 s16, Store8 s8, 
     return;
   }
   const size_t head = (size_t)slot * s16.slot_stride + (size_t)g * C * D;
-  for (int e = tid; e < kKvTile * (D / 8); e += 2 * D) {
-    const int t = t0 + e / (D / 8), d = e % (D / 8) * 8;
-    if (t >= start && t < end) *(pc::u32x4 *)(s16.k + head + (size_t)t * D + d) = *(const pc::u32x4 *)(dense_k + (row0 + path[t - start]) * D + d);
+  const int from = max(start, t0), to = min(end, t0 + kKvTile);
+  __bf16 *const block = s16.v + head + (size_t)t0 * D;
+  for (int e = tid; e < (to - from) * (D / 8); e += 2 * D) {
+    const int t = from + e / (D / 8), d = e % (D / 8) * 8, in = t - t0, at = (in & ~15) + pc::blocked_key(in & 15);
+    const size_t src = (row0 + path[t - start]) * D + d;
+    *(pc::u32x4 *)(s16.k + head + (size_t)t * D + d) = *(const pc::u32x4 *)(dense_k + src);
+    const pc::bf16x8 v = *(const pc::bf16x8 *)(dense_v + src);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) block[(d + x) * kKvTile + at] = v[x];
   }
-  for (int e = tid; e < kKvTile * D; e += 2 * D) {   // (zeros behind the last token: the padding stays finite)
-    const int p = e % kKvTile, d = e / kKvTile, t = t0 + (p & ~15) + pc::blocked_key(p & 15);
-    if (t >= start) s16.v[head + (size_t)t0 * D + e] = t < end ? dense_v[(row0 + path[t - start]) * D + d] : (__bf16)0.f;
-  }
+  if (to == end)   // zeros behind the last token: the padding stays finite
+    for (int e = tid; e < kKvTile * D; e += 2 * D) {
+      const int p = e % kKvTile;
+      if (t0 + (p & ~15) + pc::blocked_key(p & 15) >= end) block[e] = (__bf16)0.f;
+    }
 }
 
 // The values an 8-bit slot holds, as dense bf16 [kv head][token][head_dim]: code * 2^e (exact).  Work split as in
@@ -514,22 +508,6 @@ pc_status launch_kv_slices(percache_ctx *ctx, int layer, const int32_t *slots, c
       if (tokens > longest) longest = tokens;
     }
   return flush();
-}
-pc_status launch_kv_put_rows(percache_ctx *ctx, int layer, const int32_t *slots, const int32_t *lengths, int n, const __bf16 *k, const __bf16 *v, int rows,
-                             hipStream_t stream) {
-  const size_t per_slot = (size_t)ctx->cfg.n_kv_heads * rows * ctx->cfg.head_dim;
-  PieceList<kListMax> l;
-  for (int i0 = 0; i0 < n; i0 += kListMax) {
-    const int cnt = n - i0 < kListMax ? n - i0 : kListMax;
-    int longest = 0;
-    for (int i = 0; i < cnt; ++i) {
-      l.entry[i] = {slots[i0 + i], i * ctx->cfg.n_kv_heads * rows, lengths[i0 + i], 0};
-      if (lengths[i0 + i] > longest) longest = lengths[i0 + i];
-    }
-    const pc_status st = launch_copy<true>(ctx, layer, l, cnt, longest, (void *)(k + i0 * per_slot), (void *)(v + i0 * per_slot), rows, stream);
-    if (st != PC_OK) return st;
-  }
-  return PC_OK;
 }
 pc_status launch_kv_append(percache_ctx *ctx, int layer, const int32_t *slot_list, int n, bool only_8bit, const __bf16 *k, const __bf16 *v,
                            int n_tokens, hipStream_t stream) {

@@ -261,10 +261,6 @@ inline int table_formats(const std::vector<int32_t> &rows, int stride, int batch
 pc_status launch_kv_slices(percache_ctx *ctx, int layer, const int32_t *slots, const int32_t *bounds, int n_pieces, int batch, const __bf16 *k,
                            const __bf16 *v, int seq_len, hipStream_t stream);
 
-// Stores the first lengths[i] tokens of dense tensor i of [n][Hkv][rows][D] in slot slots[i] (no validation, no slot-table update).
-pc_status launch_kv_put_rows(percache_ctx *ctx, int layer, const int32_t *slots, const int32_t *lengths, int n, const __bf16 *k, const __bf16 *v, int rows,
-                             hipStream_t stream);
-
 // Appends n_tokens tokens of every dense tensor of [n][Hkv][n_tokens][D] behind the tokens that the slot of the same place
 // in the list holds (by the slot table; no validation, no slot-table update).  Negative entries are skipped, and with
 // only_8bit the bf16 slots too.
