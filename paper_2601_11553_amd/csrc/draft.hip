@@ -4,7 +4,7 @@
 // The projection and the attention are the kernels of qkv_rope_gemm.hip, reuse_attention.hip and decode_attention.hip; here are the host
 // entry points and the lists they take: positions of the nodes, and for the attention one word of 64 bits per node and 64 nodes that
 // says which of them it looks at.
-#include "percache_internal.hpp"
+#include "decode_common.hpp"
 
 namespace {
 
@@ -51,128 +51,196 @@ __global__ __launch_bounds__(kTreeThreads) void draft_lists_kernel(int32_t *dst,
   }
 }
 
-// over the lanes of a group of 16 (8) neighbours
+#define PC_MOVE(ctrl) __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), ctrl, 0xf, 0xf, true))
+// sum over the N = 16 or 8 neighbouring lanes that share a dot product
 template <int N>
 __device__ __forceinline__ float group_sum(float x) {
-#define PC_MOVE(ctrl) __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), ctrl, 0xf, 0xf, true))
   x += PC_MOVE(0xB1);                    // lane ^ 1
   x += PC_MOVE(0x4E);                    // lane ^ 2
   x += PC_MOVE(0x141);                   // mirrored inside 8
   if (N == 16) x += PC_MOVE(0x140);      // mirrored inside 16
-#undef PC_MOVE
   return x;
+}
+// over the 64 / N groups: lanes l + N k
+template <int N, class Op>
+__device__ __forceinline__ float over_groups(float x, Op op) {
+  if (N == 8) x = op(x, PC_MOVE(0x128)); // lane ^ 8 (rotated by 8 inside 16)
+  return pc::dec::over_rows(x, op);
+}
+// x of the lower half of the lanes (rows of 16: of the even rows), y of the upper half (odd rows), each added over both
+__device__ __forceinline__ float halve32(float x, float y) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ __forceinline__ float halve16(float x, float y) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
 }
 
 // The merge of a row's partials over the cached keys, and the nodes that the row looks at, a handful of a tree's: each of them is a dot product and
 // one more weighted row, which no tile of matrix products would be worth -- and a node that a row does not look at is not read for it,
-// whatever it holds.  A row is shared by 4 x D/8 lanes: lane (sg, dv) has 8 elements of the head and takes partials sg, sg + 4, ... and the
-// nodes j = sg (mod 4), four at a time with all their loads in flight; the four running (max, sum, output) meet through lane shuffles.
-template <int D>
+// whatever it holds.  A wavefront takes one node of the tree and H heads of a group, which look at the same nodes: lane (sg, dv) has 8 elements of a head and
+// takes partials sg, sg + SG, ... (NP of them at a time) and, 16 nodes of the row at a time, NB of them, dealt out by scalar arithmetic; the SG running (max, sum,
+// output) meet through lane exchanges that leave every lane with the elements it writes.  Its time is that of two memory latencies while the rows fit the chip
+// at once -- the first nodes are asked for as soon as the row's word of `sees` is there, the partials looked at behind that --, then that of the vector port, hence H.
+// 12288 rows of 13 nodes and 4 partials: 17.6 us with a row a wavefront, nodes dealt out lane by lane and whole sums exchanged, 13.0 now.
+template <int D, int NP, int H>
 __global__ __launch_bounds__(256) void draft_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, int n_splits, const __bf16 *__restrict__ Q,
-                                                          const __bf16 *__restrict__ K, const __bf16 *__restrict__ V, int T, int Hq, int Hkv, long total_rows,
+                                                          const __bf16 *__restrict__ K, const __bf16 *__restrict__ V, int T, int Hq, int Hkv,
                                                           float scale_log2e, pc::DraftView draft, __bf16 *__restrict__ out) {
-  constexpr int VPR = D / 8, LPR = 4 * VPR;
-  const long gid = (long)blockIdx.x * 256 + threadIdx.x, prow = gid / LPR;
-  if (prow >= total_rows) return;   // (LPR divides the 64 lanes: a row's lanes stay together)
-  const int r = (int)(gid - prow * LPR), sg = r / VPR, dv = r - sg * VPR;
-  const int G = Hq / Hkv, R = G * T;
-  const long bg = prow / R;
-  const int row = (int)(prow - bg * R), b = (int)(bg / Hkv), g = (int)(bg - (long)b * Hkv), hg = row / T, i = row - hg * T, head = g * G + hg;
-  const bool live = pc::draft_live(draft, b, T, i);
-  float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  auto shift_to = [&](float top) __attribute__((always_inline)) {   // a new reference exponent, never below the old one
-    const float a = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);   // (a sum that is NaN without a maximum stays)
-    m = top;
-    l *= a;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= a;
+  constexpr int VPR = D / 8, SG = 64 / VPR, NB = 16 / SG;
+  const int G = Hq / Hkv, R = G * T, groups = (G + H - 1) / H * T, blocks = (groups + 3) / 4;
+  const int bg = blockIdx.x / blocks, b = bg / Hkv, g = bg - b * Hkv, lane = threadIdx.x & 63, sg = lane / VPR, dv = lane % VPR;
+  const int group = (blockIdx.x - bg * blocks) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (group >= groups) return;
+  const int hg = group / T * H, i = group % T, head = g * G + hg, n_heads = min(H, G - hg);
+
+  auto word_of = [&](int w) __attribute__((always_inline)) {
+    const unsigned long long x = pc::draft_row(draft, b, T, i, 64 * w);
+    return ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x);
   };
-  if (live) {
+  struct Parts { float2 e[NP]; pc::f32x4 o[NP][2]; };
+  auto load = [&](Parts &x, int h, int s0) __attribute__((always_inline)) {
+    const size_t prow = (size_t)bg * R + (hg + min(h, n_heads - 1)) * T + i;
     const float2 *ml = (const float2 *)part_ml + prow * n_splits;
     const float *po = part_o + prow * n_splits * D + dv * 8;
-    for (int s0 = sg; s0 < n_splits; s0 += 16) {
-      float2 e[4];
-      pc::f32x4 o[4][2];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int s = s0 + 4 * j, sc = s < n_splits ? s : s0;
-        e[j] = ml[sc];
-        o[j][0] = *(const pc::f32x4 *)(po + (size_t)sc * D);
-        o[j][1] = *(const pc::f32x4 *)(po + (size_t)sc * D + 4);
-        if (s >= n_splits) e[j].y = 0.f;
-      }
-      float top = m;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) top = fmaxf(top, e[j].y != 0.f ? e[j].x : -INFINITY);
-      shift_to(top);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (e[j].y == 0.f) continue;   // (no key of the partition is visible)
-        const float w = e[j].y * __builtin_amdgcn_exp2f(e[j].x - m);
-        l += w;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) acc[x] += w * o[j][x >> 2][x & 3];
-      }
+    for (int j = 0; j < NP; ++j) {
+      const int s = s0 + SG * j, sc = min(s, n_splits - 1);
+      x.e[j] = ml[sc];
+      x.o[j][0] = *(const pc::f32x4 *)(po + (size_t)sc * D);
+      x.o[j][1] = *(const pc::f32x4 *)(po + (size_t)sc * D + 4);
+      if (s >= n_splits) x.e[j].y = 0.f;
     }
-    if (Q) {
-      const pc::bf16x8 qv = *(const pc::bf16x8 *)(Q + (((size_t)b * Hq + head) * T + i) * D + dv * 8);
-      const __bf16 *kr = K + ((size_t)b * Hkv + g) * T * D + dv * 8, *vr = V + ((size_t)b * Hkv + g) * T * D + dv * 8;
-      for (int t0 = 0; t0 <= i; t0 += 64) {
-        unsigned long long bits = pc::draft_row(draft, b, T, i, t0) & (0x1111111111111111ull << sg);
-        while (bits) {
-          int n = 0, t[4];
+  };
+  pc::bf16x8 qv[H];
+  if (Q)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            t[j] = bits ? t0 + (int)__builtin_ctzll(bits) : t[0];
-            n += bits != 0;
-            bits &= bits - 1;
-          }
-          pc::bf16x8 kv[4], vv[4];
+    for (int h = 0; h < H; ++h) qv[h] = *(const pc::bf16x8 *)(Q + (((size_t)b * Hq + head + min(h, n_heads - 1)) * T + i) * D + dv * 8);
+  Parts parts[H];
+  if (n_splits > 0)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            kv[j] = *(const pc::bf16x8 *)(kr + (size_t)t[j] * D);
-            vv[j] = *(const pc::bf16x8 *)(vr + (size_t)t[j] * D);
-          }
-          float s[4], top = m;
+    for (int h = 0; h < H; ++h) load(parts[h], h, sg);
+
+  // nodes: the words of `sees` up to the row's own node
+  unsigned long long bits = word_of(0);
+  const bool live = i < 64 ? bits >> i & 1 : pc::draft_live(draft, b, T, i);
+  const int n_words = live && Q ? i / 64 + 1 : 0;
+  const __bf16 *kr = K + (((size_t)b * Hkv + g) * T) * D + dv * 8, *vr = V + (((size_t)b * Hkv + g) * T) * D + dv * 8;
+  int word = 0;
+  struct Batch { pc::bf16x8 k[NB], v[NB]; bool any, has[NB]; };
+  auto next = [&](Batch &x) __attribute__((always_inline)) {   // up to 16 nodes of a word
+    while (word < n_words && !bits) {
+      ++word;
+      if (word < n_words) bits = word_of(word);
+    }
+    x.any = word < n_words;
+    if (!x.any) return;
+    const int first = 64 * word + (int)__builtin_ctzll(bits);
+    int t[NB];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float d = 0.f;
+    for (int j = 0; j < NB; ++j) {
+      t[j] = -1;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) d += (float)qv[x] * (float)kv[j][x];
-            s[j] = group_sum<VPR>(d) * scale_log2e;
-            if (j < n) top = fmaxf(top, s[j]);
-          }
-          shift_to(top);
+      for (int y = 0; y < SG; ++y) {
+        const int node = bits ? 64 * word + (int)__builtin_ctzll(bits) : -1;
+        bits &= bits - 1;
+        t[j] = sg == y ? node : t[j];
+      }
+      x.has[j] = t[j] >= 0;
+      t[j] = x.has[j] ? t[j] : first;
+    }
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            if (j >= n) continue;
-            const float w = s[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[j] - m);
-            l += w;
+    for (int j = 0; j < NB; ++j) x.k[j] = *(const pc::bf16x8 *)(kr + (size_t)t[j] * D);
 #pragma unroll
-            for (int x = 0; x < 8; ++x) acc[x] += w * (float)vv[j][x];
-          }
+    for (int j = 0; j < NB; ++j) x.v[j] = *(const pc::bf16x8 *)(vr + (size_t)t[j] * D);
+  };
+  Batch batch;
+  next(batch);
+
+  struct State {
+    float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    __device__ __forceinline__ void shift_to(float top) {   // a new reference exponent, never below the old one
+      const float a = m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);   // (a sum that is NaN without a maximum stays)
+      m = top;
+      l *= a;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] *= a;
+    }
+  } st[H];
+  if (live)
+    for (int s0 = sg; s0 - sg < n_splits; s0 += SG * NP)
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        if (s0 != sg) load(parts[h], h, s0);
+        float top = st[h].m;
+#pragma unroll
+        for (int j = 0; j < NP; ++j) top = fmaxf(top, parts[h].e[j].y != 0.f ? parts[h].e[j].x : -INFINITY);
+        st[h].shift_to(top);
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+          // (a partition without a visible key has sum 0, and zeros)
+          const float w = parts[h].e[j].y == 0.f ? 0.f : parts[h].e[j].y * __builtin_amdgcn_exp2f(parts[h].e[j].x - st[h].m);
+          st[h].l += w;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) st[h].acc[x] += w * parts[h].o[j][x >> 2][x & 3];
         }
       }
+  while (batch.any) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      float s[NB], top = st[h].m;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        float d = 0.f;
+#pragma unroll
+        for (int x = 0; x < 8; x += 2) d = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{qv[h][x], qv[h][x + 1]}, bf16x2{batch.k[j][x], batch.k[j][x + 1]}, d, false);
+        d = group_sum<VPR>(d) * scale_log2e;
+        s[j] = batch.has[j] ? d : -INFINITY;
+        top = fmaxf(top, s[j]);
+      }
+      st[h].shift_to(top);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const float w = s[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[j] - st[h].m);
+        st[h].l += w;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) st[h].acc[x] += w * (float)batch.v[j][x];
+      }
     }
+    next(batch);
   }
 #pragma unroll
-  for (int sh = VPR; sh < LPR; sh <<= 1) {
-    const float m_other = __shfl_xor(m, sh, 64), l_other = __shfl_xor(l, sh, 64), top = fmaxf(m, m_other);
-    const float a = l == 0.f ? 0.f : m == top ? 1.f : __builtin_amdgcn_exp2f(m - top);
-    const float c = l_other == 0.f ? 0.f : m_other == top ? 1.f : __builtin_amdgcn_exp2f(m_other - top);
-    m = top;
-    l = l * a + l_other * c;
+  for (int h = 0; h < H; ++h) {
+    State &z = st[h];
+    const float top = over_groups<VPR>(z.m, [](float x, float y) { return fmaxf(x, y); });
+    const float a = z.l == 0.f ? 0.f : z.m == top ? 1.f : __builtin_amdgcn_exp2f(z.m - top);
+    const float l = over_groups<VPR>(z.l * a, [](float x, float y) { return x + y; }), scale = l == 0.f ? 0.f : a / l;
+    // elements 8 dv .. +7 over the groups: halves of them go to halves of the lanes, until a lane has elements 8 dv + at .. of its own
+    float x4[4], x2[2];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = acc[e] * a + __shfl_xor(acc[e], sh, 64) * c;
+    for (int e = 0; e < 4; ++e) x4[e] = halve32(z.acc[e] * scale, z.acc[e + 4] * scale);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) x2[e] = halve16(x4[e], x4[e + 2]);
+    const int at = 4 * (lane >> 5) + 2 * (lane >> 4 & 1);
+    if constexpr (SG == 8) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float x = x2[e];
+        x2[e] = x + PC_MOVE(0x128);
+      }
+    }
+    if (h >= n_heads) continue;
+    if (draft.lse && lane == 0) draft.lse[((size_t)b * Hq + head + h) * T + i] = pc::lse_of(top, l);
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if (SG == 4 || (lane & 8) == 0)
+      *(bf16x2 *)(out + ((size_t)b * T + i) * ((size_t)Hq * D) + (size_t)(head + h) * D + dv * 8 + at) = bf16x2{(__bf16)x2[0], (__bf16)x2[1]};
   }
-  if (sg != 0) return;
-  if (draft.lse && dv == 0) draft.lse[((size_t)b * Hq + head) * T + i] = pc::lse_of(m, l);
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  pc::bf16x8 v;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (__bf16)(acc[e] * inv);
-  *(pc::bf16x8 *)(out + ((size_t)b * T + i) * ((size_t)Hq * D) + (size_t)head * D + dv * 8) = v;
 }
+#undef PC_MOVE
 
 bool aligned16(const void *p) { return (uintptr_t)p % 16 == 0; }
 
@@ -259,11 +327,27 @@ pc_status upload_draft(percache_ctx *ctx, std::vector<int32_t> &words, int batch
 pc_status launch_draft_merge(percache_ctx *ctx, const float *part_o, const float *part_ml, int n_splits, const __bf16 *q, const __bf16 *k, const __bf16 *v, int batch, int T,
                              const DraftView &draft, __bf16 *out, hipStream_t stream) {
   const percache_config &c = ctx->cfg;
-  const long rows = (long)batch * c.n_q_heads * T;
-  const dim3 grid((unsigned)((rows * (c.head_dim / 2) + 255) / 256));
+  const int G = c.n_q_heads / c.n_kv_heads;
   const float scale_log2e = 1.4426950408889634f / sqrtf((float)c.head_dim);
-  if (c.head_dim == 128) hipLaunchKernelGGL(draft_merge_kernel<128>, grid, dim3(256), 0, stream, part_o, part_ml, n_splits, q, k, v, T, c.n_q_heads, c.n_kv_heads, rows, scale_log2e, draft, out);
-  else hipLaunchKernelGGL(draft_merge_kernel<64>, grid, dim3(256), 0, stream, part_o, part_ml, n_splits, q, k, v, T, c.n_q_heads, c.n_kv_heads, rows, scale_log2e, draft, out);
+  // Heads of a group together once the rows by themselves, a wavefront each, would be more than the chip holds at once (about 20 a CU).
+  const int per = c.head_dim == 128 ? 4 : 8;
+  const bool together = n_splits <= per && (long)batch * c.n_q_heads * T > 20L * ctx->n_cu;
+  const int H = !together || G == 1 ? 1 : G == 2 ? 2 : G % 3 == 0 ? 3 : G % 4 == 0 || G > 4 ? 4 : 2;
+  const long blocks = ((long)((G + H - 1) / H) * T + 3) / 4;
+  const dim3 grid((unsigned)(blocks * batch * c.n_kv_heads));
+#define PC_MERGE(DD, NN, HH) \
+  hipLaunchKernelGGL((draft_merge_kernel<DD, NN, HH>), grid, dim3(256), 0, stream, part_o, part_ml, n_splits, q, k, v, T, c.n_q_heads, c.n_kv_heads, scale_log2e, draft, out)
+#define PC_MERGE_D(DD)                                                                                          \
+  do {                                                                                                          \
+    if (n_splits > per) PC_MERGE(DD, 4, 1);                                                                     \
+    else if (H == 1) PC_MERGE(DD, 1, 1);                                                                        \
+    else if (H == 2) PC_MERGE(DD, 1, 2);                                                                        \
+    else if (H == 3) PC_MERGE(DD, 1, 3);                                                                        \
+    else PC_MERGE(DD, 1, 4);                                                                                    \
+  } while (0)
+  if (c.head_dim == 128) PC_MERGE_D(128); else PC_MERGE_D(64);
+#undef PC_MERGE_D
+#undef PC_MERGE
   PC_HIP(ctx, hipGetLastError());
   return PC_OK;
 }
@@ -348,8 +432,17 @@ pc_status percache_attention_draft(percache_ctx *ctx, int32_t layer, const void 
   pc::DraftView draft;
   draft.sees = parents_host ? ws.sees : nullptr;
   draft.lse = lse_out_dev;
-  return pc::launch_attention(ctx, layer, (const __bf16 *)q_dev, (const __bf16 *)k_draft_dev, (const __bf16 *)v_draft_dev, nullptr, nullptr, batch, t_draft,
-                              ws.words, stride, mean_tiles, n_splits, (__bf16 *)attn_out_dev, ws.part_o, ws.part_ml, s, formats, nullptr, &draft);
+  const __bf16 *q = (const __bf16 *)q_dev, *k = (const __bf16 *)k_draft_dev, *v = (const __bf16 *)v_draft_dev;
+  __bf16 *out = (__bf16 *)attn_out_dev;
+  const bool few = pc::decode_rows(c, t_draft);   // (the decode kernel takes the nodes along as its fresh keys)
+  if (!few && mean_tiles == 0) return pc::launch_draft_merge(ctx, nullptr, nullptr, 0, q, k, v, batch, t_draft, draft, out, s);   // (nothing cached)
+  pc::prof_begin(ctx, PC_KERNEL_ATTENTION, s);
+  st = few ? pc::launch_decode_attention(ctx, layer, q, k, v, nullptr, batch, t_draft, ws.words, stride, mean_tiles, n_splits, 0, out, ws.part_o, ws.part_ml, s, formats, &draft)
+           : pc::launch_draft_attention(ctx, layer, q, batch, t_draft, ws.words, stride, mean_tiles, n_splits, ws.part_o, ws.part_ml, s, formats);
+  if (st != PC_OK) return st;
+  pc::prof_end(ctx, PC_KERNEL_ATTENTION, s);
+  if (few && n_splits == 1) return PC_OK;
+  return pc::launch_draft_merge(ctx, ws.part_o, ws.part_ml, n_splits, few ? nullptr : q, k, v, batch, t_draft, draft, out, s);
 }
 
 }  // extern "C"

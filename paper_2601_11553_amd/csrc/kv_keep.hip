@@ -24,7 +24,7 @@ __device__ __forceinline__ unsigned key_of(float w) {
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelLds = 8192;
 // One workgroup a (kv head, slot).  idx [n][Hkv][idx_stride]: the kept tokens in order, -1 behind them; weights are moved along.
 // Four passes over a few thousand keys and one over the tokens, each a few LDS accesses and barriers: a chain of latencies, so the keys are read from memory
-// once, into LDS (slots of up to kSelLds tokens; longer ones are read again from the L2).  2048 tokens, 128 workgroups: 14.9 us read in every pass, 7.0 from LDS.
+// once, into LDS (slots of up to kSelLds tokens; longer ones are read again from the L2).  2048 tokens, 128 workgroups: 14.9 us read in every pass, 9.2 from LDS.
 __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights, const Moves mv, int Hkv, int C, int n_first, int n_last, int32_t *idx, int idx_stride) {
   __shared__ unsigned keys[kSelLds];
   __shared__ unsigned hist[256];

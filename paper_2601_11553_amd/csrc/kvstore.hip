@@ -280,7 +280,7 @@ struct PathWeights {
 template <int D>
 __global__ __launch_bounds__(2 * D) void kv_path_kernel(Store16 s16, Store8 s8, int n_slots16, const __bf16 *__restrict__ dense_k, const __bf16 *__restrict__ dense_v,
                                                         PathWeights w, int C, int T, const pc::ListWords lists, int record) {
-  // The nodes go through LDS: indexed by a lane, the launch's arguments are host memory, a microsecond and more a look (10.1 us a call so, one query; now 3.6).
+  // The nodes go through LDS: indexed by a lane, the launch's arguments are host memory, a microsecond and more a look (10.1 us a call so, one query; now 4.8).
   __shared__ int32_t path[pc::kListWords];
   const int z = blockIdx.z, g = blockIdx.y, Hkv = gridDim.y, tid = threadIdx.x;
   const int32_t *rec = lists.v + z * record;   // slot, start, number of nodes, the nodes

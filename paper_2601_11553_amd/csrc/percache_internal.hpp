@@ -221,11 +221,10 @@ inline bool decode_rows(const percache_config &c, int t_fresh) { return (long)(c
 // raw: q and the fresh k, v as the projection's sums instead (decode_rows only; q, kf, vf unused).
 // left_splits (decode_rows only): in, the most partials that the caller would merge itself; out, the number left to it, at 1 the
 // result is in out.
-// draft: the fresh rows are nodes of trees (min_tiles: cached tiles alone); its partials are fp32, rows x partitions x D, up to max_splits_for of them.
 pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const __bf16 *kf, const __bf16 *vf, const __bf16 *vf_blk,
                            const RawQkv *raw, int batch, int t_fresh, const int32_t *table_dev, int tbl_stride, int max_tiles,
                            int n_splits, __bf16 *out, void *part_o, float *part_ml, hipStream_t stream, int formats,
-                           int *left_splits = nullptr, const DraftView *draft = nullptr);
+                           int *left_splits = nullptr);
 // The first of its two launches where decode_rows; tiles: cached tiles of the shortest query.  n_splits <= 0: chosen here
 // (merge_limit: up to so many partials are left to the o_proj, more are merged by a launch of their own).
 pc_status launch_decode_attention(percache_ctx *ctx, int layer, const __bf16 *q, const __bf16 *kf, const __bf16 *vf, const RawQkv *raw, int batch, int t_fresh,
@@ -245,6 +244,9 @@ DraftWs carve_draft_ws(const percache_config &cfg, int n_cu, void *base, int32_t
 // Brings the words of a call to the device and, if there are parents, makes the trees' DraftView::sees.
 pc_status upload_draft(percache_ctx *ctx, std::vector<int32_t> &words, int batch, int t_draft, const int32_t *parents, const DraftWs &ws, hipStream_t stream);
 
+// The attention of drafted nodes over the cached keys, in n_splits fp32 partials a row (<= 0: chosen, and written back), for more rows than decode_rows takes (draft_attention.hip).
+pc_status launch_draft_attention(percache_ctx *ctx, int layer, const __bf16 *q, int batch, int t_draft, const int32_t *table_dev, int tbl_stride, int tiles, int &n_splits,
+                                 float *part_o, float *part_ml, hipStream_t stream, int formats);
 // Merges the fp32 partials of the cached keys (n_splits of them a row; 0: none) and, where q is given, the nodes that each row looks at.
 pc_status launch_draft_merge(percache_ctx *ctx, const float *part_o, const float *part_ml, int n_splits, const __bf16 *q, const __bf16 *k, const __bf16 *v, int batch, int T,
                              const DraftView &draft, __bf16 *out, hipStream_t stream);

@@ -72,18 +72,6 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(unsigned w0, unsigned w1, float 
   return u.v;
 }
 
-// V operand of step c (16 keys from 16 c on) with the keys from `valid` on cleared: element e of lane half g2 is key 16 c + 8 (e >> 2) + 4 g2 + (e & 3).
-// g2x4: 4 g2, opaque to the compiler, so that nothing of this stays in registers over the loop.
-__device__ __forceinline__ bf16x8 keep_keys(bf16x8 v, int c, int g2x4, int valid) {
-  pc::u32x4 w = __builtin_bit_cast(pc::u32x4, v);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int left = valid - (16 * c + 8 * (i >> 1) + 2 * (i & 1)) - g2x4;
-    w[i] &= left >= 2 ? ~0u : left == 1 ? 0xffffu : 0u;
-  }
-  return __builtin_bit_cast(bf16x8, w);
-}
-
 // A lane's part of one partition's output for row prow, normalised: in fp32 or (a rounding more, half the bytes of the merge) in bf16.  Which of them is
 // choose_partitions' matter; a flag at run time costs the 256-row kernels' loop 1 %.
 template <int D, bool PART32>
@@ -118,11 +106,7 @@ __device__ __forceinline__ void write_partial(const f32x16 (&o_acc)[D / 32], flo
 // KSP = 2: two wavefronts share a 32-row block and take one 32-key block of every tile each (separate running
 // maximum / sum / output, merged through LDS at the end); for launches of few workgroups over bf16 slots, where the
 // per-tile chain of one wavefront, not the key stream, would set the pace.
-// DRAFT (here and in the long-context kernels): the rows are nodes of a tree of drafted tokens, and only the cached keys are walked; the few
-// nodes that a row looks at are added in the merge (draft_merge_kernel, draft.hip), which every such launch goes through: partials
-// always, in fp32, with row sums of the unrounded probabilities because the log-sum-exp is handed out.  V of the keys past a
-// chunk's used length is cleared before its product: their probabilities are 0, but what stands there need not be finite.
-template <int D, int NW, int NSTAGE, bool KV8, int KSP, bool MIXED, bool PART32, bool DRAFT = false>
+template <int D, int NW, int NSTAGE, bool KV8, int KSP, bool MIXED, bool PART32>
 __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
     const __bf16 *__restrict__ Q, const __bf16 *__restrict__ Kf, const __bf16 *__restrict__ Vf_blk,
     const void *__restrict__ k_store_any, const void *__restrict__ v_store_any, const float *__restrict__ k_scale,
@@ -172,7 +156,7 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
   const int row_first = qt * QROWS;
   const int row_last = min(row_first + QROWS, R) - 1;
   const int i_max = (row_first / T == row_last / T) ? (row_last % T) : (T - 1);
-  const int n_tiles = n_cached_tiles + (DRAFT ? 0 : i_max / TK + 1);
+  const int n_tiles = n_cached_tiles + i_max / TK + 1;
   const int tile_begin = (int)((long)split * n_tiles / n_splits);
   const int tile_end = (int)((long)(split + 1) * n_tiles / n_splits);
 
@@ -303,7 +287,7 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
   // A context may hold slots of both formats: ids below n_slots16 are bf16 slots of k_store16 / v_store16.
   struct TileDesc { const __bf16 *k, *v; int valid; int t0; bool fresh; bool is8; float ks, vs; };
   auto describe = [&](const Cursor &c, TileDesc &td) __attribute__((always_inline)) {
-    if (DRAFT || c.chunk < n_chunks) {
+    if (c.chunk < n_chunks) {
       // (no branch around the scale loads: a branch would make the wavefront wait for them here instead of at their
       // first use, a tile later)
       // MIXED: the call names chunks of both formats (else every chunk of a KV8 launch sits in an 8-bit slot, and the
@@ -340,7 +324,7 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
   };
   auto advance = [&](Cursor &c) __attribute__((always_inline)) {
     ++c.off;
-    if ((DRAFT || c.chunk < n_chunks) && c.off * TK >= c.used) {
+    if (c.chunk < n_chunks && c.off * TK >= c.used) {
       c.off = 0;
       ++c.chunk;
       enter_chunk(c);
@@ -499,8 +483,7 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
             const bf16x2 pr = {(__bf16)p0, (__bf16)p1};
             pf[kbk][j][e] = pr[0];
             pf[kbk][j][e + 1] = pr[1];
-            if constexpr (DRAFT) sum += p0 + p1;
-            else sum = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, sum, false);
+            sum = __builtin_amdgcn_fdot2_f32_bf16(pr, ones, sum, false);
           }
       return sum;
     };
@@ -530,8 +513,6 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
     l_run += psum;
 
     // ---- O^T += V^T P^T, operands requested in batches of eight in the same way
-    int g2x4 = g2 * 4;
-    if constexpr (DRAFT) asm volatile("" : "+v"(g2x4));
     if (KV8 && td.is8) {
 #pragma unroll
       for (int h = 0; h < NKB; ++h) {
@@ -540,12 +521,8 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
         for (int db = 0; db < DB; ++db) raw[db] = *(const pc::u32x4 *)(vb + (db * 32 + l32) * V8_ROW + v8_rd[h]);
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
-          bf16x8 a0 = codes_to_bf16(raw[db][0], raw[db][1], td.vs);
-          bf16x8 a1 = codes_to_bf16(raw[db][2], raw[db][3], td.vs);
-          if (DRAFT && td.valid < TK) {
-            a0 = keep_keys(a0, 2 * h, g2x4, td.valid);
-            a1 = keep_keys(a1, 2 * h + 1, g2x4, td.valid);
-          }
+          const bf16x8 a0 = codes_to_bf16(raw[db][0], raw[db][1], td.vs);
+          const bf16x8 a1 = codes_to_bf16(raw[db][2], raw[db][3], td.vs);
           o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0, pf[h][0], o_acc[db], 0, 0, 0);
           o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1, pf[h][1], o_acc[db], 0, 0, 0);
         }
@@ -558,12 +535,6 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
       for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
         for (int db = 0; db < DB; ++db) vop[db][c2] = *(const bf16x8 *)(vb + (db * 32 + l32) * L::V_ROW + v_rd[2 * h + c2]);
-      if (DRAFT && td.valid < TK) {
-#pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) vop[db][c2] = keep_keys(vop[db][c2], 2 * (kb0 + h) + c2, g2x4, td.valid);
-      }
 #pragma unroll
       for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
@@ -612,7 +583,7 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
   const float l_tot = pair_sum(l_run);
   const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
   if (!row_ok) return;
-  if (!DRAFT && n_splits == 1) {
+  if (n_splits == 1) {
     __bf16 *orow = out + ((size_t)b * T + my_i) * ((size_t)Hq * D) + (size_t)head * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -655,7 +626,7 @@ __global__ __launch_bounds__(64 * NW, 2) void reuse_attention_kernel(
 // two pairs, and merge through LDS.  For prompts whose row blocks see very different numbers of keys (a whole prompt prefilled): twice the
 // workgroups, each half as long, even out where the longest 256-row block alone takes twice the mean
 // (the rule and its figures: launch_attention).
-template <int D, bool PAIR, bool PART32, bool DRAFT = false>
+template <int D, bool PAIR, bool PART32>
 __global__ __launch_bounds__(512, 2) void reuse_attention_wide_kernel(
     const __bf16 *__restrict__ Q, const __bf16 *__restrict__ Kf, const __bf16 *__restrict__ Vf_blk,
     const __bf16 *__restrict__ k_store, const __bf16 *__restrict__ v_store, const int32_t *__restrict__ table,
@@ -698,7 +669,7 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide_kernel(
   const int row_first = qt * QROWS;
   const int row_last = min(row_first + QROWS, R) - 1;
   const int i_max = (row_first / T == row_last / T) ? (row_last % T) : (T - 1);
-  const int n_tiles = n_cached_tiles + (DRAFT ? 0 : i_max / TK + 1);
+  const int n_tiles = n_cached_tiles + i_max / TK + 1;
   const int tile_begin = (int)((long)split * n_tiles / n_splits);
   const int tile_end = (int)((long)(split + 1) * n_tiles / n_splits);
   const int n_all = tile_end - tile_begin, n = PAIR ? (n_all - odd + 1) / 2 : n_all;   // this wavefront's
@@ -714,7 +685,7 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide_kernel(
   const int w_first = row_first + __builtin_amdgcn_readfirstlane(row_wave) * 32, w_last = min(w_first + 31, R - 1);
   const bool one_head = w_first / T == w_last / T;
   const int mask_from = one_head ? max(w_first % T - (TK - 1), -1) : -1;
-  const int i_hi = w_first >= R ? -2 : DRAFT ? -1 : one_head ? w_last % T : T - 1;
+  const int i_hi = w_first >= R ? -2 : one_head ? w_last % T : T - 1;
 
   bf16x8 qf[KS];
   {
@@ -874,17 +845,11 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide_kernel(
 #pragma unroll
       for (int db = 0; db < DB; ++db) vop0[db][c2] = *(const bf16x8 *)(vb + (db * 32 + l32) * L::V_ROW + v_rd[c2]);
     const int t_valid = min(TK, q_rem), t_t0 = q_t0;
-    if (__builtin_expect(t_valid < TK || (!DRAFT && t_t0 > mask_from), 0)) {
+    if (__builtin_expect(t_valid < TK || t_t0 > mask_from, 0)) {
       int t_lane = g2 * 4;
       asm volatile("" : "+v"(t_lane));   // (keeps the 32 per-element key indices out of loop-invariant registers)
       const int lim_valid = t_valid - t_lane;
-      const int lim_causal = !DRAFT && t_t0 >= 0 ? my_i - t_t0 - t_lane : 0x7fffff00;
-      if constexpr (DRAFT) {
-#pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) vop0[db][c2] = keep_keys(vop0[db][c2], c2, t_lane, t_valid);
-      }
+      const int lim_causal = t_t0 >= 0 ? my_i - t_t0 - t_lane : 0x7fffff00;
 #pragma unroll
       for (int kbk = 0; kbk < 2; ++kbk)
 #pragma unroll
@@ -943,14 +908,6 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide_kernel(
     for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
       for (int db = 0; db < DB; ++db) vop1[db][c2] = *(const bf16x8 *)(vb + (db * 32 + l32) * L::V_ROW + v_rd[2 + c2]);
-    if (DRAFT && __builtin_expect(t_valid < TK, 0)) {
-      int t_lane = g2 * 4;
-      asm volatile("" : "+v"(t_lane));
-#pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) vop1[db][c2] = keep_keys(vop1[db][c2], 2 + c2, t_lane, t_valid);
-    }
 #pragma unroll
     for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
@@ -1037,7 +994,7 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide_kernel(
   const float l_tot = pair_sum(l_run);
   const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
   if (!row_ok) return;
-  if (!DRAFT && n_splits == 1) {
+  if (n_splits == 1) {
     __bf16 *orow = out + ((size_t)b * T + my_i) * ((size_t)Hq * D) + (size_t)head * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -1066,7 +1023,7 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide_kernel(
 // bf16 already and are requested straight into their bf16 stage.  The converted values are stored with ds_write
 // instructions the compiler does not see as stores to the LDS array: with ordinary stores to it, it waits for every
 // outstanding request before each operand read.
-template <int D, bool PART32, bool DRAFT = false>
+template <int D, bool PART32>
 __global__ __launch_bounds__(512, 2) void reuse_attention_wide8_kernel(
     const __bf16 *__restrict__ Q, const __bf16 *__restrict__ Kf, const __bf16 *__restrict__ Vf_blk,
     const uint8_t *__restrict__ k_store, const uint8_t *__restrict__ v_store, const float *__restrict__ k_scale,
@@ -1105,7 +1062,7 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide8_kernel(
   const int row_first = qt * QROWS;
   const int row_last = min(row_first + QROWS, R) - 1;
   const int i_max = (row_first / T == row_last / T) ? (row_last % T) : (T - 1);
-  const int n_tiles = n_cached_tiles + (DRAFT ? 0 : i_max / TK + 1);
+  const int n_tiles = n_cached_tiles + i_max / TK + 1;
   const int tile_begin = (int)((long)split * n_tiles / n_splits);
   const int tile_end = (int)((long)(split + 1) * n_tiles / n_splits);
   const int n = tile_end - tile_begin;
@@ -1121,7 +1078,7 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide8_kernel(
   const int w_first = row_first + __builtin_amdgcn_readfirstlane(wave) * 32, w_last = min(w_first + 31, R - 1);
   const bool one_head = w_first / T == w_last / T;
   const int mask_from = one_head ? max(w_first % T - (TK - 1), -1) : -1;
-  const int i_hi = w_first >= R ? -2 : DRAFT ? -1 : one_head ? w_last % T : T - 1;
+  const int i_hi = w_first >= R ? -2 : one_head ? w_last % T : T - 1;
 
   bf16x8 qf[KS];
   {
@@ -1346,17 +1303,11 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide8_kernel(
 #pragma unroll
       for (int db = 0; db < DB; ++db) vop0[db][c2] = *(const bf16x8 *)(vb + (db * 32 + l32) * L::V_ROW + v_rd[c2]);
     const int t_valid = m_valid, t_t0 = m_t0;
-    if (__builtin_expect(t_valid < TK || (!DRAFT && t_t0 > mask_from), 0)) {
+    if (__builtin_expect(t_valid < TK || t_t0 > mask_from, 0)) {
       int t_lane = g2 * 4;
       asm volatile("" : "+v"(t_lane));   // (keeps the 32 per-element key indices out of loop-invariant registers)
       const int lim_valid = t_valid - t_lane;
-      const int lim_causal = !DRAFT && t_t0 >= 0 ? my_i - t_t0 - t_lane : 0x7fffff00;
-      if constexpr (DRAFT) {
-#pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2)
-#pragma unroll
-          for (int db = 0; db < DB; ++db) vop0[db][c2] = keep_keys(vop0[db][c2], c2, t_lane, t_valid);
-      }
+      const int lim_causal = t_t0 >= 0 ? my_i - t_t0 - t_lane : 0x7fffff00;
 #pragma unroll
       for (int kbk = 0; kbk < 2; ++kbk)
 #pragma unroll
@@ -1415,14 +1366,6 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide8_kernel(
     for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
       for (int db = 0; db < DB; ++db) vop1[db][c2] = *(const bf16x8 *)(vb + (db * 32 + l32) * L::V_ROW + v_rd[2 + c2]);
-    if (DRAFT && __builtin_expect(t_valid < TK, 0)) {
-      int t_lane = g2 * 4;
-      asm volatile("" : "+v"(t_lane));
-#pragma unroll
-      for (int c2 = 0; c2 < 2; ++c2)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) vop1[db][c2] = keep_keys(vop1[db][c2], 2 + c2, t_lane, t_valid);
-    }
 #pragma unroll
     for (int c2 = 0; c2 < 2; ++c2)
 #pragma unroll
@@ -1479,7 +1422,7 @@ __global__ __launch_bounds__(512, 2) void reuse_attention_wide8_kernel(
   const float l_tot = pair_sum(l_run);
   const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
   if (!row_ok) return;
-  if (!DRAFT && n_splits == 1) {
+  if (n_splits == 1) {
     __bf16 *orow = out + ((size_t)b * T + my_i) * ((size_t)Hq * D) + (size_t)head * D;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -1756,19 +1699,16 @@ static pc_status launch_combine(percache_ctx *ctx, const P *part_o, const float 
 
 pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const __bf16 *kf, const __bf16 *vf, const __bf16 *vf_blk,
                            const RawQkv *raw, int batch, int t_fresh, const int32_t *table_dev, int tbl_stride, int min_tiles,
-                           int n_splits, __bf16 *out, void *part_dev, float *part_ml, hipStream_t stream, int formats, int *left_splits,
-                           const DraftView *draft) {
+                           int n_splits, __bf16 *out, void *part_dev, float *part_ml, hipStream_t stream, int formats, int *left_splits) {
   const percache_config &c = ctx->cfg;
   const int G = c.n_q_heads / c.n_kv_heads, R = G * t_fresh;
   if (decode_rows(c, t_fresh)) {
     float *part_o = (float *)part_dev;
     prof_begin(ctx, PC_KERNEL_ATTENTION, stream);
     const pc_status st = launch_decode_attention(ctx, layer, q, kf, vf, raw, batch, t_fresh, table_dev, tbl_stride,
-                                                 min_tiles - (draft ? 0 : (t_fresh + TK - 1) / TK), n_splits, left_splits ? *left_splits : 0, out, part_o, part_ml, stream,
-                                                 formats, draft);
+                                                 min_tiles - (t_fresh + TK - 1) / TK, n_splits, left_splits ? *left_splits : 0, out, part_o, part_ml, stream, formats);
     if (st != PC_OK) return st;
     prof_end(ctx, PC_KERNEL_ATTENTION, stream);
-    if (draft) return n_splits > 1 ? launch_draft_merge(ctx, part_o, part_ml, n_splits, nullptr, nullptr, nullptr, batch, t_fresh, *draft, out, stream) : PC_OK;
     const bool left = left_splits && n_splits <= *left_splits;
     if (left_splits) *left_splits = left ? n_splits : 1;
     return n_splits > 1 && !left ? launch_combine(ctx, part_o, part_ml, n_splits, batch, t_fresh, out, stream) : PC_OK;
@@ -1788,15 +1728,15 @@ pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const 
   // tile between them -- twice the workgroups, half the dependent chain per tile
   const bool halved = !wide && !use8 && c.head_dim == 128 &&
                       (long)batch * c.n_kv_heads * ((R + 63) / 64) * 4 <= ctx->n_cu;
-  const int fresh_tiles = draft ? 0 : (t_fresh + TK - 1) / TK;
+  const int fresh_tiles = (t_fresh + TK - 1) / TK;
   const int cap = max_splits_for(c, ctx->n_cu, batch, t_fresh);
-  const bool pair = !draft && n_splits <= 0 && wide && !use8 && (tbl_stride - kTblHeader) / 2 <= 64 && pair_pays(c, ctx->n_cu, batch, t_fresh, min_tiles - fresh_tiles, cap);
+  const bool pair = n_splits <= 0 && wide && !use8 && (tbl_stride - kTblHeader) / 2 <= 64 && pair_pays(c, ctx->n_cu, batch, t_fresh, min_tiles - fresh_tiles, cap);
   const int qrows = pair ? 128 : wide ? 256 : halved ? 64 : 128;
   const int q_tiles = (R + qrows - 1) / qrows;
   // A prompt with more fresh than cached tiles: the workgroups are of unequal length as it is and go heaviest first, so more
   // workgroups than CUs even out without partitions (4224 fresh rows x 16 heads over nothing cached, 264 workgroups, layer of a
   // stack: 1 partition 360 us, 2 363, 4 373 with a merge of 14; before, lightest first and every fresh tile masked: 411 to 421).
-  const bool uneven = !draft && wide && 2 * fresh_tiles > min_tiles && (long)batch * c.n_kv_heads * q_tiles >= ctx->n_cu;
+  const bool uneven = wide && 2 * fresh_tiles > min_tiles && (long)batch * c.n_kv_heads * q_tiles >= ctx->n_cu;
   if (n_splits <= 0 && (uneven || pair)) n_splits = 1;
   if (n_splits <= 0) {
     const bool d128 = c.head_dim == 128;
@@ -1804,13 +1744,11 @@ pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const 
                           : halved ? TilePace{0.79, 1.58}
                           : d128 ? (use8 ? TilePace{1.17, 1.12} : TilePace{1.16, 1.51}) : use8 ? TilePace{1.12, 1.05} : TilePace{0.68, 1.07};
     const double merge_us = (double)batch * c.n_q_heads * t_fresh * c.head_dim * 4 / 5.4e6;   // a partition's bf16 partials, written and read at 5.4 TB/s
-    const Partitions parts = choose_partitions(pace, ctx->n_cu, (long)batch * c.n_kv_heads, q_tiles, min_tiles, d128 && use8 ? 5 : 7, merge_us, draft ? 2 * cap : cap);
+    const Partitions parts = choose_partitions(pace, ctx->n_cu, (long)batch * c.n_kv_heads, q_tiles, min_tiles, d128 && use8 ? 5 : 7, merge_us, cap);
     n_splits = parts.n;
     part32 = parts.f32;
   }
   if (n_splits > cap) n_splits = cap;
-  if (draft && min_tiles == 0)   // (nothing cached)
-    return launch_draft_merge(ctx, nullptr, nullptr, 0, q, kf, vf, batch, t_fresh, *draft, out, stream);
   const void *ks, *vs;
   const float *ksc = nullptr, *vsc = nullptr;
   const __bf16 *k16 = ctx->k_store + (size_t)layer * ctx->layer_stride, *v16 = ctx->v_store + (size_t)layer * ctx->layer_stride;
@@ -1842,30 +1780,7 @@ pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const 
   hipLaunchKernelGGL((reuse_attention_wide8_kernel<128, PP>), grid, dim3(512), 0, stream, q, kf, vf_blk, (const uint8_t *)ks, (const uint8_t *)vs, ksc, vsc, \
                      ctx->n_slots16, table_dev, tbl_stride, t_fresh, c.n_q_heads, c.n_kv_heads, c.slot_capacity, n_splits, q_tiles, n_groups, scale_log2e, \
                      out, part_o, part_ml)
-#define PC_DRAFT(DD, NWW, NS, KV, KS, MX)                                                                                     \
-  hipLaunchKernelGGL((reuse_attention_kernel<DD, NWW, NS, KV, KS, MX, true, true>), grid, dim3(64 * NWW), 0, stream, q, kf, vf_blk, ks, vs, ksc, vsc, k16, v16, \
-                     ctx->n_slots16, table_dev, tbl_stride, t_fresh, c.n_q_heads, c.n_kv_heads, c.slot_capacity, n_splits, q_tiles, n_groups, scale_log2e, \
-                     out, part_o, part_ml)
-#define PC_DRAFT_WIDE(DD)                                                                                                             \
-  hipLaunchKernelGGL((reuse_attention_wide_kernel<DD, false, true, true>), grid, dim3(512), 0, stream, q, kf, vf_blk, k16, v16, table_dev, tbl_stride, \
-                     t_fresh, c.n_q_heads, c.n_kv_heads, c.slot_capacity, n_splits, q_tiles, n_groups, scale_log2e, out, part_o, part_ml)
-  const bool few_chunks = (tbl_stride - kTblHeader) / 2 <= 64;
-  if (draft && c.head_dim == 128) {
-    if (mixed) { if (wide) PC_DRAFT(128, 8, 2, true, 1, true); else PC_DRAFT(128, 4, 2, true, 1, true); }
-    else if (use8 && wide && few_chunks && c.slot_capacity / TK <= 32)
-      hipLaunchKernelGGL((reuse_attention_wide8_kernel<128, true, true>), grid, dim3(512), 0, stream, q, kf, vf_blk, (const uint8_t *)ks, (const uint8_t *)vs, ksc, vsc,
-                         ctx->n_slots16, table_dev, tbl_stride, t_fresh, c.n_q_heads, c.n_kv_heads, c.slot_capacity, n_splits, q_tiles, n_groups, scale_log2e,
-                         out, part_o, part_ml);
-    else if (use8) { if (wide) PC_DRAFT(128, 8, 2, true, 1, false); else PC_DRAFT(128, 4, 2, true, 1, false); }
-    else if (wide) { if (few_chunks) PC_DRAFT_WIDE(128); else PC_DRAFT(128, 8, 2, false, 1, false); }
-    else if (halved) PC_DRAFT(128, 4, 2, false, 2, false);
-    else PC_DRAFT(128, 4, 2, false, 1, false);
-  } else if (draft) {
-    if (mixed) PC_DRAFT(64, 4, 2, true, 1, true);
-    else if (use8) PC_DRAFT(64, 4, 2, true, 1, false);
-    else if (wide) { if (few_chunks) PC_DRAFT_WIDE(64); else PC_DRAFT(64, 8, 4, false, 1, false); }
-    else PC_DRAFT(64, 4, 4, false, 1, false);
-  } else if (use8 && mixed) {
+  if (use8 && mixed) {
     if (c.head_dim == 128) {
       if (wide) PC_ATTN(128, 8, 2, true, 1, true); else PC_ATTN(128, 4, 2, true, 1, true);
     } else {
@@ -1888,8 +1803,6 @@ pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const 
   } else {
     if (wide) PC_ATTN(64, 8, 4, false, 1, false); else PC_ATTN(64, 4, 4, false, 1, false);
   }
-#undef PC_DRAFT_WIDE
-#undef PC_DRAFT
 #undef PC_WIDE8_P
 #undef PC_ATTN_P
 #undef PC_WIDE
@@ -1897,7 +1810,6 @@ pc_status launch_attention(percache_ctx *ctx, int layer, const __bf16 *q, const 
 #undef PC_ATTN
   prof_end(ctx, PC_KERNEL_ATTENTION, stream);
   PC_HIP(ctx, hipGetLastError());
-  if (draft) return launch_draft_merge(ctx, (const float *)part_dev, part_ml, n_splits, q, kf, vf, batch, t_fresh, *draft, out, stream);
   if (n_splits == 1) return PC_OK;
   return part32 ? launch_combine(ctx, (const float *)part_dev, part_ml, n_splits, batch, t_fresh, out, stream)
                 : launch_combine(ctx, part_o, part_ml, n_splits, batch, t_fresh, out, stream);
