@@ -135,68 +135,108 @@ struct Image {
   static constexpr int HALF = kKvTile * D * 2, BYTES = 2 * HALF + 256;
 };
 
-// One workgroup a (slot, kv head, 64 kept tokens): the tokens' K rows and V columns are gathered into LDS as a bf16 block (8-bit slots: code * 2^e, exact), and
-// written in the destination's format, an 8-bit block quantised afresh.  K: 16-byte pieces of the tokens' rows.  V: a token is one element in each of the D rows of
-// its block, so a lane takes two neighbouring places of the new block and goes down the rows: two 2-byte loads from the few lines that hold 64 kept tokens, one
-// 4-byte LDS store.
+// One workgroup a (slot, kv head, 64 kept tokens): the tokens' K rows are gathered in registers as bf16 (8-bit slots: code * 2^e, exact), V in LDS as a bf16 block, and
+// written in the destination's format, an 8-bit block quantised afresh.  K: 16-byte pieces of the tokens' rows.  V: a token is one element in each of the D rows of its
+// block, so the blocks that hold kept tokens are read one after the other, 16 bytes of a row a lane (left out where none of them is kept), and the kept elements
+// put where they belong; read element by element, two bytes a lane, the addresses took longer than the bytes.  16 slots x 8 heads, 1000 of 1536 tokens
+// on average, D = 128, half of either format: 43.6 us element by element, 30.2 so (111 MB).
 template <int D>
 __global__ __launch_bounds__(256) void keep_move_kernel(Store st, const Moves mv, const int32_t *__restrict__ idx, int idx_stride, int Hkv, int C, char *__restrict__ images,
                                                         int tiles) {
-  constexpr int KP = D / 8, V_ROW = kKvTile + 8;     // 16-byte pieces of a K row; elements of a V row in LDS (padded)
-  __shared__ __align__(16) __bf16 lk[kKvTile * D], lv[D * V_ROW];
-  __shared__ int32_t list[kKvTile];
+  constexpr int KP = D / 8, KR = kKvTile * KP / 256, V_ROW = kKvTile + 8;     // 16-byte pieces of a K row, and a thread's; elements of a V row in LDS (the last 8 unused)
+  __shared__ __align__(16) __bf16 lv[D * V_ROW];
+  __shared__ int32_t list[kKvTile], from[kKvTile], rank0[kKvTile];      // kept tokens; source blocks that hold some, and the first of theirs
+  __shared__ unsigned long long held[kKvTile];                          // which of a source block's tokens are kept
+  __shared__ int n_from;
   __shared__ float red[4][2];
   const int z = blockIdx.z, g = blockIdx.y, tile = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int src = mv.src[z], dst = mv.dst[z], n = min(mv.keep[z], mv.have[z]) - tile * kKvTile;   // kept tokens from this block on
   if (n <= 0) return;
   const bool src8 = src >= st.n_slots16, dst8 = dst >= st.n_slots16;
   const size_t sh = (size_t)(src8 ? src - st.n_slots16 : src) * Hkv + g, dh = (size_t)(dst8 ? dst - st.n_slots16 : dst) * Hkv + g;
-  if (tid < kKvTile) list[tid] = tid < n ? idx[((size_t)z * Hkv + g) * idx_stride + tile * kKvTile + tid] : -1;
-  __syncthreads();
   const int bpc = C / kKvTile;
-#pragma unroll
-  for (int r = 0; r < kKvTile * KP / 256; ++r) {
-    const int e = tid + r * 256, t = list[e / KP], c = e % KP;
-    pc::u32x4 w = {0, 0, 0, 0};
-    if (t >= 0) {
-      if (src8) {
-        const uint2 q = *(const uint2 *)(st.k8 + (sh * C + t) * D + c * 8);
-        const float s = st.k_scale[sh * bpc + t / kKvTile];
-        pc::bf16x8 v;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) v[x] = (__bf16)(__builtin_amdgcn_cvt_f32_fp8((int)((x < 4 ? q.x : q.y) >> (8 * (x & 3))), 0) * s);
-        w = __builtin_bit_cast(pc::u32x4, v);
-      } else {
-        w = *(const pc::u32x4 *)(st.k16 + (sh * C + t) * D + c * 8);
-      }
+  if (tid < kKvTile) {   // (one wavefront)
+    const int t = tid < n ? idx[((size_t)z * Hkv + g) * idx_stride + tile * kKvTile + tid] : -1;
+    const int block = t >= 0 ? t / kKvTile : -1, before = __shfl_up(block, 1, 64);
+    const bool first = t >= 0 && (lane == 0 || block != before);
+    const unsigned long long firsts = __ballot(first);
+    const int r = __popcll(firsts & (~0ull >> (63 - lane))) - 1;
+    list[lane] = t;
+    held[lane] = 0;
+    if (first) {
+      from[r] = block;
+      rank0[r] = lane;
     }
-    *(pc::u32x4 *)(lk + e * 8) = w;
+    if (lane == 0) n_from = __popcll(firsts);
+    __builtin_amdgcn_wave_barrier();
+    if (t >= 0) atomicOr(&held[r], 1ull << (t % kKvTile));
   }
-  {
-    const int p = 2 * (lane & 31);   // (p and p + 1 hold neighbouring keys)
-    const int key = (p & ~15) + pc::blocked_key(p & 15), t[2] = {list[key], list[key + 1]};
-    size_t at[2];
-    float s[2] = {1.f, 1.f};
+  if (n < kKvTile)   // places that no token fills
+    for (int e = tid; e < D * V_ROW / 8; e += 256) *(pc::u32x4 *)(lv + e * 8) = pc::u32x4{0, 0, 0, 0};
+  __syncthreads();
+  pc::u32x4 kr[KR];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int tc = max(t[x], 0), in = tc % kKvTile;
-      at[x] = (sh * C + (tc - in)) * D + (src8 ? pc::blocked_pos8(in) : (in & ~15) + pc::blocked_key(in & 15));
-      if (src8) s[x] = st.v_scale[sh * bpc + tc / kKvTile];
-    }
-#pragma unroll 8
-    for (int r = 0; r < D / 8; ++r) {
-      const int d = r * 8 + wave * 2 + (lane >> 5);
-      unsigned w = 0;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        __bf16 v;
-        if (src8) v = (__bf16)(__builtin_amdgcn_cvt_f32_fp8((int)st.v8[at[x] + (size_t)d * kKvTile], 0) * s[x]);
-        else v = st.v16[at[x] + (size_t)d * kKvTile];
-        w |= (t[x] >= 0 ? (unsigned)__builtin_bit_cast(unsigned short, v) : 0u) << (16 * x);
-      }
-      *(unsigned *)(lv + d * V_ROW + p) = w;
+  for (int r = 0; r < KR; ++r) {
+    const int e = tid + r * 256, t = max(list[e / KP], 0), c = e % KP;
+    if (src8) {
+      const uint2 q = *(const uint2 *)(st.k8 + (sh * C + t) * D + c * 8);
+      kr[r] = pc::u32x4{q.x, q.y, __float_as_uint(st.k_scale[sh * bpc + t / kKvTile]), 0};
+    } else {
+      kr[r] = *(const pc::u32x4 *)(st.k16 + (sh * C + t) * D + c * 8);
     }
   }
+  // V: a thread has the same 16 bytes of every row that it reads of a block, E tokens
+  auto gather_v = [&](auto src8_c) __attribute__((always_inline)) {
+    constexpr bool S8 = decltype(src8_c)::value;
+    constexpr int E = S8 ? 16 : 8, PER = kKvTile / E, N = D * PER / 256;
+    const int c = tid % PER, d0 = tid / PER;
+    const int nf = n_from;
+    for (int f = 0; f < nf; ++f) {
+      const unsigned long long m = held[f];
+      const int block = from[f];
+      // (the keys of these places: the first one's, and steps from it that do not depend on the thread -- see blocked_key, blocked_key8)
+      const int key0 = S8 ? 32 * (c >> 1) + 4 * (c & 1) : 16 * (c >> 1) + 4 * (c & 1), r0 = rank0[f] + __popcll(m & ((1ull << key0) - 1));
+      const unsigned mine = (unsigned)(m >> key0);
+      int to[E];
+      bool any = false;
+#pragma unroll
+      for (int y = 0; y < E; ++y) {
+        const int step = (S8 ? 16 * (y >> 3) + 8 * (y >> 2 & 1) : 8 * (y >> 2)) + (y & 3), kept = r0 + __popc(mine & ((1u << step) - 1));
+        const bool is = mine >> step & 1;
+        to[y] = is ? (kept & ~15) + pc::blocked_key(kept & 15) : kKvTile;   // (the others: into the padding)
+        any |= is;
+      }
+      if (!any) continue;
+      const float s = S8 ? st.v_scale[sh * bpc + block] : 1.f;
+      const char *p = (S8 ? (const char *)st.v8 : (const char *)st.v16) + ((sh * C + (size_t)block * kKvTile) * D + c * E) * (S8 ? 1 : 2) + d0 * kKvTile * (S8 ? 1 : 2);
+      pc::u32x4 w[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = *(const pc::u32x4 *)(p + i * (256 / PER) * kKvTile * (S8 ? 1 : 2));
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        __bf16 *row = lv + (d0 + i * (256 / PER)) * V_ROW;
+#pragma unroll
+        for (int y = 0; y < E; ++y) {
+          if (S8) row[to[y]] = (__bf16)(__builtin_amdgcn_cvt_f32_fp8((int)(w[i][y / 4] >> (8 * (y & 3))), 0) * s);
+          else row[to[y]] = __builtin_bit_cast(pc::bf16x8, w[i])[y];
+        }
+      }
+    }
+  };
+  if (src8) gather_v(std::true_type{}); else gather_v(std::false_type{});
+  if (src8) {
+#pragma unroll
+    for (int r = 0; r < KR; ++r) {
+      const float s = __uint_as_float(kr[r][2]);
+      pc::bf16x8 v;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x] = (__bf16)(__builtin_amdgcn_cvt_f32_fp8((int)(kr[r][x >> 2] >> (8 * (x & 3))), 0) * s);
+      kr[r] = __builtin_bit_cast(pc::u32x4, v);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < KR; ++r)
+    if (list[(tid + r * 256) / KP] < 0) kr[r] = pc::u32x4{0, 0, 0, 0};
   __syncthreads();
   char *const image = images ? images + (((size_t)z * Hkv + g) * tiles + tile) * Image<D>::BYTES : nullptr;
   const bool through = src == dst;   // (in place: the block's image)
@@ -205,7 +245,7 @@ __global__ __launch_bounds__(256) void keep_move_kernel(Store st, const Moves mv
 #pragma unroll
     for (int r = 0; r < kKvTile * KP / 256; ++r) {
       const int e = tid + r * 256;
-      if (e / KP < n) *(pc::u32x4 *)(ko + e * 16) = *(const pc::u32x4 *)(lk + e * 8);
+      if (e / KP < n) *(pc::u32x4 *)(ko + e * 16) = kr[r];
       *(pc::u32x4 *)(vo + e * 16) = *(const pc::u32x4 *)(lv + e / 8 * V_ROW + e % 8 * 8);
     }
     return;
@@ -214,7 +254,7 @@ __global__ __launch_bounds__(256) void keep_move_kernel(Store st, const Moves mv
 #pragma unroll
   for (int r = 0; r < kKvTile * KP / 256; ++r) {
     const int e = tid + r * 256;
-    const pc::bf16x8 k = *(const pc::bf16x8 *)(lk + e * 8), v = *(const pc::bf16x8 *)(lv + e / 8 * V_ROW + e % 8 * 8);
+    const pc::bf16x8 k = __builtin_bit_cast(pc::bf16x8, kr[r]), v = *(const pc::bf16x8 *)(lv + e / 8 * V_ROW + e % 8 * 8);
 #pragma unroll
     for (int x = 0; x < 8; ++x) {
       amax[0] = fmaxf(amax[0], fabsf((float)k[x]));
@@ -237,8 +277,8 @@ __global__ __launch_bounds__(256) void keep_move_kernel(Store st, const Moves mv
     if (through) ((float *)(image + 2 * Image<D>::HALF))[tid] = s;
     else (tid ? st.v_scale : st.k_scale)[dh * bpc + tile] = s;
   }
-  auto codes = [&](const __bf16 *x, float inv) __attribute__((always_inline)) {
-    const pc::bf16x8 v = *(const pc::bf16x8 *)x;
+  auto codes = [&](pc::u32x4 x, float inv) __attribute__((always_inline)) {
+    const pc::bf16x8 v = __builtin_bit_cast(pc::bf16x8, x);
     return make_uint2(pc::fp8::encode4((float)v[0] * inv, (float)v[1] * inv, (float)v[2] * inv, (float)v[3] * inv),
                       pc::fp8::encode4((float)v[4] * inv, (float)v[5] * inv, (float)v[6] * inv, (float)v[7] * inv));
   };
@@ -246,10 +286,10 @@ __global__ __launch_bounds__(256) void keep_move_kernel(Store st, const Moves mv
 #pragma unroll
   for (int r = 0; r < kKvTile * KP / 256; ++r) {
     const int e = tid + r * 256;
-    if (e / KP < n) *(uint2 *)(ko + e * 8) = codes(lk + e * 8, ki);
+    if (e / KP < n) *(uint2 *)(ko + e * 8) = codes(kr[r], ki);
     // bytes 8 c .. of a V row are the bf16 block's elements 8 c' .., c' = c with its two low bits exchanged (blocked_key8, blocked_key)
-    const int c = e % 8, from = (c & 4) | (c & 1) << 1 | (c & 2) >> 1;
-    *(uint2 *)(vo + e * 8) = codes(lv + e / 8 * V_ROW + from * 8, vi);
+    const int c = e % 8, at = (c & 4) | (c & 1) << 1 | (c & 2) >> 1;
+    *(uint2 *)(vo + e * 8) = codes(*(const pc::u32x4 *)(lv + e / 8 * V_ROW + at * 8), vi);
   }
 }
 
