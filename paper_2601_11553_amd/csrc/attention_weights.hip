@@ -2,8 +2,9 @@
 // handed out.  With it the softmax needs no second pass, so a key's weight is one product and one exponential a row, and the keys are read once.
 //
 // The keys stay, the rows pass by: a slot's keys are matrix operands that go over the rows of every query that uses the slot, 32 rows at a
-// time.  So a slot shared by several queries (a system prompt's chunk) is read once, its sums have one owner and one order -- no atomics, no
-// second launch -- and are added to the running sums in place.  The rows are on the M side of the product: a lane then has 16 rows of one
+// time.  So a slot shared by several queries (a system prompt's chunk) is read once, its sums have one owner and one order -- no atomics -- and are added to the
+// running sums in place; only where that would keep one wavefront at work when the others are done are a slot's users split among several, whose sums a second
+// launch adds up (weights_join_kernel).  The rows are on the M side of the product: a lane then has 16 rows of one
 // key, whose exponentials it adds up by itself.  The log-sum-exp, which belongs to rows, comes in as one more step of the contraction: -lse sqrt(D) as
 // the sum of three bf16 numbers (24 bits) against ones.
 //
@@ -21,13 +22,23 @@ using pc::u32x4;
 using pc::dec::codes8;
 using pc::dec::fast_exp2;
 
-// Lists of a call (int32 words): the entries, the users of those that have not just one, then -- with paths -- their n_path [batch] and nodes [batch][max_path].
+// Lists of a call (int32 words): the entries, the users of those that have not just one, the slots split among several entries, then -- with paths -- n_path [batch] and the
+// nodes [batch][max_path].
 struct Entry {
   int32_t slot;     // slot id; -1 - b: the draft keys of query b
-  int32_t piece0;   // first of its pieces among all entries'
-  int32_t keys;     // 32 x the longest used length among its users, + the 64-key tiles of a piece (at most 31)
-  int32_t user;     // its one user, who uses all of its keys; -1 - u: two words per user from word u of the users on, behind their number (two words)
+  int32_t piece0;   // first of its pieces among all entries' (few rows: the cost of the entries before it)
+  int32_t keys;     // 32 x the longest used length among its users, + the 64-key tiles of a piece (few rows: what a tile costs; at most 31)
+  int32_t user;     // its one user, who uses all of its keys; -1 - u: the u-th of the users' records is {their number, of a split slot 1 + the place of its sums}, theirs are behind it
 };
+struct User {
+  int32_t query, used, rows, unused;   // rows: counting rows of a head
+};
+struct Split {
+  int32_t slot, longest, parts, place;   // place: of its first entry's sums in Args::parts, 64 floats each: [entry][kv head][tile]
+};
+// Few rows: what a tile costs for each block of 32 rows.  A tile of draft keys has its rows and what they look at to load for itself, about three tiles' time: eight of them
+// in one share, as a tile each, made a call of 35 us one of 42.
+constexpr int kDraftCost = 3, kMostCost = 31;
 constexpr int kMostKeys = 1 << 26;
 constexpr int kRowsSpan = 2;   // tiles that weights_rows_kernel holds
 
@@ -40,28 +51,28 @@ struct Args {
   int n_slots16;
   const Entry *entries;
   int n_entries;
-  const int2 *users;
+  const User *users;
   const int32_t *n_path, *path;  // null: every row counts
   int max_path;
+  int share;                     // few rows: the cost that a wavefront takes
   int T, Hq, Hkv, C;
   float scale_log2e, sqrt_d;
   const float *w_in;   // [slots][Hkv][C], may be null (zero) and may be w_out
-  float *w_out, *w_draft;
+  float *w_out, *w_draft, *parts;
   pc::DraftView draft;
 };
 
-// The entry of a piece: the last one that starts at or before it.  A lane looks at every 64th entry and hands over the words of the one found.
-__device__ __forceinline__ Entry find_entry(const Args &a, int piece, int lane) {
-  int4 mine = {0, 0, 0, 0};
+// The entry of a piece: the last one that starts at or before it (-1: none).  A lane looks at every 64th entry.
+__device__ __forceinline__ int find_entry(const Args &a, int piece, int lane) {
+  int found = -1;
   for (int e0 = 0; e0 < a.n_entries; e0 += 64) {
-    const int4 e = ((const int4 *)a.entries)[min(e0 + lane, a.n_entries - 1)];
-    const unsigned long long before = __ballot(e0 + lane < a.n_entries && e.y <= piece);
+    const int at = ((const int4 *)a.entries)[min(e0 + lane, a.n_entries - 1)].y;
+    const unsigned long long before = __ballot(e0 + lane < a.n_entries && at <= piece);
     if (!before) break;
-    const int at = 63 - __builtin_clzll(before);
-    mine = {__builtin_amdgcn_readlane(e.x, at), __builtin_amdgcn_readlane(e.y, at), __builtin_amdgcn_readlane(e.z, at), __builtin_amdgcn_readlane(e.w, at)};
+    found = e0 + 63 - __builtin_clzll(before);
     if (before != ~0ull) break;
   }
-  return {mine.x, mine.y, mine.z, mine.w};
+  return found;
 }
 
 // The rows that look at an entry's keys, in blocks of 32 (head of the group, counting row) of one user.  A wavefront's view of them.
@@ -70,11 +81,11 @@ struct Rows {
   static constexpr int KS = D / 16;
   const Args &a;
   const int g, lane, l32, g2, G;
-  const Entry ent;
-  const bool is_draft;
-  const int longest;
-  int n_users;
-  const int2 *list;   // (of several users)
+  Entry ent;
+  bool is_draft;
+  int longest;
+  int n_users, place;   // (place: 1 + that of its sums, a split slot's)
+  const User *list;     // (of several users)
   unsigned long long *row_sees;   // [tiles][32] of this wavefront, draft keys: what each row of the block looks at
 
   struct Cursor { int u, r0, R, n_rows, b, used; };
@@ -83,21 +94,34 @@ struct Rows {
   struct Ready { bf16x8 ext; unsigned ok; };
 
   __device__ __forceinline__ Rows(const Args &args, const Entry &e, int g_, int lane_, unsigned long long *sees)
-      : a(args), g(g_), lane(lane_), l32(lane_ & 31), g2(lane_ >> 5), G(args.Hq / args.Hkv), ent(e), is_draft(e.slot < 0), longest(e.keys >> 5), row_sees(sees) {
+      : a(args), g(g_), lane(lane_), l32(lane_ & 31), g2(lane_ >> 5), G(args.Hq / args.Hkv), row_sees(sees) {
+    set(e);
+  }
+  __device__ __forceinline__ void set(const Entry &e) {
+    ent = e;
+    is_draft = e.slot < 0;
+    longest = e.keys >> 5;
     n_users = 1;
+    place = 0;
     list = nullptr;
     if (ent.user < 0) {
       list = a.users + (-1 - ent.user);
-      n_users = list[0].x;
+      n_users = __builtin_amdgcn_readfirstlane(list->query);
+      place = __builtin_amdgcn_readfirstlane(list->used);
       ++list;
     }
   }
   __device__ __forceinline__ void look(Cursor &c) const {
-    int2 user = make_int2(ent.user, longest);
-    if (list) user = list[c.u];
-    c.b = user.x;
-    c.used = user.y;
-    c.n_rows = a.n_path ? a.n_path[c.b] : a.T;
+    if (list) {
+      const User user = list[c.u];
+      c.b = __builtin_amdgcn_readfirstlane(user.query);
+      c.used = __builtin_amdgcn_readfirstlane(user.used);
+      c.n_rows = __builtin_amdgcn_readfirstlane(user.rows);
+    } else {
+      c.b = ent.user;
+      c.used = longest;
+      c.n_rows = a.n_path ? __builtin_amdgcn_readfirstlane(a.n_path[c.b]) : a.T;
+    }
     c.R = G * c.n_rows;
   }
   __device__ __forceinline__ void settle(Cursor &c) const {   // over users whose rows lie before row r0
@@ -113,8 +137,18 @@ struct Rows {
     return c;
   }
   __device__ __forceinline__ bool done(const Cursor &c) const { return c.u >= n_users; }
-  __device__ __forceinline__ void request(const Cursor &c, Block &blk) const {
-    const int row = min(c.r0 + l32, c.R - 1), h = row / c.n_rows, j = row - h * c.n_rows, i = a.n_path ? a.path[(size_t)c.b * a.max_path + j] : j;
+  __device__ __forceinline__ Cursor behind(Cursor c) const {
+    c.r0 += 32;
+    settle(c);
+    return c;
+  }
+  // the node of a lane's row (with paths: a load of its own, which request() waits for)
+  __device__ __forceinline__ int node_of(const Cursor &c) const {
+    const int row = min(c.r0 + l32, c.R - 1), j = row % c.n_rows;
+    return a.n_path ? a.path[(size_t)c.b * a.max_path + j] : j;
+  }
+  __device__ __forceinline__ void request(const Cursor &c, int i, Block &blk) const {
+    const int h = min(c.r0 + l32, c.R - 1) / c.n_rows;
     const size_t at = ((size_t)c.b * a.Hq + g * G + h) * a.T + i;
     blk.lse = a.lse[at];
 #pragma unroll
@@ -205,6 +239,12 @@ struct Rows {
   __device__ __forceinline__ size_t weight_at(int t0) const {
     return is_draft ? ((size_t)(-1 - ent.slot) * a.Hkv + g) * a.T + t0 + lane : ((size_t)ent.slot * a.Hkv + g) * a.C + t0 + lane;
   }
+  // where a tile's sums go, and whether what stands there is added to
+  __device__ __forceinline__ bool adds() const { return !is_draft && !place && a.w_in; }
+  __device__ __forceinline__ float *sums_at(int t0) const {
+    if (place) return a.parts + ((size_t)(place - 1) + (size_t)g * ((longest + kKvTile - 1) / kKvTile) + t0 / kKvTile) * kKvTile + lane;
+    return (is_draft ? a.w_draft : a.w_out) + weight_at(t0);
+  }
   // the row of a key, bf16 and (8-bit slots) codes
   __device__ __forceinline__ bool is8(int fmt) const { return fmt != 0 && !is_draft && (fmt == 1 || ent.slot >= a.n_slots16); }
   __device__ __forceinline__ const __bf16 *keys16() const {
@@ -213,89 +253,171 @@ struct Rows {
   __device__ __forceinline__ size_t head8() const { return (size_t)(ent.slot - a.n_slots16) * a.Hkv + g; }
 };
 
-// Few rows: one wavefront walks the tiles of a piece with the keys in registers, the next tile's requested ahead, and its rows -- where they are one block -- loaded
-// once.  Up to 2 wavefronts a SIMD, each with 16 KB on the way.  FMT: 0 bf16 slots, 1 8-bit slots, 2 both.
+// Few rows: one wavefront walks a share of all tiles with the keys in registers, the next tile's requested ahead -- across the end of an entry, too --, and its rows --
+// where they are one block -- loaded once for all tiles of a query.  The shares are equal, so that all end together: a tile counts as one, or as what its blocks of rows make
+// of it (Entry::keys), and belongs to the share that it starts in.  Up to 2 wavefronts a SIMD, each with 16 KB on the way.  FMT: 0 bf16 slots, 1 8-bit slots, 2 both.
+// 8 queries, 15 rows of a kv head (24 heads over 8) over 12.4k keys each, one chunk shared: 195 MB in 37.5 us (5.2 TB/s); 48.6 with the keys loaded as operands and with pieces of at most six tiles of one slot.
 template <int D, int FMT>
 __global__ __launch_bounds__(64, 2) void weights_stream_kernel(const Args a) {
   constexpr int KS = D / 16;
+  __shared__ __align__(16) char stage[kKvTile * D * 2];
   __shared__ __align__(16) unsigned long long row_sees[32];
-  const int lane = threadIdx.x, g = blockIdx.x % a.Hkv, piece = blockIdx.x / a.Hkv;
-  const Rows<D> rows(a, find_entry(a, piece, lane), g, lane, row_sees);
-  const int longest = rows.longest, span = rows.ent.keys & 31, tile0 = (piece - rows.ent.piece0) * span, tile_end = min(tile0 + span, (longest + kKvTile - 1) / kKvTile);
-  const bool is8 = rows.is8(FMT);
-  u32x4 raw[2][KS];
-  float raw_scale = 1.f;
-  auto request_keys = [&](int tile) __attribute__((always_inline)) {
-    const int t0 = tile * kKvTile, last = min(kKvTile, longest - t0) - 1;   // (past a ragged end: the last key's)
-    if (FMT != 0 && is8) {
-      const size_t head = rows.head8();
-      raw_scale = a.k_scale[head * (a.C / kKvTile) + tile];
+  const int lane = threadIdx.x, g = blockIdx.x % a.Hkv, lo = blockIdx.x / a.Hkv * a.share, hi = lo + a.share;
+  // the first tile that starts in [lo, hi)
+  int e = find_entry(a, lo, lane);
+  if (e < 0) return;
+  auto entry = [&](int at) __attribute__((always_inline)) {
+    const int4 w = ((const int4 *)a.entries)[at];
+    return Entry{w.x, w.y, w.z, w.w};
+  };
+  auto tiles_of = [](const Entry &x) __attribute__((always_inline)) { return ((x.keys >> 5) + kKvTile - 1) / kKvTile; };
+  auto end_of = [&](const Entry &x) __attribute__((always_inline)) { return min(tiles_of(x), (hi - x.piece0 + (x.keys & 31) - 1) / (x.keys & 31)); };   // behind its tiles in here
+  Entry ent = entry(e);
+  int tile = (lo - ent.piece0 + (ent.keys & 31) - 1) / (ent.keys & 31);
+  if (tile >= tiles_of(ent)) {
+    if (++e >= a.n_entries) return;
+    ent = entry(e);
+    tile = 0;
+  }
+  int tile_end = end_of(ent);
+  if (tile >= tile_end) return;
+  Rows<D> rows(a, ent, g, lane, row_sees);
+  // A tile comes through LDS: instruction i of its request fills bytes [1024 i, +1024), 16-byte chunks XOR-swizzled inside the rows.  (Loaded as operands, 32 bytes of 32 rows an
+  // instruction, a line passes the first-level cache four times: 16 KB of each of 8 wavefronts do not stay in it.)
+  auto swz = [](int row_bytes, int row) __attribute__((always_inline)) { return row_bytes == 256 ? (row & 15) : row_bytes == 128 ? ((row >> 1) & 7) : ((row >> 2) & 3); };
+  float next_scale = 1.f;
+  auto copy = [&](const char *src, auto row_bytes_c, int rows_there) __attribute__((always_inline)) {
+    constexpr int RB = decltype(row_bytes_c)::value, LPR = RB / 16, ROWS = 64 / LPR;   // lanes of a row, rows of an instruction
+    const int row = lane / LPR, c = lane % LPR;
+    auto fill = [&](int i, int from) __attribute__((always_inline)) {
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(src + (unsigned)from), (__attribute__((address_space(3))) void *)(stage + i * 1024), 16, 0, 2);
+    };
+    if (rows_there >= kKvTile) {
+      int base = row * RB + (c ^ swz(RB, row)) * 16;   // (i ROWS reaches the swizzle's upper bits alone)
+      asm volatile("" : "+v"(base));                   // (the addresses do not stay in registers over the tiles)
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const uint8_t *row = a.k8 + (head * a.C + t0 + min(kb * 32 + rows.l32, last)) * D + rows.g2 * 8;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const uint2 w = *(const uint2 *)(row + ks * 16);
-          raw[kb][ks] = u32x4{w.x, w.y, 0, 0};
-        }
-      }
+      for (int i = 0; i < kKvTile / ROWS; ++i) fill(i, i * 1024 + (base ^ (swz(RB, i * ROWS) * 16)));
     } else {
-      const __bf16 *base = rows.keys16();
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        const __bf16 *row = base + (size_t)(t0 + min(kb * 32 + rows.l32, last)) * D + rows.g2 * 8;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) raw[kb][ks] = *(const u32x4 *)(row + ks * 16);
-      }
+#pragma unroll 1
+      for (int i = 0; i < kKvTile / ROWS; ++i) fill(i, min(i * ROWS + row, rows_there - 1) * RB + (c ^ swz(RB, i * ROWS + row)) * 16);
     }
   };
-  request_keys(tile0);
-  const typename Rows<D>::Cursor first = rows.begin(0);
-  typename Rows<D>::Cursor at = first;
+  // (a slot's block is there to its end, whatever stands behind the used length: no key's sum looks at another key.  Behind the draft keys there is nothing.)
+  auto request_keys = [&](const Entry &of, int tile) __attribute__((always_inline)) {
+    const int t0 = tile * kKvTile;
+    if (FMT != 0 && of.slot >= 0 && (FMT == 1 || of.slot >= a.n_slots16)) {
+      const size_t head = (size_t)(of.slot - a.n_slots16) * a.Hkv + g;
+      next_scale = a.k_scale[head * (a.C / kKvTile) + tile];
+      copy((const char *)(a.k8 + (head * a.C + t0) * D), std::integral_constant<int, D>{}, kKvTile);
+    } else {
+      const __bf16 *base = of.slot < 0 ? a.k_draft + ((size_t)(-1 - of.slot) * a.Hkv + g) * a.T * D : a.k16 + ((size_t)of.slot * a.Hkv + g) * a.C * D;
+      copy((const char *)(base + (size_t)t0 * D), std::integral_constant<int, D * 2>{}, of.slot < 0 ? a.T - t0 : kKvTile);
+    }
+  };
+  request_keys(ent, tile);
+  typename Rows<D>::Cursor first, at;
   typename Rows<D>::Block blk;
   typename Rows<D>::Ready ready;
-  if (!rows.done(at)) {
-    rows.request(at, blk);
-    ready = rows.finish(blk, tile0, 1);
-  }
-  for (int tile = tile0; tile < tile_end; ++tile) {
-    const int t0 = tile * kKvTile;
-    bf16x8 k[2][KS];
-    const float scale = raw_scale;
+  // (a tile's sums are written under the next one's: before its own keys' wait they would be waited for)
+  float *left_at = nullptr, left_sum = 0.f;
+  auto put = [&]() __attribute__((always_inline)) { if (left_at) *left_at = left_sum; };
+  // Rows are waited for where they are asked for: where the branches meet, the wait would be for everything, the next tile's keys among it.
+  auto arrived = [](typename Rows<D>::Block &x) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) k[kb][ks] = FMT != 0 && is8 ? codes8(make_uint2(raw[kb][ks][0], raw[kb][ks][1]), scale) : __builtin_bit_cast(bf16x8, raw[kb][ks]);
-    if (tile + 1 < tile_end) request_keys(tile + 1);
-    const bool mine = t0 + lane < longest;
-    const size_t w_at = rows.weight_at(t0);
-    float before = 0.f;
-    if (mine && !rows.is_draft && a.w_in) before = a.w_in[w_at];
-    float acc[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
-    auto key = [&](int kb, int ks) __attribute__((always_inline)) { return k[kb][ks]; };
-    if (!rows.done(first)) {
-      bool again = tile > tile0 && (rows.is_draft || at.u != first.u || at.r0 != first.r0);
-      at = first;
-      while (true) {
-        if (again) {
-          rows.request(at, blk);
-          ready = rows.finish(blk, tile, 1);
-        }
-        rows.pay(key, blk, ready, t0, 0, acc);
-        typename Rows<D>::Cursor nx = at;
-        nx.r0 += 32;
-        rows.settle(nx);
-        if (rows.done(nx)) break;
-        at = nx;
-        again = true;
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(x.q[ks]));
+  };
+  bool same = false;   // the rows held are the entry's first block
+  while (true) {
+    // (the entry behind this one, looked up early)
+    const bool more = e + 1 < a.n_entries;
+    const Entry next = entry(more ? e + 1 : e);
+    const int next_end = more && next.piece0 < hi ? end_of(next) : 0;
+    const int longest = rows.longest;
+    const bool is8 = rows.is8(FMT);
+    if (!same) {
+      first = at = rows.begin(0);
+      if (!rows.done(at)) {
+        rows.request(at, rows.node_of(at), blk);
+        ready = rows.finish(blk, tile, 1);
+        arrived(blk);
       }
+    } else {
+      blk.left = longest;
     }
-    const float sum = rows.total(acc);
-    if (mine) {
-      if (rows.is_draft) a.w_draft[w_at] = sum;
-      else a.w_out[w_at] = before + sum;
+    bool fresh = true;   // blk is the first block, of this tile
+    for (; tile < tile_end; ++tile) {
+      const int t0 = tile * kKvTile;
+      const float scale = next_scale;
+      __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+      asm volatile("" ::: "memory");
+      bf16x8 k[2][KS];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int row = kb * 32 + rows.l32;
+          if (FMT != 0 && is8) {
+            typedef unsigned u32x2 __attribute__((ext_vector_type(2)));   // (not the struct uint2: its loads are taken to alias the direct loads into LDS)
+            const u32x2 w = *(const u32x2 *)(stage + row * D + ((ks ^ swz(D, row)) * 16) + rows.g2 * 8);
+            k[kb][ks] = codes8(make_uint2(w[0], w[1]), scale);
+          } else {
+            k[kb][ks] = *(const bf16x8 *)(stage + row * (D * 2) + (((2 * ks + rows.g2) ^ swz(D * 2, row)) * 16));
+          }
+        }
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): the stage is free
+      asm volatile("" ::: "memory");
+      put();
+      const bool mine = t0 + lane < longest;
+      float before = 0.f;   // (asked for ahead of the next keys: it is waited for first)
+      if (mine && rows.adds()) before = a.w_in[rows.weight_at(t0)];
+      if (tile + 1 < tile_end) request_keys(ent, tile + 1);
+      else if (next_end > 0) request_keys(next, 0);
+      float acc[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+      auto key = [&](int kb, int ks) __attribute__((always_inline)) { return k[kb][ks]; };
+      if (!rows.done(first)) {
+        if (!fresh && (rows.is_draft || at.u != first.u || at.r0 != first.r0)) {
+          rows.request(first, rows.node_of(first), blk);
+          ready = rows.finish(blk, tile, 1);
+          arrived(blk);
+        }
+        at = first;
+        typename Rows<D>::Cursor nx = rows.behind(at);
+        int node = 0;
+        if (!rows.done(nx)) node = rows.node_of(nx);
+        while (true) {   // the next block's rows are on the way during a block's products, and the nodes of the one behind it
+          typename Rows<D>::Block ahead;
+          const bool more_rows = !rows.done(nx);
+          typename Rows<D>::Cursor nx2 = nx;
+          int node2 = 0;
+          if (more_rows) {
+            rows.request(nx, node, ahead);
+            nx2 = rows.behind(nx);
+            if (!rows.done(nx2)) node2 = rows.node_of(nx2);
+          }
+          rows.pay(key, blk, ready, t0, 0, acc);
+          if (!more_rows) break;
+          arrived(ahead);
+          blk = ahead;
+          ready = rows.finish(blk, tile, 1);
+          at = nx;
+          nx = nx2;
+          node = node2;
+        }
+      }
+      fresh = false;
+      left_sum = before + rows.total(acc);
+      left_at = mine ? rows.sums_at(t0) : nullptr;
     }
+    if (next_end <= 0) break;
+    // one query's next slot: its rows are here already
+    same = ent.user >= 0 && next.user == ent.user && !rows.is_draft && next.slot >= 0 && at.r0 == first.r0;
+    ent = next;
+    ++e;
+    rows.set(ent);
+    tile = 0;
+    tile_end = next_end;
   }
+  put();
 }
 
 // Many rows: a workgroup of four wavefronts keeps the keys of up to two tiles in LDS as bf16 (16-byte pieces XOR-swizzled inside rows of 256 bytes by row & 15, of
@@ -309,7 +431,8 @@ __global__ __launch_bounds__(256, 4) void weights_rows_kernel(const Args a) {
   __shared__ __align__(16) unsigned long long row_sees[4][kRowsSpan * 32];
   __shared__ float sums[4][kRowsSpan][kKvTile];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = blockIdx.x % a.Hkv, piece = blockIdx.x / a.Hkv;
-  const Rows<D> rows(a, find_entry(a, piece, lane), g, lane, row_sees[wave]);
+  const int4 words = ((const int4 *)a.entries)[find_entry(a, piece, lane)];
+  const Rows<D> rows(a, Entry{words.x, words.y, words.z, words.w}, g, lane, row_sees[wave]);
   const int longest = rows.longest, span = rows.ent.keys & 31, tile0 = (piece - rows.ent.piece0) * span;
   const int n_tiles = min(tile0 + span, (longest + kKvTile - 1) / kKvTile) - tile0, first_key = tile0 * kKvTile, n_keys = min(longest - first_key, n_tiles * kKvTile);
   auto swz = [](int row) __attribute__((always_inline)) { return ROW == 256 ? (row & 15) : ((row >> 1) & 7); };
@@ -346,7 +469,7 @@ __global__ __launch_bounds__(256, 4) void weights_rows_kernel(const Args a) {
   for (int ks = 0; ks < KS; ++ks) k_rd[ks] = rows.l32 * ROW + (((2 * ks + rows.g2) ^ swz(rows.l32)) * 16);
   for (typename Rows<D>::Cursor at = rows.begin(32 * wave); !rows.done(at);) {
     typename Rows<D>::Block blk;
-    rows.request(at, blk);
+    rows.request(at, rows.node_of(at), blk);
     const typename Rows<D>::Ready ready = rows.finish(blk, tile0, n_tiles);
 #pragma unroll
     for (int t = 0; t < kRowsSpan; ++t)
@@ -363,10 +486,21 @@ __global__ __launch_bounds__(256, 4) void weights_rows_kernel(const Args a) {
   const int t0 = first_key + wave * kKvTile;
   if (wave < n_tiles && t0 + lane < longest) {
     const float sum = (sums[0][wave][lane] + sums[1][wave][lane]) + (sums[2][wave][lane] + sums[3][wave][lane]);
-    const size_t w_at = rows.weight_at(t0);
-    if (rows.is_draft) a.w_draft[w_at] = sum;
-    else a.w_out[w_at] = (a.w_in ? a.w_in[w_at] : 0.f) + sum;
+    *rows.sums_at(t0) = (rows.adds() ? a.w_in[rows.weight_at(t0)] : 0.f) + sum;
   }
+}
+
+// The sums of split slots, in the order of their parts.  One wavefront a (tile, kv head, slot).
+__global__ __launch_bounds__(64) void weights_join_kernel(const Args a, const Split *__restrict__ splits) {
+  const Split sp = splits[blockIdx.z];
+  const int g = blockIdx.y, tile = blockIdx.x, key = tile * kKvTile + threadIdx.x, tiles = (sp.longest + kKvTile - 1) / kKvTile;
+  if (key >= sp.longest) return;
+  const float *part = a.parts + ((size_t)sp.place + (size_t)g * tiles + tile) * kKvTile + threadIdx.x;
+  const size_t w_at = ((size_t)sp.slot * a.Hkv + g) * a.C + key;
+  float sum = a.w_in ? a.w_in[w_at] : 0.f;
+#pragma unroll 8
+  for (int p = 0; p < sp.parts; ++p) sum += part[(size_t)p * a.Hkv * tiles * kKvTile];
+  a.w_out[w_at] = sum;
 }
 
 }  // namespace
@@ -398,7 +532,7 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
   if ((uintptr_t)workspace_dev % pc::kAlign) return pc::fail(ctx, PC_EINVAL, "workspace must be 256-byte aligned");
 
   // The slots in the order of their first mention, each with its users in the order of the batch (a query that names a slot twice: two users)
-  struct Slot { int32_t slot, longest, n_users, blocks, only, only_used, at; };
+  struct Slot { int32_t slot, longest, n_users, blocks, only, only_used; };
   const int stride = pc::tbl_stride(max_chunks), G = c.n_q_heads / c.n_kv_heads;
   auto rows_of = [&](int b) { return G * (path_host ? n_path_host[b] : t_draft); };
   std::vector<Slot> slots;
@@ -420,7 +554,7 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
       if (used == 0) continue;
       if (of_slot[slot] < 0) {
         of_slot[slot] = (int)slots.size();
-        slots.push_back({slot, 0, 0, 0, 0, 0, 0});
+        slots.push_back({slot, 0, 0, 0, 0, 0});
       } else {
         several = true;
       }
@@ -429,67 +563,108 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
   }
   if (draft_weights_out_dev)
     for (int b = 0; b < batch; ++b) {
-      slots.push_back({-1 - b, 0, 0, 0, 0, 0, 0});
+      slots.push_back({-1 - b, 0, 0, 0, 0, 0});
       use(slots.back(), b, t_draft);
     }
   if (slots.empty()) return PC_OK;
-  // Many rows of a query to a key: weights_rows_kernel.  A piece has as many tiles as give every workgroup that the chip holds at once (8 of one wavefront a CU, 4 of four) one
-  // of them, fewer where a tile has more blocks of rows than the others; what has more of them comes first.
+  // Many rows of a query to a key: weights_rows_kernel, in pieces of two tiles, fewer where a tile has more blocks of rows than the others; what has more of them comes first.
+  // Else weights_stream_kernel, in shares of equal cost for all wavefronts that the chip holds at once (8 a CU).  A slot's users are split where a tile would have more blocks
+  // of rows than `most`: as many as the others, or four more than a wavefront's share has tiles (a block takes about the time of a tile, the launch that adds the sums up four).  us, 4 prompts of 256 rows (16 heads over 8) over 8 chunks of 384 tokens on average,
+  // one of them shared: whole 36.8, split 27.9 and 4.0 for the sums.
   int most_rows = 0, least_blocks = INT32_MAX;
   long all_tiles = 0;
   for (int b = 0; b < batch; ++b) most_rows = std::max(most_rows, rows_of(b));
   const bool by_rows = most_rows > 64;
+  const int waves = std::max(1, 8 * ctx->n_cu / c.n_kv_heads);   // (of a kv head)
+  auto tiles_of = [](const Slot &sl) { return (sl.longest + kKvTile - 1) / kKvTile; };
   for (const Slot &sl : slots) {
-    all_tiles += (sl.longest + kKvTile - 1) / kKvTile;
+    all_tiles += tiles_of(sl);
     if (sl.blocks) least_blocks = std::min(least_blocks, sl.blocks);
   }
-  const long held = (by_rows ? 4L : 8L) * ctx->n_cu, share = (all_tiles * c.n_kv_heads + held - 1) / held;
-  const int most = by_rows ? kRowsSpan : 16;
+  const int most = by_rows ? least_blocks : (int)std::min<long>(kMostCost, all_tiles / waves + 4);
   if (several) {
     std::stable_sort(slots.begin(), slots.end(), [](const Slot &x, const Slot &y) { return x.blocks > y.blocks; });
     for (size_t e = 0; e < slots.size(); ++e)
       if (slots[e].slot >= 0) of_slot[slots[e].slot] = (int)e;
   }
-  std::vector<int32_t> words;
-  words.reserve(slots.size() * 4 + (several ? (size_t)batch * max_chunks * 2 : 0) + (path_host ? (size_t)batch * (max_path + 1) : 0) + ((size_t)batch * t_draft + 1) / 2 + 2);
-  int pieces = 0, n_users = 0;
-  for (Slot &sl : slots) {
-    const int span = (int)std::max(1L, std::min((long)most, share * least_blocks / std::max(1, sl.blocks)));
-    int32_t user = sl.only;
-    if (sl.n_users != 1 || sl.only_used != sl.longest) {   // (none or several, or one that uses less than another, none of whose rows counts)
-      user = -1 - n_users;
-      sl.at = 1 + n_users;
-      n_users += sl.n_users + 1;
+  // the users of slots that have several, or one that uses less than another, none of whose rows counts
+  std::vector<std::vector<std::pair<int32_t, int32_t>>> lists;
+  std::vector<int32_t> list_of(slots.size(), -1);
+  for (size_t e = 0; e < slots.size(); ++e)
+    if (slots[e].n_users != 1 || slots[e].only_used != slots[e].longest) {
+      list_of[e] = (int)lists.size();
+      lists.emplace_back();
     }
-    const int32_t w[4] = {sl.slot, pieces, sl.longest * 32 + span, user};
-    words.insert(words.end(), w, w + 4);
-    pieces += ((sl.longest + kKvTile - 1) / kKvTile + span - 1) / span;
-  }
-  const size_t user_at = words.size();
-  words.resize(user_at + 2 * (size_t)n_users, 0);
-  if (n_users) {
-    for (const Slot &sl : slots)
-      if (sl.at) words[user_at + 2 * (size_t)(sl.at - 1)] = sl.n_users;
-    std::vector<int32_t> filled(slots.size(), 0);
+  if (!lists.empty())
     for (int b = 0; b < batch; ++b) {
       const int32_t *row = rows.data() + (size_t)b * stride;
       for (int ci = 0; ci < row[0]; ++ci) {
         const int slot = row[pc::kTblHeader + 2 * ci], used = row[pc::kTblHeader + 2 * ci + 1];
-        if (used == 0 || rows_of(b) == 0) continue;
-        const int e = of_slot[slot];
-        if (!slots[e].at) continue;
-        int32_t *w = words.data() + user_at + 2 * (size_t)(slots[e].at + filled[e]++);
-        w[0] = b;
-        w[1] = used;
+        if (used != 0 && rows_of(b) != 0 && list_of[of_slot[slot]] >= 0) lists[list_of[of_slot[slot]]].push_back({b, used});
       }
     }
+  const pc::DraftWs ws = pc::carve_draft_ws(c, ctx->n_cu, workspace_dev, batch, t_draft, max_chunks);
+  const size_t room = (size_t)((float *)ws.part_ml - ws.part_o) / kKvTile;   // tiles' sums that the workspace holds
+  std::vector<int32_t> words, splits;
+  std::vector<User> users;
+  words.reserve(slots.size() * 4 + (several ? (size_t)batch * max_chunks * 4 : 0) + (path_host ? (size_t)batch * (max_path + 1) : 0) + ((size_t)batch * t_draft + 1) / 2 + 2);
+  long pieces = 0;
+  size_t place = 0;
+  int most_split = 0;
+  for (size_t e = 0; e < slots.size(); ++e) {
+    const Slot &sl = slots[e];
+    const int tiles = tiles_of(sl);
+    auto add = [&](int blocks, int32_t user) {
+      const int each = by_rows ? std::max(1, std::min(kRowsSpan, kRowsSpan * least_blocks / std::max(1, blocks))) : std::min(kMostCost, (sl.slot < 0 ? kDraftCost : 1) * std::max(1, blocks));
+      const int32_t w[4] = {sl.slot, (int32_t)pieces, sl.longest * 32 + each, user};
+      words.insert(words.end(), w, w + 4);
+      pieces += by_rows ? (tiles + each - 1) / each : tiles * each;
+    };
+    if (list_of[e] < 0) {
+      add(sl.blocks, sl.only);
+      continue;
+    }
+    const auto &list = lists[list_of[e]];
+    // groups of users of at most `most` blocks (or of one user)
+    std::vector<size_t> ends;
+    std::vector<int> blocks;
+    for (size_t u = 0; u < list.size(); ++u) {
+      const int n = (rows_of(list[u].first) + 31) / 32;
+      if (u == 0 || blocks.back() + n > most) {
+        ends.push_back(u);
+        blocks.push_back(0);
+      }
+      ends.back() = u + 1;
+      blocks.back() += n;
+    }
+    const size_t parts = ends.size(), sums = (size_t)c.n_kv_heads * tiles;
+    const bool split = parts > 1 && place + parts * sums <= room;
+    if (!split) {
+      ends.assign(1, list.size());
+      blocks.assign(1, sl.blocks);
+    } else {
+      const int32_t w[4] = {sl.slot, sl.longest, (int32_t)parts, (int32_t)place};
+      splits.insert(splits.end(), w, w + 4);
+      most_split = std::max(most_split, tiles);
+    }
+    for (size_t k = 0, u = 0; k < ends.size(); ++k) {
+      add(blocks[k], -1 - (int32_t)users.size());
+      users.push_back({(int32_t)(ends[k] - u), split ? 1 + (int32_t)place : 0, 0, 0});
+      for (; u < ends[k]; ++u) users.push_back({list[u].first, list[u].second, rows_of(list[u].first) / G, 0});
+      if (split) place += sums;
+    }
   }
+  const int n_entries = (int)(words.size() / 4);
+  if (pieces * c.n_kv_heads >= (1L << 31)) return pc::fail(ctx, PC_ESHAPE, "too many keys for one call");
+  const size_t split_at = words.size();   // (16-byte aligned, as the entries)
+  words.insert(words.end(), splits.begin(), splits.end());
+  const size_t user_at = words.size();
+  if (!users.empty()) words.insert(words.end(), &users[0].query, &users[0].query + 4 * users.size());
   const size_t n_path_at = words.size(), path_at = n_path_at + batch;
   if (path_host) {
     words.insert(words.end(), n_path_host, n_path_host + batch);
     words.insert(words.end(), path_host, path_host + (size_t)batch * max_path);
   }
-  const pc::DraftWs ws = pc::carve_draft_ws(c, ctx->n_cu, workspace_dev, batch, t_draft, max_chunks);
   const int32_t *parents = draft_weights_out_dev ? parents_host : nullptr;   // (nothing else looks at the tree)
   hipStream_t s = (hipStream_t)stream;
   st = pc::upload_draft(ctx, words, batch, t_draft, parents, ws, s);
@@ -504,8 +679,8 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
   a.k_scale = ctx->k_scale + (size_t)layer * ctx->n_slots8 * c.n_kv_heads * (c.slot_capacity / kKvTile);
   a.n_slots16 = ctx->n_slots16;
   a.entries = (const Entry *)ws.words;
-  a.n_entries = (int)slots.size();
-  a.users = (const int2 *)(ws.words + user_at);
+  a.n_entries = n_entries;
+  a.users = (const User *)(ws.words + user_at);
   a.n_path = path_host ? ws.words + n_path_at : nullptr;
   a.path = ws.words + path_at;
   a.max_path = max_path;
@@ -518,9 +693,11 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
   a.w_in = weights_in_dev;
   a.w_out = weights_out_dev;
   a.w_draft = draft_weights_out_dev;
+  a.parts = ws.part_o;
   a.draft.sees = parents ? ws.sees : nullptr;
   const int formats = pc::table_formats(rows, stride, batch), fmt = !(formats & 1) ? 0 : (formats & 2) ? 2 : 1;
-  const dim3 grid((unsigned)(pieces * c.n_kv_heads));
+  a.share = (int)((pieces + waves - 1) / waves);
+  const dim3 grid((unsigned)((by_rows ? pieces : (pieces + a.share - 1) / a.share) * c.n_kv_heads));
 #define PC_WEIGHTS_F(DD, FF)                                                                                         \
   do {                                                                                                               \
     if (by_rows) hipLaunchKernelGGL((weights_rows_kernel<DD, FF>), grid, dim3(256), 0, s, a);                         \
@@ -530,6 +707,8 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
   if (c.head_dim == 128) PC_WEIGHTS(128); else PC_WEIGHTS(64);
 #undef PC_WEIGHTS_F
 #undef PC_WEIGHTS
+  if (!splits.empty())
+    hipLaunchKernelGGL(weights_join_kernel, dim3((unsigned)most_split, (unsigned)c.n_kv_heads, (unsigned)(splits.size() / 4)), dim3(64), 0, s, a, (const Split *)(ws.words + split_at));
   PC_HIP(ctx, hipGetLastError());
   return PC_OK;
 }

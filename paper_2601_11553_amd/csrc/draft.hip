@@ -283,8 +283,8 @@ DraftWs carve_draft_ws(const percache_config &c, int n_cu, void *base, int32_t b
   size_t off = 0;
   auto take = [&](size_t bytes) { char *r = p ? p + off : nullptr; off += align_up(bytes); return r; };
   const size_t B = batch, T = t_draft, ft = (T + kKvTile - 1) / kKvTile, rows = B * c.n_q_heads * T, nc = max_chunks;
-  // attention: chunk table, packed parents; projection: positions; weights: entries, users, paths (of at most t_draft nodes), packed parents
-  w.words = (int32_t *)take((B * (8 * (nc + 1) + 3 * T + 8) + 16) * sizeof(int32_t));
+  // attention: chunk table, packed parents; projection: positions; weights: entries, users, splits (14 words a chunk and query at most), paths (of at most t_draft nodes), packed parents
+  w.words = (int32_t *)take((B * (14 * (nc + 1) + 3 * T + 8) + 16) * sizeof(int32_t));
   w.sees = (uint2 *)take(t_draft <= kMaxNodes ? B * T * ft * sizeof(uint2) : 0);
   const size_t cap = max_splits_for(c, n_cu, batch, t_draft);
   w.part_o = (float *)take(rows * cap * c.head_dim * sizeof(float));
