@@ -287,7 +287,8 @@ __device__ __forceinline__ void mainloop_wide(char *lds, WRow w_row, const T *__
 // round trip of a stage (0.6 to 1.1 us against 0.3 to 0.4 us of MFMA work per k-step): 8 wavefronts and a ring of NSTG stages,
 // all of them requested ahead; the one barrier of a k-step sits between its halves, where the rest of its stage is in registers.  Wavefronts w and w + 4 own the same block of the tile and take one half of every stage's
 // k-elements each (kh = w >> 2), so a SIMD has two instruction streams at no more operand reads per MFMA; their sums meet
-// once, in LDS: on return acc[t] holds the whole sums of feature block kh (of fb_lo, fb_hi) in the layout of mainloop.
+// once, in LDS: on return of mainloop_deep sum[t] holds the whole sums of feature block kh (of fb_lo, fb_hi) in the layout of mainloop, of
+// mainloop_deep_tokens (two token blocks) those of both feature blocks of token block kh.
 template <int NTB, int NSTG>
 struct DeepShape {
   static constexpr int NWV = 8, BT = 64 * NTB;
@@ -299,8 +300,8 @@ struct DeepShape {
 };
 
 template <int NTB, int NSTG, class T, class WRow>
-__device__ __forceinline__ void mainloop_deep(char *lds, WRow w_row, const T *__restrict__ X, int ldx, int m0, int M, int K,
-                                              int fb_lo, int fb_hi, int wt, f32x16 (&sum)[NTB]) {
+__device__ __forceinline__ void deep_products(char *lds, WRow w_row, const T *__restrict__ X, int ldx, int m0, int M, int K,
+                                              int fb_lo, int fb_hi, int wt, f32x16 (&acc)[2][NTB]) {
   using S = DeepShape<NTB, NSTG>;
   using V8 = typename Vec8<T>::type;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), kh = wave >> 2;
@@ -320,7 +321,6 @@ __device__ __forceinline__ void mainloop_deep(char *lds, WRow w_row, const T *__
                                                                                   (wave + (k < S::W_INSTR ? k : k - S::W_INSTR) * S::NWV) * 1024),
                                        16, 0, 0);
   };
-  f32x16 acc[2][NTB];
 #pragma unroll
   for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -382,8 +382,16 @@ __device__ __forceinline__ void mainloop_deep(char *lds, WRow w_row, const T *__
     st = next;
   }
   wait_vmcnt<0>();  // (the surplus requests)
-  // each wavefront hands the block that it does not keep to its partner
   __syncthreads();
+}
+
+template <int NTB, int NSTG, class T, class WRow>
+__device__ __forceinline__ void mainloop_deep(char *lds, WRow w_row, const T *__restrict__ X, int ldx, int m0, int M, int K,
+                                              int fb_lo, int fb_hi, int wt, f32x16 (&sum)[NTB]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kh = wave >> 2;
+  f32x16 acc[2][NTB];
+  deep_products<NTB, NSTG>(lds, w_row, X, ldx, m0, M, K, fb_lo, fb_hi, wt, acc);
+  // each wavefront hands the block that it does not keep to its partner
   f32x4 *const give = (f32x4 *)(lds + wave * (NTB * 4096)), *const take = (f32x4 *)(lds + (wave ^ 4) * (NTB * 4096));
 #pragma unroll
   for (int t = 0; t < NTB; ++t) {
@@ -400,6 +408,31 @@ __device__ __forceinline__ void mainloop_deep(char *lds, WRow w_row, const T *__
       const f32x4 o = take[(t * 4 + q) * 64 + lane];
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[t][4 * q + e] += o[e];
+    }
+  }
+}
+template <int NSTG, class T, class WRow>
+__device__ __forceinline__ void mainloop_deep_tokens(char *lds, WRow w_row, const T *__restrict__ X, int ldx, int m0, int M, int K,
+                                                     int fb_lo, int fb_hi, int wt, f32x16 (&sum)[2][1]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kh = wave >> 2;
+  f32x16 acc[2][2];
+  deep_products<2, NSTG>(lds, w_row, X, ldx, m0, M, K, fb_lo, fb_hi, wt, acc);
+  f32x4 *const give = (f32x4 *)(lds + wave * 8192), *const take = (f32x4 *)(lds + (wave ^ 4) * 8192);
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    const f32x16 v = kh ? acc[a][0] : acc[a][1];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) give[(a * 4 + q) * 64 + lane] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+  }
+  __syncthreads();
+#pragma unroll
+  for (int a = 0; a < 2; ++a) {
+    sum[a][0] = kh ? acc[a][1] : acc[a][0];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 o = take[(a * 4 + q) * 64 + lane];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[a][0][4 * q + e] += o[e];
     }
   }
 }

@@ -20,8 +20,9 @@ using pc::gemm::pack4;
 // still two workgroups per CU).
 // EXTRA: the bias / head-norm variants (see QkvExtras) are compiled in.
 // WIDE: 8 wavefronts on two heads (256 features) x the same token tile, one workgroup per CU (D = 128, no EXTRA).
-template <int D, int NTB, bool EXTRA, bool WIDE = false>
-__global__ __launch_bounds__(WIDE ? 512 : 256, WIDE ? 1 : 2) void qkv_rope_kernel(const __bf16 *__restrict__ X, const __bf16 *__restrict__ W, int M,
+// DEEP: 8 wavefronts on the tile of two blocks, one workgroup per CU, on mainloop_deep_tokens (no EXTRA).
+template <int D, int NTB, bool EXTRA, bool WIDE = false, bool DEEP = false>
+__global__ __launch_bounds__(WIDE || DEEP ? 512 : 256, WIDE || DEEP ? 1 : 2) void qkv_rope_kernel(const __bf16 *__restrict__ X, const __bf16 *__restrict__ W, int M,
                                                           int H, int t_fresh, int Hq, int Hkv,
                                                           const int32_t *__restrict__ table, int tbl_stride, int node_stride,
                                                           const float2 *__restrict__ rope, __bf16 *__restrict__ Q,
@@ -31,11 +32,13 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, WIDE ? 1 : 2) void qkv_rope_kerne
   extern __shared__ __align__(16) char lds[];  // Shape<NTB>::LDS_BYTES
 
   static_assert(!WIDE || (D == 128 && !EXTRA), "the wide tile is built for head size 128 without the variants");
+  static_assert(!DEEP || (NTB == 2 && !EXTRA && !WIDE), "the deep tile is built for two blocks without the variants");
+  constexpr int NT = DEEP ? 1 : NTB;  // token blocks whose sums a wavefront ends up with
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int wf = wave & 1, wt = (wave >> 1) & 1, half = wave >> 2;  // (half: which of the tile's two heads; 0 unless WIDE)
+  const int wf = wave & 1, wt = (wave >> 1) & 1, kh = DEEP ? wave >> 2 : 0, half = WIDE ? wave >> 2 : 0;  // (half: which of the tile's two heads)
   const int l32 = lane & 31, g = lane >> 5;
   int bx = blockIdx.x, by = blockIdx.y;
-  if constexpr (WIDE) {
+  if constexpr (WIDE || DEEP) {
     // One tile per CU: give each XCD (workgroup ids go round-robin over the 8) a compact patch of the tile grid, so
     // that the weight and token rows its tiles share are fetched into its L2 once.  Ids of one XCD become consecutive
     // positions, and positions walk strips of `sw` feature tiles, token tile by token tile.
@@ -54,8 +57,10 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, WIDE ? 1 : 2) void qkv_rope_kerne
   const int fb_lo = (D == 128) ? 4 * half + wf : 2 * wf;
   const int fb_hi = (D == 128) ? 4 * half + wf + 2 : 2 * wf + 1;
 
-  f32x16 acc[2][NTB];
-  if constexpr (WIDE)
+  f32x16 acc[2][NT];
+  if constexpr (DEEP)
+    pc::gemm::mainloop_deep_tokens<4>(lds, [&](int row) __attribute__((always_inline)) { return W + (size_t)(f0 + row) * H; }, X, H, m0, M, H, fb_lo, fb_hi, wt, acc);
+  else if constexpr (WIDE)
     pc::gemm::mainloop_wide<NTB>(lds, [&](int row) __attribute__((always_inline)) { return W + (size_t)(f0 + row) * H; }, X, H, m0, M, H, fb_lo, fb_hi, wt, acc);
   else
     pc::gemm::mainloop<NTB>(lds, [&](int row) __attribute__((always_inline)) { return W + (size_t)(f0 + row) * H; }, X, H, m0, M, H, fb_lo, fb_hi, acc);
@@ -117,8 +122,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256, WIDE ? 1 : 2) void qkv_rope_kerne
     }
   }
 #pragma unroll
-  for (int t = 0; t < NTB; ++t) {
-    const int m_raw = m0 + (wt * NTB + t) * 32 + l32;
+  for (int t = 0; t < NT; ++t) {
+    const int m_raw = m0 + (wt * NTB + kh + t) * 32 + l32;
     const bool m_ok = m_raw < M;
     const int m = m_ok ? m_raw : M - 1;
     const int b = m / t_fresh, i = m - b * t_fresh;
@@ -531,6 +536,26 @@ pc_status launch_qkv_rope(percache_ctx *ctx, const __bf16 *x, const __bf16 *w, i
     return PC_OK;
   }
   dim3 grid(F / BF, (M + 64 * ntb - 1) / (64 * ntb));
+  // Drafted nodes: tiles of 128 tokens whose stages are all requested ahead, where they go to the CUs in one round -- there the two-stage loop waits out a
+  // stage's round trip every k-step.  (The calls that were here before keep the order of their sums.)  us a call, this | the tiles above: 48 heads, K = 2048, 504 rows
+  // 25.2 | 31.6, 400 rows 25.0 | 30.1, 630 rows 26.8 | 32.4; 32 heads, K = 1024, 800 rows 18.2 | 19.2
+  const long deep_tiles = (long)(F / BF) * ((M + 127) / 128);
+  if (node_stride && M > 64 && deep_tiles <= ctx->n_cu) {
+    grid = dim3(F / BF, (M + 127) / 128);
+#define PC_DEEP(DD)                                                                                                                                   \
+  do {                                                                                                                                                \
+    constexpr int lds_bytes = pc::gemm::DeepShape<2, 4>::LDS_BYTES;                                                                                    \
+    PC_HIP(ctx, hipFuncSetAttribute((const void *)qkv_rope_kernel<DD, 2, false, false, true>, hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes)); \
+    prof_begin(ctx, PC_KERNEL_QKV_ROPE, stream);                                                                                                      \
+    hipLaunchKernelGGL((qkv_rope_kernel<DD, 2, false, false, true>), grid, dim3(512), lds_bytes, stream, x, w, M, c.hidden, t_fresh, c.n_q_heads,       \
+                       c.n_kv_heads, table_dev, tbl_stride, node_stride, rope, q, k, v, extras, vb_large);                                             \
+  } while (0)
+    if (c.head_dim == 128) PC_DEEP(128); else PC_DEEP(64);
+#undef PC_DEEP
+    prof_end(ctx, PC_KERNEL_QKV_ROPE, stream);
+    PC_HIP(ctx, hipGetLastError());
+    return PC_OK;
+  }
 #define PC_LAUNCH_E(DD, NN, EE)                                                                                        \
   do {                                                                                                                \
     constexpr int lds_bytes = pc::gemm::Shape<NN>::LDS_BYTES;                                                         \
