@@ -5,7 +5,7 @@
 // time.  So a slot shared by several queries (a system prompt's chunk) is read once, its sums have one owner and one order -- no atomics -- and are added to the
 // running sums in place; only where that would keep one wavefront at work when the others are done are a slot's users split among several, whose sums a second
 // launch adds up (weights_join_kernel).  The rows are on the M side of the product: a lane then has 16 rows of one
-// key, whose exponentials it adds up by itself.  The log-sum-exp, which belongs to rows, comes in as one more step of the contraction: -lse sqrt(D) as
+// key, whose exponentials it adds up by itself.  The log-sum-exp, which belongs to rows, comes in as the last step of the contraction: -lse sqrt(D) as
 // the sum of three bf16 numbers (24 bits) against ones.
 //
 // With few rows (a decoding step) the key stream bounds it: weights_stream_kernel.  With many the exponentials do (24 clocks of the vector port
@@ -191,11 +191,12 @@ struct Rows {
 #pragma unroll
       for (int x = 0; x < 16; ++x) s[kb][x] = 0.f;
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.ext, ones, s[kb], 0, 0, 0);
-#pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(blk.q[ks], key(kb, ks), s[kb], 0, 0, 0);
+    // (the log-sum-exp last: ahead of the others, every step would be rounded at its size)
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(r.ext, ones, s[kb], 0, 0, 0);
     auto p = [&](int kb, int x) __attribute__((always_inline)) { return fast_exp2(s[kb][x] * a.scale_log2e); };
     // (register x of lane half g2 is row 8 (x / 4) + 4 g2 + x % 4.)  What does not count is selected away, not multiplied by 0: it need not be finite
     auto kept = [](float v, int bits, int at) __attribute__((always_inline)) {
