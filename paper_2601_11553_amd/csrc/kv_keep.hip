@@ -23,12 +23,13 @@ __device__ __forceinline__ unsigned key_of(float w) {
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelLds = 8192;
 // One workgroup a (kv head, slot).  idx [n][Hkv][idx_stride]: the kept tokens in order, -1 behind them; weights are moved along.
-// Four passes over a few thousand keys and one over the tokens, each a few LDS accesses and barriers: a chain of latencies, so the keys are read from memory
-// once, into LDS (slots of up to kSelLds tokens; longer ones are read again from the L2).  2048 tokens, 128 workgroups: 14.9 us read in every pass, 9.2 from LDS.
+// Up to four passes over a few thousand keys (the last ones mostly spared: few tokens share three digits) and one over the tokens, each a few LDS accesses and barriers: a chain of latencies, so the keys are read from memory
+// once, into LDS (slots of up to kSelLds tokens; longer ones are read again from the L2).  2048 tokens, 128 workgroups: 14.9 us read in every pass, 9.5 from LDS, 8.6 with
+// the passes spared and the sums of digits taken inside the vector pipe.
 __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights, const Moves mv, int Hkv, int C, int n_first, int n_last, int32_t *idx, int idx_stride) {
   __shared__ unsigned keys[kSelLds];
   __shared__ unsigned hist[256];
-  __shared__ unsigned found[2];                         // the digit, and how many tokens have a larger one
+  __shared__ unsigned found[3];                         // the digit, how many tokens have a larger one, and how many this one
   __shared__ int wave_n[kSelWaves][2];
   const int g = blockIdx.x, z = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int have = mv.have[z], keep = mv.keep[z];
@@ -38,6 +39,7 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
   const int lo = n_first, hi = have - n_last;           // the tokens that compete (keep < have: n_first + n_last <= keep < have)
   int need = keep >= have ? 0 : keep - n_first - n_last;
   unsigned top = 0, mask = 0;                           // the digits found so far
+  bool whole = false;                                   // every token with these digits is kept: the others need not be found
   const bool in_lds = have <= kSelLds;
   auto key_at = [&](int t) __attribute__((always_inline)) { return in_lds ? keys[t] : key_of(w_src[t]); };
   if (need > 0 && in_lds)
@@ -56,12 +58,16 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
         unsigned n[4], sum = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum += n[j] = hist[255 - 4 * lane - j];
+        // sums over the lanes up to this one: inside rows of 16, then over the rows before
         unsigned upto = sum;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const unsigned x = __shfl_up(upto, o, 64);
-          if (lane >= o) upto += x;
-        }
+#define PC_ADD(ctrl, rows) upto += (unsigned)__builtin_amdgcn_update_dpp(0, (int)upto, ctrl, rows, 0xf, false)
+        PC_ADD(0x111, 0xf);
+        PC_ADD(0x112, 0xf);
+        PC_ADD(0x114, 0xf);
+        PC_ADD(0x118, 0xf);
+        PC_ADD(0x142, 0xa);
+        PC_ADD(0x143, 0xc);
+#undef PC_ADD
         unsigned before = upto - sum;
         if (before < (unsigned)need && upto >= (unsigned)need)
 #pragma unroll
@@ -69,6 +75,7 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
             if (before < (unsigned)need && before + n[j] >= (unsigned)need) {
               found[0] = 255 - 4 * lane - j;
               found[1] = before;
+              found[2] = n[j];
             }
             before += n[j];
           }
@@ -77,9 +84,11 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
       top |= found[0] << shift;
       mask |= 255u << shift;
       need -= found[1];   // (hist and found are written again behind the next barriers only)
+      whole = (unsigned)need == found[2];
+      if (whole) break;
     }
   }
-  // `need` tokens with the key `top` are kept, the first ones, and all with a larger key (keep >= have: every token)
+  // `need` tokens with the key `top` are kept, the first ones (whole: every token that starts with its digits), and all with a larger key (keep >= have: every token)
   int at = 0, ties = 0;
   for (int t0 = 0; t0 < have; t0 += kSelThreads) {
     const int t = t0 + tid;
@@ -89,8 +98,8 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
       w = w_src[t];
       const bool fixed = keep >= have || t < lo || t >= hi;
       const unsigned k = key_of(w);
-      in = fixed || (mask && k > top);
-      tie = !fixed && mask && k == top;
+      in = fixed || (mask && (whole ? k >= top : k > top));
+      tie = !fixed && mask && !whole && k == top;
     }
     const unsigned long long tie_b = __ballot(tie), below = (1ull << lane) - 1;
     if (lane == 0) wave_n[wave][0] = __popcll(tie_b);
