@@ -285,10 +285,10 @@ __global__ __launch_bounds__(2 * D) void kv_path_kernel(Store16 s16, Store8 s8, 
   const int z = blockIdx.z, g = blockIdx.y, Hkv = gridDim.y, tid = threadIdx.x;
   const int32_t *rec = lists.v + z * record;   // slot, start, number of nodes, the nodes
   const int slot = rec[0], start = rec[1], n = rec[2], end = start + n;
-  for (int j = tid; j < n; j += 2 * D) path[j] = rec[3 + j];
-  __syncthreads();
   const int blk = start / kKvTile + blockIdx.x, t0 = blk * kKvTile;
   if (slot < 0 || t0 >= end) return;
+  for (int j = tid; j < n; j += 2 * D) path[j] = rec[3 + j];
+  __syncthreads();
   const size_t row0 = ((size_t)z * Hkv + g) * T;
   if (w.out && tid < kKvTile && t0 + tid >= start && t0 + tid < end)
     w.out[((size_t)slot * Hkv + g) * C + t0 + tid] = w.draft[row0 + path[t0 + tid - start]];
@@ -577,12 +577,13 @@ pc_status percache_kv_append_path(percache_ctx *ctx, int32_t layer, const void *
     pc::ListWords lists;
     int blocks = 0;
     for (int z = 0; z < cnt; ++z) {
-      const int b = b0 + z, n = n_path_host[b], end = start[b] + n;
+      // (a skipped query has no nodes here: its path may be longer than a record)
+      const int b = b0 + z, n = append_slots_host[b] < 0 ? 0 : n_path_host[b], end = start[b] + n;
       int32_t *rec = lists.v + z * record;
       rec[0] = append_slots_host[b];
       rec[1] = start[b];
       rec[2] = n;
-      for (int j = 0; j < n && j < longest; ++j) rec[3 + j] = path_host[(size_t)b * max_path + j];
+      for (int j = 0; j < n; ++j) rec[3 + j] = path_host[(size_t)b * max_path + j];
       const int touched = rec[0] < 0 ? 0 : (end + kKvTile - 1) / kKvTile - start[b] / kKvTile;
       if (touched > blocks) blocks = touched;
     }
