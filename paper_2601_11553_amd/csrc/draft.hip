@@ -209,11 +209,17 @@ __global__ __launch_bounds__(256) void draft_merge_kernel(const float *__restric
           // (a partition without a visible key has sum 0, and zeros)
           const float w = parts[h].e[j].y == 0.f ? 0.f : parts[h].e[j].y * __builtin_amdgcn_exp2f(parts[h].e[j].x - st[h].m);
           st[h].l += w;
+          // (left out where there is no partition: what was read in its place need not be finite)
+          if (parts[h].e[j].y != 0.f)
 #pragma unroll
-          for (int x = 0; x < 8; ++x) st[h].acc[x] += w * parts[h].o[j][x >> 2][x & 3];
+            for (int x = 0; x < 8; ++x) st[h].acc[x] += w * parts[h].o[j][x >> 2][x & 3];
         }
       }
   while (batch.any) {
+    // (places that no node fills hold the first one's V, which need not be finite)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (!batch.has[j]) batch.v[j] = pc::bf16x8{};
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

@@ -3,8 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import draft_ref as ref
+
 from gpu_util import DEV, bf16, host
-from test_gpu_draft import make, stored
+from test_gpu_draft import cached, make, random_tree, stored
 
 pytestmark = pytest.mark.gpu
 
@@ -48,4 +50,38 @@ def test_a_skipped_query_behind_a_full_list():
         got = pc.percache_kv_get(0, s)
         assert torch.equal(got[0][:, 0], k[s, :, path[s, 0]]) and torch.equal(got[1][:, 0], v[s, :, path[s, 0]])
     assert all(pc.percache_kv_len(0, s) == 1 for s in range(207))
+    pc.close()
+
+
+# rows of a kv head up to 32 (one kernel with the nodes), above, and so many that heads are merged together
+@pytest.mark.parametrize("Hq,Hkv,D,T,B", [(4, 2, 128, 7, 1), (4, 2, 64, 16, 2), (6, 2, 128, 20, 2), (8, 2, 64, 30, 1), (2, 1, 128, 200, 1), (16, 4, 64, 70, 8)])
+@pytest.mark.parametrize("formats,n_splits", [("bf16", 0), ("bf16", 1), ("bf16", 2), ("bf16", 5), ("8bit", 0), ("mixed", 3)])
+def test_infinite_values_that_a_row_sees(Hq, Hkv, D, T, B, formats, n_splits):
+    """V of a cached key (bf16 slots) and of nodes infinite in some dimensions: infinite there, NaN where both signs meet, and the usual numbers elsewhere."""
+    pc, g, _ = make(33, Hq, Hkv, D, 128, formats, [128] * (2 * B))
+    for b in range(B):
+        if formats != "8bit":   # (slot b of each pair is a bf16 one in a mixed store too)
+            k, v = pc.percache_kv_get(0, b)
+            v[:, 40, [3, 9]] = float("inf")
+            pc.percache_kv_put(0, b, k, v)
+    kv = stored(pc)
+    q, k, v = bf16(g.standard_normal((B, Hq, T, D))), bf16(g.standard_normal((B, Hkv, T, D))), bf16(g.standard_normal((B, Hkv, T, D)))
+    v[:, :, 0, 5] = float("inf")
+    v[:, :, T // 2, 7] = -float("inf")
+    v[:, :, 1, 9] = -float("inf")
+    parents = [random_tree(g, T, T - 1) for _ in range(B)]
+    ids, used = np.array([[b, B + b] for b in range(B)]), np.array([[128, 65 + b] for b in range(B)])
+    out, lse = pc.percache_attention_draft(0, q, k, v, slot_ids=ids, used_len=used, parents=parents, n_splits=n_splits, lse_out=True)
+    torch.cuda.synchronize()
+    assert torch.isfinite(lse[:, :, :T - 1]).all()
+    got = host(out).astype(np.float64).reshape(B, T, Hq, D)
+    for b in range(B):
+        kc, vc = cached(kv, ids[b], used[b])
+        with np.errstate(invalid="ignore"):
+            want, _, size, _, _ = ref.attend(host(q[b]).astype(np.float64), kc, vc, host(k[b]).astype(np.float64), host(v[b]).astype(np.float64),
+                                             ref.ancestors(parents[b]))
+        fine = np.isfinite(want)
+        assert not fine.all()
+        assert np.array_equal(np.isnan(got[b]), np.isnan(want)) and np.array_equal(got[b][np.isinf(want)], want[np.isinf(want)])
+        assert (np.abs(got[b][fine] - want[fine]) <= (2.0 ** -7 + 2.0 ** -13) * size[fine]).all()
     pc.close()
