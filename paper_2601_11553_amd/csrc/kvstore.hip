@@ -277,23 +277,24 @@ struct PathWeights {
   const float *draft;   // [B][Hkv][T]
   float *out;           // [slots][Hkv][C], null: no weights
 };
+constexpr int kPathHeader = 4;   // words of a record before its nodes: slot, start, number of nodes, query
 template <int D>
 __global__ __launch_bounds__(2 * D) void kv_path_kernel(Store16 s16, Store8 s8, int n_slots16, const __bf16 *__restrict__ dense_k, const __bf16 *__restrict__ dense_v,
                                                         PathWeights w, int C, int T, const pc::ListWords lists, int record) {
   // The nodes go through LDS: indexed by a lane, the launch's arguments are host memory, a microsecond and more a look (10.1 us a call so, one query; now 4.8).
   __shared__ int32_t path[pc::kListWords];
-  const int z = blockIdx.z, g = blockIdx.y, Hkv = gridDim.y, tid = threadIdx.x;
-  const int32_t *rec = lists.v + z * record;   // slot, start, number of nodes, the nodes
-  const int slot = rec[0], start = rec[1], n = rec[2], end = start + n;
+  const int g = blockIdx.y, Hkv = gridDim.y, tid = threadIdx.x;
+  const int32_t *rec = lists.v + blockIdx.z * record;
+  const int slot = rec[0], start = rec[1], n = rec[2], b = rec[3], end = start + n;
   const int blk = start / kKvTile + blockIdx.x, t0 = blk * kKvTile;
-  if (slot < 0 || t0 >= end) return;
-  for (int j = tid; j < n; j += 2 * D) path[j] = rec[3 + j];
+  if (t0 >= end) return;
+  for (int j = tid; j < n; j += 2 * D) path[j] = rec[kPathHeader + j];
   __syncthreads();
-  const size_t row0 = ((size_t)z * Hkv + g) * T;
+  const size_t row0 = ((size_t)b * Hkv + g) * T;
   if (w.out && tid < kKvTile && t0 + tid >= start && t0 + tid < end)
     w.out[((size_t)slot * Hkv + g) * C + t0 + tid] = w.draft[row0 + path[t0 + tid - start]];
   if (slot >= n_slots16) {
-    const Entry e = {slot - n_slots16, z * Hkv * T, n, start};
+    const Entry e = {slot - n_slots16, b * Hkv * T, n, start};
     quant_block<D>(s8, dense_k, dense_v, C, e, e.slot, g, T, [&](int i) { return n ? path[max(i, 0)] : 0; });
     return;
   }
@@ -557,7 +558,6 @@ pc_status percache_kv_append_path(percache_ctx *ctx, int32_t layer, const void *
   if ((long)batch * c.n_kv_heads * t_draft >= (1L << 31)) return pc::fail(ctx, PC_ESHAPE, "more than 2^31 rows");
   std::vector<char> named(c.n_slots, 0);
   std::vector<int32_t> start(batch, 0);
-  int longest = 0;
   for (int b = 0; b < batch; ++b) {
     const int slot = append_slots_host[b];
     if (slot < 0) continue;
@@ -568,29 +568,41 @@ pc_status percache_kv_append_path(percache_ctx *ctx, int32_t layer, const void *
     if (start[b] < 0 || start[b] > have) return pc::fail(ctx, PC_ELEN, "query %d: start %d outside [0,%d]", b, start[b], have);
     if ((long)start[b] + n_path_host[b] > c.slot_capacity)
       return pc::fail(ctx, PC_ELEN, "slot %d: %d tokens behind %d do not fit the capacity %d", slot, n_path_host[b], start[b], c.slot_capacity);
-    if (n_path_host[b] > longest) longest = n_path_host[b];
   }
-  const int record = longest + 3;
-  if (record > pc::kListWords) return pc::fail(ctx, PC_ESHAPE, "a path of %d nodes, at most %d are supported", longest, pc::kListWords - 3);
-  for (int b0 = 0, cnt; b0 < batch; b0 += cnt) {
-    cnt = pc::kListWords / record < batch - b0 ? pc::kListWords / record : batch - b0;
+  // A record for every query that has a slot; a path that a launch's list does not hold is cut behind whole blocks of its slot, and goes piece by piece.
+  struct Piece { int b, first, n; };   // nodes first .. first + n - 1 of query b's path
+  const int most = pc::kListWords - kPathHeader;
+  std::vector<Piece> pieces;
+  int longest = 0;
+  for (int b = 0; b < batch; ++b) {
+    if (append_slots_host[b] < 0) continue;
+    int first = 0;
+    do {
+      const int left = n_path_host[b] - first, at = start[b] + first, n = left <= most ? left : (at + most) / kKvTile * kKvTile - at;
+      pieces.push_back({b, first, n});
+      if (n > longest) longest = n;
+      first += n;
+    } while (first < n_path_host[b]);
+  }
+  const int record = longest + kPathHeader, n_pieces = (int)pieces.size();
+  for (int p0 = 0, cnt; p0 < n_pieces; p0 += cnt) {
+    cnt = pc::kListWords / record < n_pieces - p0 ? pc::kListWords / record : n_pieces - p0;
     pc::ListWords lists;
     int blocks = 0;
     for (int z = 0; z < cnt; ++z) {
-      // (a skipped query has no nodes here: its path may be longer than a record)
-      const int b = b0 + z, n = append_slots_host[b] < 0 ? 0 : n_path_host[b], end = start[b] + n;
+      const Piece &p = pieces[p0 + z];
       int32_t *rec = lists.v + z * record;
-      rec[0] = append_slots_host[b];
-      rec[1] = start[b];
-      rec[2] = n;
-      for (int j = 0; j < n; ++j) rec[3 + j] = path_host[(size_t)b * max_path + j];
-      const int touched = rec[0] < 0 ? 0 : (end + kKvTile - 1) / kKvTile - start[b] / kKvTile;
+      rec[0] = append_slots_host[p.b];
+      rec[1] = start[p.b] + p.first;
+      rec[2] = p.n;
+      rec[3] = p.b;
+      for (int j = 0; j < p.n; ++j) rec[kPathHeader + j] = path_host[(size_t)p.b * max_path + p.first + j];
+      const int touched = (rec[1] + p.n + kKvTile - 1) / kKvTile - rec[1] / kKvTile;
       if (touched > blocks) blocks = touched;
     }
     if (blocks == 0) continue;
-    const size_t at = (size_t)b0 * c.n_kv_heads * t_draft;
-    const __bf16 *k = (const __bf16 *)k_dev + at * c.head_dim, *v = (const __bf16 *)v_dev + at * c.head_dim;
-    const PathWeights w = {draft_weights_dev ? draft_weights_dev + at : nullptr, weights_dev};
+    const __bf16 *k = (const __bf16 *)k_dev, *v = (const __bf16 *)v_dev;
+    const PathWeights w = {draft_weights_dev, weights_dev};
     const dim3 grid(blocks, c.n_kv_heads, cnt);
     if (c.head_dim == 128)
       hipLaunchKernelGGL(kv_path_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, store16(ctx, layer), store8(ctx, layer), ctx->n_slots16, k, v, w, c.slot_capacity, t_draft, lists, record);

@@ -112,14 +112,16 @@ struct Context {
   }
 };
 
-// what kv_path_kernel reads of its lists: a record's three words, then as many nodes as the third says
+// what kv_path_kernel reads of its lists: a record's four words (slot, token, nodes, query), then as many nodes as the third says
+constexpr int kHeader = 4;
 void check_records(const char *what) {
   for (const PathLaunch &p : paths) {
-    expect(p.record >= 3 && (long)p.record * p.queries <= pc::kListWords, what);
+    expect(p.record >= kHeader && (long)p.record * p.queries <= pc::kListWords, what);
     for (int z = 0; z < p.queries && (z + 1) * p.record <= pc::kListWords; ++z) {
       const int32_t *rec = p.lists.v + z * p.record;
-      expect(rec[2] >= 0 && 3 + rec[2] <= p.record, what);
-      for (int j = 0; j < rec[2] && 3 + j < p.record; ++j) expect(rec[3 + j] >= 0 && rec[3 + j] < p.T, what);
+      expect(rec[0] >= 0 && rec[2] >= 0 && kHeader + rec[2] <= p.record, what);
+      expect((rec[1] + rec[2] + 63) / 64 - rec[1] / 64 <= p.blocks, what);
+      for (int j = 0; j < rec[2] && kHeader + j < p.record; ++j) expect(rec[kHeader + j] >= 0 && rec[kHeader + j] < p.T, what);
     }
   }
 }
@@ -160,10 +162,41 @@ void skipped_queries() {
     expect(append(x, 900, {std::vector<int32_t>(900, 1), {}}, {-1, -1}) == PC_OK && paths.empty(), "nothing to launch");
   }
 }
+
+// paths that a launch's list does not hold go in pieces that end with a block of their slot
+void long_paths() {
+  const char *what = "a long path's pieces";
+  for (int have : {0, 1, 37, 63, 64, 700})
+    for (int n : {827, 828, 829, 830, 892, 1656, 3000}) {
+      Context x(3, 4096);
+      if (have) x.put(0, have);
+      x.put(2, 9);
+      std::vector<std::vector<int32_t>> nodes(4);
+      for (int j = 0; j < n; ++j) nodes[0].push_back((j * 7 + 3) % 5000);
+      nodes[1] = {1, 2, 3};
+      nodes[2].assign(4000, 8);
+      nodes[3] = {4999};
+      expect(append(x, 5000, nodes, {0, 1, -1, 2}) == PC_OK, "call");
+      expect(percache_kv_len(x.ctx, 0, 0) == have + n && percache_kv_len(x.ctx, 0, 1) == 3 && percache_kv_len(x.ctx, 0, 2) == 10, "lengths");
+      check_records(what);
+      int at[3] = {have, 0, 9};
+      for (const PathLaunch &p : paths)
+        for (int z = 0; z < p.queries; ++z) {
+          const int32_t *rec = p.lists.v + z * p.record;
+          const int b = rec[3], slot = rec[0], base = slot == 0 ? have : slot == 1 ? 0 : 9;
+          expect(slot == (b == 3 ? 2 : b) && rec[1] == at[slot], what);
+          for (int j = 0; j < rec[2]; ++j) expect(rec[kHeader + j] == nodes[b][rec[1] - base + j], what);
+          at[slot] += rec[2];
+          expect(at[slot] == base + (int)nodes[b].size() || at[slot] % 64 == 0, what);
+        }
+      expect(at[0] == have + n && at[1] == 3 && at[2] == 10, what);
+    }
+}
 }  // namespace
 
 int main() {
   skipped_queries();
+  long_paths();
   std::printf(bad ? "launch driver: %d FAILED checks\n" : "launch driver: ok\n", bad);
   return bad ? 1 : 0;
 }

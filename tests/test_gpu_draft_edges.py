@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from oracle import draft_ref as ref
+from oracle import kv_fp8
 
 from gpu_util import DEV, bf16, host
 from test_gpu_draft import cached, make, random_tree, stored
@@ -84,4 +85,35 @@ def test_infinite_values_that_a_row_sees(Hq, Hkv, D, T, B, formats, n_splits):
         assert not fine.all()
         assert np.array_equal(np.isnan(got[b]), np.isnan(want)) and np.array_equal(got[b][np.isinf(want)], want[np.isinf(want)])
         assert (np.abs(got[b][fine] - want[fine]) <= (2.0 ** -7 + 2.0 ** -13) * size[fine]).all()
+    pc.close()
+
+
+@pytest.mark.parametrize("formats", ["bf16", "8bit", "mixed"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_paths_longer_than_a_launch_takes(D, formats):
+    """Paths of a thousand nodes and more, which go in pieces, among short ones, with the nodes' weights; starts inside and at the ends of blocks."""
+    cuts = [(0, 1500), (37, 829), (640, 1408), (5, 3), (100, 1000), (2048, 0)]
+    B, T, Hkv, C = len(cuts), 1600, 2, 2048
+    pc, g, kv = make(34, 2, Hkv, D, C, formats, [max(a, 1) + 3 if a < C else C for a, _ in cuts])
+    k, v = bf16(g.standard_normal((B, Hkv, T, D))), bf16(3 * g.standard_normal((B, Hkv, T, D)))
+    path = np.array([g.integers(0, T, T) for _ in range(B)])
+    w, dw = torch.rand((B, Hkv, C), device=DEV), torch.rand((B, Hkv, T), device=DEV)
+    want_w = w.clone()
+    order = [4, 0, 5, 2, 1, 3]   # slot of each query
+    pc.percache_kv_append_path(0, k, v, order, path, n_path=[cuts[s][1] for s in order], start=[cuts[s][0] for s in order], weights=w, draft_weights=dw)
+    torch.cuda.synchronize()
+    n8 = {"bf16": 0, "8bit": B, "mixed": B // 2}[formats]
+    for b, s in enumerate(order):
+        a, n = cuts[s]
+        assert pc.percache_kv_len(0, s) == a + n
+        at = torch.as_tensor(path[b, :n].astype(np.int64), device=DEV)
+        want_w[s, :, a:a + n] = dw[b][:, at]
+        got = pc.percache_kv_get(0, s)
+        for x, new, got_x in ((0, k, got[0]), (1, v, got[1])):
+            full = np.concatenate([kv[s][x][:, :a], host(new[b][:, at]).astype(np.float64)], 1)
+            lo = a // 64 * 64
+            if s >= B - n8 and full.shape[1] > lo:
+                full[:, lo:] = kv_fp8.round_trip(full[:, lo:])
+            assert np.array_equal(host(got_x), full.astype(np.float32)), (s, x)
+    assert torch.equal(w, want_w)
     pc.close()
