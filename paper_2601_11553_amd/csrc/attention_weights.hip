@@ -582,6 +582,7 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
     all_tiles += tiles_of(sl);
     if (sl.blocks) least_blocks = std::min(least_blocks, sl.blocks);
   }
+  if (least_blocks == INT32_MAX) least_blocks = 1;   // (no row counts for any slot)
   const int most = by_rows ? least_blocks : (int)std::min<long>(kMostCost, all_tiles / waves + 4);
   if (several) {
     std::stable_sort(slots.begin(), slots.end(), [](const Slot &x, const Slot &y) { return x.blocks > y.blocks; });

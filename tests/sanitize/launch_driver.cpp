@@ -192,11 +192,29 @@ void long_paths() {
       expect(at[0] == have + n && at[1] == 3 && at[2] == 10, what);
     }
 }
+
+// weights for slots none of whose rows counts (the query with a long path has no chunks): their number of row blocks is no limit for anybody
+void weights_without_counting_rows() {
+  Context x(1, 64);
+  x.put(0, 60);
+  const int T = 200;
+  std::vector<int32_t> ids = {0, 0}, used = {60, 0}, n_chunks = {1, 0}, path(2 * T), n_path = {0, T};
+  for (int j = 0; j < T; ++j) path[j] = path[T + j] = j;
+  const size_t bytes = percache_draft_workspace_bytes(x.ctx, 2, T, 1);
+  void *ws = aligned(bytes);
+  std::vector<float> w(64);
+  const int before = other_launches;
+  expect(percache_attention_weights(x.ctx, 0, x.arena, nullptr, w.data(), 2, T, ids.data(), used.data(), n_chunks.data(), 1, nullptr, path.data(), n_path.data(), T,
+                                    nullptr, w.data(), nullptr, ws, bytes, nullptr) == PC_OK, "weights");
+  expect(other_launches > before, "weights: launches");
+  std::free(ws);
+}
 }  // namespace
 
 int main() {
   skipped_queries();
   long_paths();
+  weights_without_counting_rows();
   std::printf(bad ? "launch driver: %d FAILED checks\n" : "launch driver: ok\n", bad);
   return bad ? 1 : 0;
 }

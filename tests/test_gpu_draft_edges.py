@@ -117,3 +117,16 @@ def test_paths_longer_than_a_launch_takes(D, formats):
             assert np.array_equal(host(got_x), full.astype(np.float32)), (s, x)
     assert torch.equal(w, want_w)
     pc.close()
+
+
+def test_weights_of_slots_none_of_whose_rows_counts():
+    """A query with chunks and an empty path beside one with a long path and no chunk, without draft keys: the sums stay as they are."""
+    pc, g, kv = make(35, 2, 1, 64, 192, "mixed", [190, 0])
+    T = 200
+    q, lse = bf16(g.standard_normal((2, 2, T, 64))), torch.zeros((2, 2, T), device=DEV)
+    start = torch.rand((2, 1, 192), device=DEV)
+    w = torch.full_like(start, -1.0)
+    pc.percache_attention_weights(0, q, None, lse, start, w, slot_ids=[[0], [0]], used_len=[[150], [0]], n_chunks=[1, 0], path=[list(range(T))] * 2, n_path=[0, T])
+    torch.cuda.synchronize()
+    assert torch.equal(w[0, :, :150], start[0, :, :150]) and (w[0, :, 150:] == -1).all() and (w[1] == -1).all()
+    pc.close()
