@@ -200,7 +200,7 @@ class Percache:
         self._step_ws = None
         self._lookup_ws = None
         self._topk_ws = None
-        self._draft_ws = None
+        self._draft_ws = {}
         self._draft_bytes = {}
 
     # ------------------------------------------------------------------ helpers
@@ -496,11 +496,13 @@ class Percache:
         return attn_out
 
     # ------------------------------------------------------------------ drafted tokens, eviction inside a slot
-    def _draft_workspace(self, nbytes: int):
+    def _draft_workspace(self, nbytes: int, stream):
+        """Each stream's own: one that is outgrown goes back to the memory of the stream it was made on, where nothing else has used it."""
         import torch
-        if self._draft_ws is None or self._draft_ws.numel() < nbytes + 256:
-            self._draft_ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
-        return (self._draft_ws.data_ptr() + 255) // 256 * 256
+        ws = self._draft_ws.get(stream)
+        if ws is None or ws.numel() < nbytes + 256:
+            ws = self._draft_ws[stream] = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        return (ws.data_ptr() + 255) // 256 * 256
 
     def _draft_need(self, batch, t_draft, max_chunks) -> int:
         key = (batch, t_draft, max_chunks)
@@ -560,9 +562,10 @@ class Percache:
             self._want("q_out", q_out, (batch, Hq, t_draft, D), bf16)
             self._want("k_out", k_out, (batch, Hkv, t_draft, D), bf16)
             self._want("v_out", v_out, (batch, Hkv, t_draft, D), bf16)
+        stream = self._raw_stream()
         need = self._draft_need(batch, t_draft, 0)
         st = self.lib.percache_qkv_rope_draft(self.ctx, x.data_ptr(), wqkv.data_ptr(), batch, t_draft, par_p, p0_p, q_out.data_ptr(), _ptr(k_out), _ptr(v_out),
-                                              self._draft_workspace(need), need, self._raw_stream())
+                                              self._draft_workspace(need, stream), need, stream)
         self._check(st)
         return q_out, k_out, v_out
 
@@ -587,9 +590,10 @@ class Percache:
             lse_out = torch.empty((batch, Hq, t_draft), dtype=torch.float32, device=self.device)
         else:
             self._want("lse_out", lse_out, (batch, Hq, t_draft), torch.float32)
+        stream = self._raw_stream()
         need = self._draft_need(batch, t_draft, max_chunks)
         st = self.lib.percache_attention_draft(self.ctx, layer, q.data_ptr(), k_draft.data_ptr(), v_draft.data_ptr(), batch, t_draft, ids_p, ul_p, nc_p, max_chunks,
-                                               par_p, n_splits, attn_out.data_ptr(), _ptr(lse_out), self._draft_workspace(need), need, self._raw_stream())
+                                               par_p, n_splits, attn_out.data_ptr(), _ptr(lse_out), self._draft_workspace(need, stream), need, stream)
         self._check(st)
         return attn_out, lse_out
 
@@ -613,10 +617,11 @@ class Percache:
             self._want("draft_weights", draft_weights, (batch, Hkv, t_draft), torch.float32)
         elif k_draft is not None:
             draft_weights = torch.empty((batch, Hkv, t_draft), dtype=torch.float32, device=self.device)
+        stream = self._raw_stream()
         need = self._draft_need(batch, t_draft, max_chunks)
         st = self.lib.percache_attention_weights(self.ctx, layer, q.data_ptr(), _ptr(k_draft), _ptr(lse), batch, t_draft, ids_p, ul_p, nc_p, max_chunks, par_p,
                                                  path_p, n_path_p, max_path, _ptr(weights_in), _ptr(weights_out), _ptr(draft_weights),
-                                                 self._draft_workspace(need), need, self._raw_stream())
+                                                 self._draft_workspace(need, stream), need, stream)
         self._check(st)
         return draft_weights
 
@@ -649,9 +654,10 @@ class Percache:
             idx_out = torch.empty((n, c.n_kv_heads, max(most, 0)), dtype=torch.int32, device=self.device)
         else:
             self._want("idx_out", idx_out, (n, c.n_kv_heads, max(most, 0)), torch.int32)
+        stream = self._raw_stream()
         need = self.lib.percache_kv_keep_workspace_bytes(self.ctx, n, most)
-        st = self.lib.percache_kv_keep(self.ctx, layer, sl_p, dst_p, n, kp_p, n_first, n_last, _ptr(weights), idx_out.data_ptr(), self._draft_workspace(need), need,
-                                       self._raw_stream())
+        st = self.lib.percache_kv_keep(self.ctx, layer, sl_p, dst_p, n, kp_p, n_first, n_last, _ptr(weights), idx_out.data_ptr(), self._draft_workspace(need, stream), need,
+                                       stream)
         self._check(st)
         return idx_out
 

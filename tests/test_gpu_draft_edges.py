@@ -130,3 +130,46 @@ def test_weights_of_slots_none_of_whose_rows_counts():
     torch.cuda.synchronize()
     assert torch.equal(w[0, :, :150], start[0, :, :150]) and (w[0, :, 150:] == -1).all() and (w[1] == -1).all()
     pc.close()
+
+
+class WorkspacesOf:
+    """The library with a look at the workspace and the stream that a call is given."""
+
+    def __init__(self, lib):
+        self.lib, self.seen = lib, []
+
+    def __getattr__(self, name):
+        call = getattr(self.lib, name)
+        if name not in ("percache_qkv_rope_draft", "percache_attention_draft", "percache_attention_weights", "percache_kv_keep"):
+            return call
+
+        def looked_at(*args):
+            self.seen.append((args[-3], args[-3] + args[-2], args[-1]))
+            return call(*args)
+        return looked_at
+
+
+def test_a_workspace_is_used_on_one_stream_only():
+    """Work that is still running on one stream keeps its lists and partials whatever another one asks for, and what is given back, its memory."""
+    pc, g, kv = make(36, 4, 2, 64, 128, "bf16", [128, 128, 100])
+    pc.lib = WorkspacesOf(pc.lib)
+    x, wqkv = bf16(g.standard_normal((1, 9, 256))), bf16(0.05 * g.standard_normal((8 * 64, 256)))
+    w = torch.zeros((3, 2, 128), device=DEV)
+    streams = [None, torch.cuda.Stream(), torch.cuda.Stream()]
+    results = []
+    torch.cuda.synchronize()
+    for n in (1, 4):   # (the second time larger ones)
+        for s in streams:
+            with torch.cuda.stream(s):
+                q, k, v = pc.percache_qkv_rope_draft(x.expand(n, 9, 256).contiguous(), wqkv, [256] * n)
+                out, lse = pc.percache_attention_draft(0, q, k, v, slot_ids=[[0, 1]] * n, lse_out=True)
+                paid = pc.percache_attention_weights(0, q, k, lse, None, w, slot_ids=[[0, 1]] * n)
+                pc.percache_kv_keep(0, [2], 100, w)
+            torch.cuda.synchronize()
+            results.append((out[0], lse[0], paid[0]))
+    assert all(torch.equal(a, b) for i in (1, 2, 4, 5) for a, b in zip(results[i // 3 * 3], results[i]))
+    seen = pc.lib.seen
+    assert len(seen) == 24 and len({s for _, _, s in seen}) == 3
+    for lo, hi, s in seen:
+        assert all(s == s2 or hi <= lo2 or hi2 <= lo for lo2, hi2, s2 in seen)
+    pc.close()
