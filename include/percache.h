@@ -285,10 +285,14 @@ pc_status percache_attention_reuse(percache_ctx *ctx, int32_t layer, const void 
  *
  * percache_qkv_rope_draft: steps 1-2 of percache_prefill_reuse for the nodes, node i at position pos0_host[b] + depth(i) (roots: depth 0; padding
  *   too).  The positions are the caller's: behind slots from which tokens were evicted (percache_kv_keep) the cached length is not
- *   the position any more.  x_dev [batch, t_draft, hidden]; q_out_dev [batch, Hq, t_draft, D], k_out_dev, v_out_dev [batch, Hkv, t_draft, D], bf16.
+ *   the position any more.  Without the variants of percache_block_weights (bias, head norms).  x_dev [batch, t_draft, hidden];
+ *   q_out_dev [batch, Hq, t_draft, D], k_out_dev, v_out_dev [batch, Hkv, t_draft, D], bf16.
  * percache_attention_draft: step 3.  attn_out_dev [batch, t_draft, Hq * D] bf16, zero for padding.  lse_out_dev (may be NULL): float
  *   [batch, Hq, t_draft], the log-sum-exp of the scores q.k / sqrt(D) that a row sees, -infinity for padding.  What a row does not see takes no part,
- *   infinities and NaN included.  n_splits as in percache_attention_reuse.  L_pre is not checked against max_pos - t_draft here.
+ *   infinities and NaN included.  n_splits as in percache_attention_reuse.  L_pre is checked as if one token were fresh (L_pre + 1 <= max_pos): the
+ *   nodes' positions are those of the projection.  The probabilities of cached keys are rounded to bf16 for the product with V, as in every
+ *   attention of this library; sums, log-sum-exp and the nodes' probabilities are fp32.  A node costs every row that sees it a dot product:
+ *   meant for trees and short sequences, a prompt goes through percache_attention_reuse.
  * percache_attention_weights: what the rows pay to each key, from the log-sum-exp of the same rows,
  *     w(key) = sum over the queries that use it, the query heads of its kv head and their rows that count, of exp(q.k / sqrt(D) - lse),
  *   rows with lse -infinity none.  path_host == NULL: every row counts; else the nodes of each query's path (after verification: the
@@ -300,7 +304,8 @@ pc_status percache_attention_reuse(percache_ctx *ctx, int32_t layer, const void 
  * percache_kv_append_path: token start_host[b] + j of slot append_slots_host[b] (negative: skipped) becomes row path[j] of k_dev, v_dev
  *   [batch, Hkv, t_draft, D]; tokens that the slot held from start on are dropped (start_host NULL: behind its last token, nothing is dropped).
  *   With draft_weights_dev and weights_dev (both or neither) the nodes' weights go along: weights[slot, kv head, start + j].  In an 8-bit slot
- *   everything from the block of token start on is quantised afresh, as by percache_kv_append.  A slot may appear once.
+ *   everything from the block of token start on is quantised afresh, as by percache_kv_append.  A slot may appear once.  Weights behind the
+ *   path's last token stay as they are.
  * Workspace of the first three: percache_draft_workspace_bytes (max_chunks 0 for the projection), 256-byte aligned.  The calls bring their
  * lists to the device as the calls with host chunk lists do. */
 size_t percache_draft_workspace_bytes(const percache_ctx *ctx, int32_t batch, int32_t t_draft, int32_t max_chunks);
@@ -330,6 +335,8 @@ pc_status percache_kv_append_path(percache_ctx *ctx, int32_t layer, const void *
  * Needs n_first + n_last <= keep_host[i].  dst_slots_host NULL: in place; else the kept tokens (and weights) go to slot dst_slots_host[i], of either
  * format, and the source stays as it is (dst == source: in place).  No slot may appear twice otherwise.  An 8-bit destination is quantised
  * afresh from the values the source reads back.
+ * Weights behind the kept ones stay as they are -- those of evicted tokens, in place: before tokens are appended there without weights of
+ * their own (percache_kv_append, a stack's step) the caller sets them, to zero as a rule, or the new tokens start from the old ones' sums.
  *   idx_out_dev (may be NULL): int32 [n, Hkv, largest keep], the token each kept one was, -1 behind them.
  *   workspace_dev >= percache_kv_keep_workspace_bytes(ctx, n, largest keep), 256-byte aligned. */
 size_t percache_kv_keep_workspace_bytes(const percache_ctx *ctx, int32_t n, int32_t max_keep);

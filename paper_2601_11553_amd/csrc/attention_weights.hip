@@ -1,12 +1,12 @@
 // What a layer's query rows pay to every key: w_t = sum over rows of e^(q.k_t / sqrt(D) - lse), from the rows' log-sum-exp that the attention
 // handed out.  With it the softmax needs no second pass, so a key's weight is one product and one exponential a row, and the keys are read once.
 //
-// The keys stay, the rows pass by: a slot's keys are matrix operands that go over the rows of every query that uses the slot, 32 rows at a
-// time.  So a slot shared by several queries (a system prompt's chunk) is read once, its sums have one owner and one order -- no atomics -- and are added to the
-// running sums in place; only where that would keep one wavefront at work when the others are done are a slot's users split among several, whose sums a second
-// launch adds up (weights_join_kernel).  The rows are on the M side of the product: a lane then has 16 rows of one
-// key, whose exponentials it adds up by itself.  The log-sum-exp, which belongs to rows, comes in as the last step of the contraction: -lse sqrt(D) as
-// the sum of three bf16 numbers (24 bits) against ones.
+// The keys stay, the rows pass by: a slot's keys are matrix operands that go over the rows of every query that uses the slot, 32 rows at a time.  So
+// a slot shared by several queries (a system prompt's chunk) is read once, its sums have one owner and one order -- no atomics -- and are added to
+// the running sums in place; only where that would keep one wavefront at work when the others are done are a slot's users split among several, whose
+// sums a second launch adds up (weights_join_kernel).  The rows are on the M side of the product: a lane then has 16 rows of one key, whose
+// exponentials it adds up by itself.  The log-sum-exp, which belongs to rows, comes in as the last step of the contraction: -lse sqrt(D) as the sum
+// of three bf16 numbers (24 bits) against ones.
 //
 // With few rows (a decoding step) the key stream bounds it: weights_stream_kernel.  With many the exponentials do (24 clocks of the vector port
 // for each 64 of them, where the matrix cores take 18): weights_rows_kernel.
@@ -22,8 +22,8 @@ using pc::u32x4;
 using pc::dec::codes8;
 using pc::dec::fast_exp2;
 
-// Lists of a call (int32 words): the entries, the users of those that have not just one, the slots split among several entries, then -- with paths -- n_path [batch] and the
-// nodes [batch][max_path].
+// Lists of a call (int32 words): the entries, the users of those that have not just one, the slots split among several entries, then -- with paths --
+// n_path [batch] and the nodes [batch][max_path].
 struct Entry {
   int32_t slot;     // slot id; -1 - b: the draft keys of query b
   int32_t piece0;   // first of its pieces among all entries' (few rows: the cost of the entries before it)
@@ -36,8 +36,8 @@ struct User {
 struct Split {
   int32_t slot, longest, parts, place;   // place: of its first entry's sums in Args::parts, 64 floats each: [entry][kv head][tile]
 };
-// Few rows: what a tile costs for each block of 32 rows.  A tile of draft keys has its rows and what they look at to load for itself, about three tiles' time: eight of them
-// in one share, as a tile each, made a call of 35 us one of 42.
+// Few rows: what a tile costs for each block of 32 rows.  A tile of draft keys has its rows and what they look at to load for itself, about three
+// tiles' time: eight of them in one share, as a tile each, made a call of 35 us one of 42.
 constexpr int kDraftCost = 3, kMostCost = 31;
 constexpr int kMostKeys = 1 << 26;
 constexpr int kRowsSpan = 2;   // tiles that weights_rows_kernel holds
@@ -254,10 +254,11 @@ struct Rows {
   __device__ __forceinline__ size_t head8() const { return (size_t)(ent.slot - a.n_slots16) * a.Hkv + g; }
 };
 
-// Few rows: one wavefront walks a share of all tiles with the keys in registers, the next tile's requested ahead -- across the end of an entry, too --, and its rows --
-// where they are one block -- loaded once for all tiles of a query.  The shares are equal, so that all end together: a tile counts as one, or as what its blocks of rows make
-// of it (Entry::keys), and belongs to the share that it starts in.  Up to 2 wavefronts a SIMD, each with 16 KB on the way.  FMT: 0 bf16 slots, 1 8-bit slots, 2 both.
-// 8 queries, 15 rows of a kv head (24 heads over 8) over 12.4k keys each, one chunk shared: 195 MB in 37.5 us (5.2 TB/s); 48.6 with the keys loaded as operands and with pieces of at most six tiles of one slot.
+// Few rows: one wavefront walks a share of all tiles with the keys in registers, the next tile's requested ahead -- across the end of an entry, too
+// --, and its rows -- where they are one block -- loaded once for all tiles of a query.  The shares are equal, so that all end together: a tile
+// counts as one, or as what its blocks of rows make of it (Entry::keys), and belongs to the share that it starts in.  Up to 2 wavefronts a SIMD, each
+// with 16 KB on the way.  FMT: 0 bf16 slots, 1 8-bit slots, 2 both. 8 queries, 15 rows of a kv head (24 heads over 8) over 12.4k keys each, one chunk
+// shared: 195 MB in 37.5 us (5.2 TB/s); 48.6 with the keys loaded as operands and with pieces of at most six tiles of one slot.
 template <int D, int FMT>
 __global__ __launch_bounds__(64, 2) void weights_stream_kernel(const Args a) {
   constexpr int KS = D / 16;
@@ -283,8 +284,8 @@ __global__ __launch_bounds__(64, 2) void weights_stream_kernel(const Args a) {
   int tile_end = end_of(ent);
   if (tile >= tile_end) return;
   Rows<D> rows(a, ent, g, lane, row_sees);
-  // A tile comes through LDS: instruction i of its request fills bytes [1024 i, +1024), 16-byte chunks XOR-swizzled inside the rows.  (Loaded as operands, 32 bytes of 32 rows an
-  // instruction, a line passes the first-level cache four times: 16 KB of each of 8 wavefronts do not stay in it.)
+  // A tile comes through LDS: instruction i of its request fills bytes [1024 i, +1024), 16-byte chunks XOR-swizzled inside the rows.  (Loaded as
+  // operands, 32 bytes of 32 rows an instruction, a line passes the first-level cache four times: 16 KB of each of 8 wavefronts do not stay in it.)
   auto swz = [](int row_bytes, int row) __attribute__((always_inline)) { return row_bytes == 256 ? (row & 15) : row_bytes == 128 ? ((row >> 1) & 7) : ((row >> 2) & 3); };
   float next_scale = 1.f;
   auto copy = [&](const char *src, auto row_bytes_c, int rows_there) __attribute__((always_inline)) {
@@ -421,10 +422,10 @@ __global__ __launch_bounds__(64, 2) void weights_stream_kernel(const Args a) {
   put();
 }
 
-// Many rows: a workgroup of four wavefronts keeps the keys of up to two tiles in LDS as bf16 (16-byte pieces XOR-swizzled inside rows of 256 bytes by row & 15, of
-// 128 bytes by (row >> 1) & 7); the wavefronts take every fourth block of rows each.  Small pieces of work and four wavefronts a SIMD: while one waits for its lists,
-// keys or rows, the others keep the vector port busy.  (Two wavefronts a SIMD with the keys in registers, or four tiles in LDS and the next block's rows requested
-// ahead: 4 prompts of 256 rows x 16 heads over 3100 keys 51 and 43 us.)
+// Many rows: a workgroup of four wavefronts keeps the keys of up to two tiles in LDS as bf16 (16-byte pieces XOR-swizzled inside rows of 256 bytes by
+// row & 15, of 128 bytes by (row >> 1) & 7); the wavefronts take every fourth block of rows each.  Small pieces of work and four wavefronts a SIMD:
+// while one waits for its lists, keys or rows, the others keep the vector port busy.  (Two wavefronts a SIMD with the keys in registers, or four
+// tiles in LDS and the next block's rows requested ahead: 4 prompts of 256 rows x 16 heads over 3100 keys 51 and 43 us.)
 template <int D, int FMT>
 __global__ __launch_bounds__(256, 4) void weights_rows_kernel(const Args a) {
   constexpr int KS = D / 16, ROW = D * 2, TILE = kKvTile * ROW;
@@ -568,10 +569,11 @@ extern "C" pc_status percache_attention_weights(percache_ctx *ctx, int32_t layer
       use(slots.back(), b, t_draft);
     }
   if (slots.empty()) return PC_OK;
-  // Many rows of a query to a key: weights_rows_kernel, in pieces of two tiles, fewer where a tile has more blocks of rows than the others; what has more of them comes first.
-  // Else weights_stream_kernel, in shares of equal cost for all wavefronts that the chip holds at once (8 a CU).  A slot's users are split where a tile would have more blocks
-  // of rows than `most`: as many as the others, or four more than a wavefront's share has tiles (a block takes about the time of a tile, the launch that adds the sums up four).  us, 4 prompts of 256 rows (16 heads over 8) over 8 chunks of 384 tokens on average,
-  // one of them shared: whole 36.8, split 27.9 and 4.0 for the sums.
+  // Many rows of a query to a key: weights_rows_kernel, in pieces of two tiles, fewer where a tile has more blocks of rows than the others; what has
+  // more of them comes first. Else weights_stream_kernel, in shares of equal cost for all wavefronts that the chip holds at once (8 a CU).  A slot's
+  // users are split where a tile would have more blocks of rows than `most`: as many as the others, or four more than a wavefront's share has tiles
+  // (a block takes about the time of a tile, the launch that adds the sums up four).  us, 4 prompts of 256 rows (16 heads over 8) over 8 chunks of
+  // 384 tokens on average, one of them shared: whole 36.8, split 27.9 and 4.0 for the sums.
   int most_rows = 0, least_blocks = INT32_MAX;
   long all_tiles = 0;
   for (int b = 0; b < batch; ++b) most_rows = std::max(most_rows, rows_of(b));

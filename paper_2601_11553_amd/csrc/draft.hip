@@ -1,17 +1,17 @@
 // Verification of drafted tokens: each query brings a tree of t_draft nodes (a node behind its parent), all of them run through a layer at
 // once.  Node i sits at position pos0 + depth(i) and attends over [cached chunks ; its ancestors ; itself],
 //   o_i = sum_j e^(s_ij - lse_i) v_j,   s_ij = q_i.k_j / sqrt(D),   lse_i = log sum_j e^s_ij.
-// The projection and the attention are the kernels of qkv_rope_gemm.hip, reuse_attention.hip and decode_attention.hip; here are the host
-// entry points and the lists they take: positions of the nodes, and for the attention one word of 64 bits per node and 64 nodes that
-// says which of them it looks at.
+// The projection is that of qkv_rope_gemm.hip, the attention decode_attention.hip up to 32 rows a kv head and draft_attention.hip above.  Here are
+// the host entry points, the lists they take -- positions of the nodes, and for the attention one word of 64 bits per node and 64 nodes that
+// says which of them it looks at --, and the merge of the attention's partials with the nodes.
 #include "decode_common.hpp"
 
 namespace {
 
-// One workgroup a query: ancestors by pointer doubling, sees[i] |= sees[up[i]], up[i] = up[up[i]], in log2(longest path) rounds, between the lanes of a wavefront (up to 64
-// nodes; 48 nodes 3.6 us through LDS, 2.6 so) or between two LDS buffers.  The parents come packed, two to a word, as a launch argument (FROM_ARG; with the words in front of them, which workgroup
-// `batch` then copies) or from device memory.  16 bits of parents a node travel instead of 64 bits or more of `sees`: 8 queries of 64
-// nodes with their chunk list still fit a launch's arguments.
+// One workgroup a query: ancestors by pointer doubling, sees[i] |= sees[up[i]], up[i] = up[up[i]], in log2(longest path) rounds, between the lanes of
+// a wavefront (up to 64 nodes; 48 nodes 3.6 us through LDS, 2.6 so) or between two LDS buffers.  The parents come packed, two to a word, as a launch
+// argument (FROM_ARG; with the words in front of them, which workgroup `batch` then copies) or from device memory.  16 bits of parents a node travel
+// instead of 64 bits or more of `sees`: 8 queries of 64 nodes with their chunk list still fit a launch's arguments.
 constexpr int kTreeThreads = 256;
 template <bool FROM_ARG>
 __global__ __launch_bounds__(kTreeThreads) void draft_lists_kernel(int32_t *dst, int n_words, const pc::ListWords lists, const int32_t *packed, int batch, int T,
@@ -105,12 +105,14 @@ __device__ __forceinline__ float halve16(float x, float y) {
 }
 
 // The merge of a row's partials over the cached keys, and the nodes that the row looks at, a handful of a tree's: each of them is a dot product and
-// one more weighted row, which no tile of matrix products would be worth -- and a node that a row does not look at is not read for it,
-// whatever it holds.  A wavefront takes one node of the tree and H heads of a group, which look at the same nodes: lane (sg, dv) has 8 elements of a head and
-// takes partials sg, sg + SG, ... (NP of them at a time) and, 16 nodes of the row at a time, NB of them, dealt out by scalar arithmetic; the SG running (max, sum,
-// output) meet through lane exchanges that leave every lane with the elements it writes.  Its time is that of two memory latencies while the rows fit the chip
-// at once -- the first nodes are asked for as soon as the row's word of `sees` is there, the partials looked at behind that --, then that of the vector port, hence H.
-// 12288 rows of 13 nodes and 4 partials: 17.6 us with a row a wavefront, nodes dealt out lane by lane and whole sums exchanged, 13.0 now.
+// one more weighted row, which no tile of matrix products would be worth -- and a node that a row does not look at is not read for it, whatever it
+// holds.  (In a long plain sequence a row looks at half of the nodes: 4 sequences over 8 x 512 keys each, 16 heads over 8, the merge alone 26 us at
+// 128 nodes, 74 at 256, 218 at 512, where percache_attention_reuse takes 44, 54 and 92 for the whole call.)  A wavefront takes one node of the tree
+// and H heads of a group, which look at the same nodes: lane (sg, dv) has 8 elements of a head and takes partials sg, sg + SG, ... (NP of them at a
+// time) and, 16 nodes of the row at a time, NB of them, dealt out by scalar arithmetic; the SG running (max, sum, output) meet through lane exchanges
+// that leave every lane with the elements it writes.  Its time is that of two memory latencies while the rows fit the chip at once -- the first nodes
+// are asked for as soon as the row's word of `sees` is there, the partials looked at behind that --, then that of the vector port, hence H. 12288
+// rows of 13 nodes and 4 partials: 17.6 us with a row a wavefront, nodes dealt out lane by lane and whole sums exchanged, 13.0 now.
 template <int D, int NP, int H>
 __global__ __launch_bounds__(256) void draft_merge_kernel(const float *__restrict__ part_o, const float *__restrict__ part_ml, int n_splits, const __bf16 *__restrict__ Q,
                                                           const __bf16 *__restrict__ K, const __bf16 *__restrict__ V, int T, int Hq, int Hkv,
@@ -314,7 +316,8 @@ DraftWs carve_draft_ws(const percache_config &c, int n_cu, void *base, int32_t b
   size_t off = 0;
   auto take = [&](size_t bytes) { char *r = p ? p + off : nullptr; off += align_up(bytes); return r; };
   const size_t B = batch, T = t_draft, ft = (T + kKvTile - 1) / kKvTile, rows = B * c.n_q_heads * T, nc = max_chunks;
-  // attention: chunk table, packed parents; projection: positions; weights: entries, users, splits (14 words a chunk and query at most), paths (of at most t_draft nodes), packed parents
+  // attention: chunk table, packed parents; projection: positions; weights: entries, users, splits (14 words a chunk and query at most), paths (of at
+  // most t_draft nodes), packed parents
   w.words = (int32_t *)take((B * (14 * (nc + 1) + 3 * T + 8) + 16) * sizeof(int32_t));
   w.sees = (uint2 *)take(t_draft <= kMaxNodes ? B * T * ft * sizeof(uint2) : 0);
   const size_t cap = max_splits_for(c, n_cu, batch, t_draft);

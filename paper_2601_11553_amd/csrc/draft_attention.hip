@@ -1,21 +1,26 @@
 // Attention of the nodes of drafted trees, more than 32 rows a kv head, over the cached keys (the nodes that a row looks at are added in the merge, draft.hip).
 //
-// What bounds it: 64 to 192 rows share a key, which is about where the key stream and the matrix cores take equally long, and a matrix operand read from LDS should
-// serve as many rows as the registers hold outputs for.  The long-context kernel of a prompt (reuse_attention.hip) has 32 rows a wavefront: its eight wavefronts read
-// 256 KB of operands for a 32 KB tile, as many clocks of LDS as of the matrix cores, and 192 rows leave two of them without work.  Here a workgroup is RG groups of
-// rows x two halves of a 64-key tile, a wavefront NR blocks of 16 rows x 32 keys (16x16x32 products):
+// What bounds it: 64 to 192 rows share a key, which is about where the key stream and the matrix cores take equally long, and a matrix operand read
+// from LDS should serve as many rows as the registers hold outputs for.  The long-context kernel of a prompt (reuse_attention.hip) has 32 rows a
+// wavefront: its eight wavefronts read 256 KB of operands for a 32 KB tile, as many clocks of LDS as of the matrix cores, and 192 rows leave two of
+// them without work.  Here a workgroup is RG groups of rows x two halves of a 64-key tile, a wavefront NR blocks of 16 rows x 32 keys (16x16x32
+// products):
 //   - every operand serves NR blocks: 128 KB of LDS a tile whatever NR, and 192 rows are 4 x 3 blocks, nothing idle;
-//   - scores come out transposed, S^T = K Q^T, a lane with 4 keys of each of two 16-key blocks of one row, which is the B operand of O^T += V^T P^T as it stands.  Which
-//     key is which row of a block is free: the K rows are read in the order in which V lies (the 8 keys of lane group g: 16 (g % 2) + 4 (g / 2) + 8 j + e, block j), so that
-//     an operand of V is one 16-byte read (8 bytes of codes);
-//   - a ring of stages filled by direct global->LDS loads, the scales of a tile of codes among them, one barrier a tile (it says that tile t has landed for every wavefront
-//     and that tile t - 1 has been read);
-//   - up to 64 rows over codes: RG = 2, half the wavefronts with two blocks each, so that a code is turned into bf16 half as often, and two workgroups on a CU;
+//   - scores come out transposed, S^T = K Q^T, a lane with 4 keys of each of two 16-key blocks of one row, which is the B operand of O^T += V^T P^T
+//     as it stands.  Which key is which row of a block is free: the K rows are read in the order in which V lies (the 8 keys of lane group g: 16 (g %
+//     2) + 4 (g / 2) + 8 j + e, block j), so that an operand of V is one 16-byte read (8 bytes of codes);
+//   - a ring of stages filled by direct global->LDS loads, the scales of a tile of codes among them, one barrier a tile (it says that tile t has
+//     landed for every wavefront and that tile t - 1 has been read);
+//   - up to 64 rows over codes: RG = 2, half the wavefronts with two blocks each, so that a code is turned into bf16 half as often, and two
+//     workgroups on a CU;
 //   - the two halves of a row's keys meet once, through LDS, and leave one fp32 partial.
-// 8 queries x 8 kv heads, 192 rows over 12.4k keys (bf16, D = 128): 102 us (0.78 PF of products), the long-context kernel with its masks 107.  A tile takes 1.4 us there, of
-// which (timed with the part left out) the products of either kind take 0.3, the reads of LDS 0.2, the exponentials and the requests 0.15 each; the two wavefronts of a SIMD half
-// a tile apart, and the requests behind the reads, changed nothing.  Of the launch's 102 us a wavefront lives 80: the longest query has 1.1 times the mean's keys, and
-// there is the first tile to wait for.  6 queries x 8 kv heads, 63 rows over 157 tiles of codes: 34 us (4.6 TB/s; the prompt's kernel 37).
+// 8 queries x 8 kv heads, 192 rows over 12.4k keys (bf16, D = 128): 89 us (0.87 PF of products), 106 in a process's first thirty launches, while the
+// clock settles.  With a part left out, us a call that took 102: the products of either kind 84, the reads of LDS 88, the exponentials or the
+// requests 93; the two wavefronts of a SIMD half a tile apart, and the requests behind the reads, changed nothing.  A wavefront lives four fifths of
+// the launch: the longest query has 1.1 times the mean's keys, and there is the first tile to wait for.  6 queries x 8 kv heads, 63 rows over 157
+// tiles of codes, one chunk shared: 31 us (3.7 TB/s of codes).
+//
+// Precision: a probability is rounded to bf16 for the product with V (its sum is taken before), everything else is fp32.
 #include "decode_common.hpp"
 
 namespace {
@@ -149,8 +154,9 @@ __global__ __launch_bounds__(128 * RG, 2) void draft_attention_kernel(
     }
   };
 
-  // ---- requests: instruction i of a tile half fills its bytes [1024 i, +1024); 16-byte chunks XOR-swizzled inside a row so that the 16 rows that are read at once fall into
-  // different banks (of V 16 consecutive ones, of K rows 0..7 and 16..23, or 8 more): rows of 256 bytes one to a line of all banks, of 128 bytes two, of 64 bytes four
+  // ---- requests: instruction i of a tile half fills its bytes [1024 i, +1024); 16-byte chunks XOR-swizzled inside a row so that the 16 rows that
+  // are read at once fall into different banks (of V 16 consecutive ones, of K rows 0..7 and 16..23, or 8 more): rows of 256 bytes one to a line of
+  // all banks, of 128 bytes two, of 64 bytes four
   auto swz = [](int row_bytes, int row) __attribute__((always_inline)) { return row_bytes == 256 ? (row & 15) : row_bytes == 128 ? ((row >> 1) & 7) : ((row >> 2) & 3); };
   auto swz_k = [&](int row_bytes, int row) __attribute__((always_inline)) { return swz(row_bytes, (row & 7) | (row >> 1 & 8)); };
   constexpr int N16 = L::K16 / 1024, N8 = L::K8 / 1024;   // instructions of a tile half (K or V)
@@ -197,9 +203,9 @@ __global__ __launch_bounds__(128 * RG, 2) void draft_attention_kernel(
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int r = 0; r < NR; ++r) s[j][r] = f32x4{0.f, 0.f, 0.f, 0.f};
-    // Operands of V as they lie in LDS (codes: the first two words).  What is read together is held together: everything of K and the first VB of V ahead of the
-    // products, the rest of V (where the registers do not hold all of it) ahead of the softmax.  (Codes are read as vectors: a load of the struct uint2 is taken to alias
-    // the direct loads into LDS and waits for all of them.)
+    // Operands of V as they lie in LDS (codes: the first two words).  What is read together is held together: everything of K and the first VB of V
+    // ahead of the products, the rest of V (where the registers do not hold all of it) ahead of the softmax.  (Codes are read as vectors: a load of
+    // the struct uint2 is taken to alias the direct loads into LDS and waits for all of them.)
     constexpr int VB = NR == 3 && D == 128 ? DB / 2 : DB;
     pc::u32x4 v[DB];
     float vs8 = 1.f;
@@ -345,8 +351,8 @@ __global__ __launch_bounds__(128 * RG, 2) void draft_attention_kernel(
     const int valid = min(TK, cmp.left);
     const bool b8 = is8(cmp);
     advance(cmp);
-    // what this wavefront has in flight for the tiles behind this one (mixed formats: counted as the smaller kind, which waits for more; a wavefront that a half of a small
-    // tile of codes has no instruction for asks for the scales only)
+    // what this wavefront has in flight for the tiles behind this one (mixed formats: counted as the smaller kind, which waits for more; a wavefront
+    // that a half of a small tile of codes has no instruction for asks for the scales only)
     constexpr int BF16 = 2 * (N16 / NW), CODES = 2 * (N8 >= NW ? N8 / NW : 1) + 1, IPT = FMT == 0 ? BF16 : FMT == 1 ? CODES : BF16 < CODES ? BF16 : CODES;
     const int later = min(NSTG - 2, n - 1 - t);
     if (later <= 0) PC_WAIT_VMCNT(0);
@@ -406,12 +412,13 @@ float tile_us(int D, int fmt, int nr) {
   if (D == 128) return fmt == 0 ? 0.52f + 0.30f * nr : fmt == 1 ? 0.45f + 0.38f * nr : 0.75f + 0.36f * nr;
   return fmt == 0 ? 0.42f + 0.23f * nr : fmt == 1 ? 0.34f + 0.29f * nr : 0.62f + 0.26f * nr;
 }
-// Row blocks of a wavefront and partitions of the key axis.  Blocks: the least time of all row blocks of a tile, so as many rows share an operand as pays (both kinds of
-// tiles in one kernel leave registers for two blocks at D = 128).  Partitions: the least of an estimate that has the rounds in which the workgroups go, tiles of
-// 1.7 times the time where two share a CU, 4 us for a workgroup's start and end, and the partials' bytes there and back.
-// Over 138 calls (33 to 448 rows, 1 to 16 queries, 22 to 213 tiles, all formats and both head sizes, each timed at up to 19 counts) the counts so chosen take 1.01 times the
-// best one's time on average, 1.19 at worst.  us a call, too few | this | too many partitions: 8 kv heads x 8 queries, 126 rows over 53 tiles (bf16, D = 128, 4 kv heads 32
-// | 4) 35 | 29 | 37; blocks of 64 rows against blocks of 192 over the 280 rows of 7 query heads: 0.82 us x 5 | 1.42 x 2 a tile.
+// Row blocks of a wavefront and partitions of the key axis.  Blocks: the least time of all row blocks of a tile, so as many rows share an operand as
+// pays (both kinds of tiles in one kernel leave registers for two blocks at D = 128).  Partitions: the least of an estimate that has the rounds in
+// which the workgroups go, tiles of 1.7 times the time where two share a CU, 4 us for a workgroup's start and end, and the partials' bytes there and
+// back. Over 138 calls (33 to 448 rows, 1 to 16 queries, 22 to 213 tiles, all formats and both head sizes, each timed at up to 19 counts) the counts
+// so chosen take 1.01 times the best one's time on average, 1.19 at worst.  us a call, too few | this | too many partitions: 8 kv heads x 8 queries,
+// 126 rows over 53 tiles (bf16, D = 128, 4 kv heads 32 | 4) 35 | 29 | 37; blocks of 64 rows against blocks of 192 over the 280 rows of 7 query heads:
+// 0.82 us x 5 | 1.42 x 2 a tile.
 struct Plan {
   int nr, q_tiles, n_splits;
 };

@@ -22,10 +22,11 @@ __device__ __forceinline__ unsigned key_of(float w) {
 }
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64, kSelLds = 8192;
-// One workgroup a (kv head, slot).  idx [n][Hkv][idx_stride]: the kept tokens in order, -1 behind them; weights are moved along.
-// Up to four passes over a few thousand keys (the last ones mostly spared: few tokens share three digits) and one over the tokens, each a few LDS accesses and barriers: a chain of latencies, so the keys are read from memory
-// once, into LDS (slots of up to kSelLds tokens; longer ones are read again from the L2).  2048 tokens, 128 workgroups: 14.9 us read in every pass, 9.5 from LDS, 8.6 with
-// the passes spared and the sums of digits taken inside the vector pipe.
+// One workgroup a (kv head, slot).  idx [n][Hkv][idx_stride]: the kept tokens in order, -1 behind them; weights are moved along. Up to four passes
+// over a few thousand keys (the last ones mostly spared: few tokens share three digits) and one over the tokens, each a few LDS accesses and
+// barriers: a chain of latencies, so the keys are read from memory once, into LDS (slots of up to kSelLds tokens; longer ones are read again from the
+// L2).  2048 tokens, 128 workgroups: 14.9 us read in every pass, 9.5 from LDS, 8.6 with the passes spared and the sums of digits taken inside the
+// vector pipe.
 __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights, const Moves mv, int Hkv, int C, int n_first, int n_last, int32_t *idx, int idx_stride) {
   __shared__ unsigned keys[kSelLds];
   __shared__ unsigned hist[256];
@@ -88,7 +89,8 @@ __global__ __launch_bounds__(kSelThreads) void keep_select_kernel(float *weights
       if (whole) break;
     }
   }
-  // `need` tokens with the key `top` are kept, the first ones (whole: every token that starts with its digits), and all with a larger key (keep >= have: every token)
+  // `need` tokens with the key `top` are kept, the first ones (whole: every token that starts with its digits), and all with a larger key (keep >=
+  // have: every token)
   int at = 0, ties = 0;
   for (int t0 = 0; t0 < have; t0 += kSelThreads) {
     const int t = t0 + tid;
@@ -144,11 +146,11 @@ struct Image {
   static constexpr int HALF = kKvTile * D * 2, BYTES = 2 * HALF + 256;
 };
 
-// One workgroup a (slot, kv head, 64 kept tokens): the tokens' K rows are gathered in registers as bf16 (8-bit slots: code * 2^e, exact), V in LDS as a bf16 block, and
-// written in the destination's format, an 8-bit block quantised afresh.  K: 16-byte pieces of the tokens' rows.  V: a token is one element in each of the D rows of its
-// block, so the blocks that hold kept tokens are read one after the other, 16 bytes of a row a lane (left out where none of them is kept), and the kept elements
-// put where they belong; read element by element, two bytes a lane, the addresses took longer than the bytes.  16 slots x 8 heads, 1000 of 1536 tokens
-// on average, D = 128, half of either format: 43.6 us element by element, 30.2 so (111 MB).
+// One workgroup a (slot, kv head, 64 kept tokens): the tokens' K rows are gathered in registers as bf16 (8-bit slots: code * 2^e, exact), V in LDS as
+// a bf16 block, and written in the destination's format, an 8-bit block quantised afresh.  K: 16-byte pieces of the tokens' rows.  V: a token is one
+// element in each of the D rows of its block, so the blocks that hold kept tokens are read one after the other, 16 bytes of a row a lane (left out
+// where none of them is kept), and the kept elements put where they belong; read element by element, two bytes a lane, the addresses took longer than
+// the bytes.  16 slots x 8 heads, 1000 of 1536 tokens on average, D = 128, half of either format: 43.6 us element by element, 30.2 so (111 MB).
 template <int D>
 __global__ __launch_bounds__(256) void keep_move_kernel(Store st, const Moves mv, const int32_t *__restrict__ idx, int idx_stride, int Hkv, int C, char *__restrict__ images,
                                                         int tiles) {
