@@ -344,6 +344,53 @@ pc_status percache_kv_keep(percache_ctx *ctx, int32_t layer, const int32_t *slot
                            const int32_t *keep_host, int32_t n_first, int32_t n_last, float *weights_dev, int32_t *idx_out_dev,
                            void *workspace_dev, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------- prompts of different lengths in one call
+ * A server's requests have prompts of different lengths, and single tokens of running requests go beside them.  Their fresh rows stand one behind
+ * the other ("packed"): request s has rows [start_host[s], start_host[s + 1]) of n_rows, possibly none; rows before the first and behind the
+ * last request belong to nobody and are left as they are.  Tensors are by heads, [heads, n_rows, D]: percache_kv_slice takes packed K and V as
+ * the one sequence that they are to it (bounds: the requests' first rows) and stores every request's in a slot of its own.
+ *
+ * percache_qkv_norm_rope: rows of a QKV projection finished in one pass.  Row r of qkv_dev ([n_rows, (Hq + 2 Hkv) * D] bf16, rows row_stride elements
+ *   apart) plus the bias (may be NULL); q and k heads through an RMSNorm with gain q_norm, k_norm ([D], either may be NULL); pairs
+ *   (m, m + D/2) of q and k turned by pos[axis(m)][r] * theta^(-2m/D); one rounding.  pos_dev: int32 [n_axes, n_rows], 1 <= n_axes <= 4 (text: one
+ *   axis; images and video: time, height, width); axis_host: uint8 [D/2], the axis of every pair, in any arrangement (NULL with one axis).  A
+ *   position outside [0, max_pos) makes the pairs that go by it NaN.  Outputs [Hq or Hkv, n_rows, D]; they must not overlap the input.
+ * percache_attention_packed: row i of request s over [its cached chunks ; its own rows t <= i], as percache_attention_reuse (the chunk list likewise, one
+ *   entry a request; every request's chunks in slots of any format).  attn_out_dev [n_rows, Hq * D] bf16; lse_out_dev (may be NULL): float
+ *   [Hq, n_rows], the log-sum-exp of a row's scores.  Positions are those of q and k already, so L_pre is checked as if one token were
+ *   fresh.  What a row does not see takes no part, infinities and NaN included: cached tokens behind the used length, later rows, other requests.
+ *   n_splits > 0 cuts every row block's keys into that many partitions (at most percache_packed_max_splits), 0: chosen by the library.
+ *   workspace_dev >= percache_packed_workspace_bytes(ctx, n_seq, n_rows, max_chunks), 256-byte aligned.  The call brings its lists to the device as
+ *   the calls with host chunk lists do. */
+pc_status percache_qkv_norm_rope(percache_ctx *ctx, const void *qkv_dev, int64_t row_stride, int32_t n_rows, const int32_t *pos_dev,
+                                 int32_t n_axes, const uint8_t *axis_host, const void *qkv_bias_dev, const void *q_norm_dev,
+                                 const void *k_norm_dev, float eps, void *q_out_dev, void *k_out_dev, void *v_out_dev, void *stream);
+size_t percache_packed_workspace_bytes(const percache_ctx *ctx, int32_t n_seq, int32_t n_rows, int32_t max_chunks);
+int32_t percache_packed_max_splits(const percache_ctx *ctx, int32_t n_seq, int32_t n_rows);
+pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void *q_dev, const void *k_dev, const void *v_dev, int32_t n_rows,
+                                    const int32_t *start_host, int32_t n_seq, const int32_t *slot_ids_host, const int32_t *used_len_host,
+                                    const int32_t *n_chunks_host, int32_t max_chunks, int32_t n_splits, void *attn_out_dev, float *lse_out_dev,
+                                    void *workspace_dev, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------- several continuations of a prompt
+ * percache_kv_fork: slot dst_slots_host[i] becomes, in layers [layer0, layer0 + n_layers), a copy of the first n_tokens_host[i] tokens of slot
+ *   src_slots_host[i] (n_tokens_host NULL: all it holds in that layer), element for element: 8-bit codes and scales as they are.  All copies take
+ *   what the slots held before the call, so slots may change places.  Source and destination hold the same format (percache_kv_keep moves
+ *   tokens between formats); a source may appear often, a destination once; a slot copied to itself is cut to n_tokens.
+ * percache_beam_select: request b goes on from `beams` beams with scores_dev[b][i] (float [batch, beams]; -infinity: the beam does not exist) and logits
+ *   [batch * beams, vocab] (rows row_stride elements apart; fp32 0: bf16, 1: float).  Candidate (i, t) has
+ *     scores[b][i] + logits[b][i][t] - log sum_u e^logits[b][i][u];
+ *   the `best` largest, best first, equal ones by the lower beam, then the lower token: parent_out_dev, token_out_dev int32 [batch, best],
+ *   score_out_dev float [batch, best]; -1, -1, -infinity where there are fewer.  A logit of -infinity is never chosen.  A beam whose score or
+ *   log-sum-exp is not finite has no candidates.  beams, best at most 64, beams * best at most 2048.
+ *   workspace_dev >= percache_beam_select_workspace_bytes(...), 256-byte aligned. */
+pc_status percache_kv_fork(percache_ctx *ctx, int32_t layer0, int32_t n_layers, const int32_t *src_slots_host, const int32_t *dst_slots_host,
+                           const int32_t *n_tokens_host, int32_t n, void *stream);
+size_t percache_beam_select_workspace_bytes(const percache_ctx *ctx, int32_t batch, int32_t beams, int32_t vocab, int32_t best);
+pc_status percache_beam_select(percache_ctx *ctx, const void *logits_dev, int32_t fp32, int64_t row_stride, const float *scores_dev, int32_t batch,
+                               int32_t beams, int32_t vocab, int32_t best, int32_t *parent_out_dev, int32_t *token_out_dev,
+                               float *score_out_dev, void *workspace_dev, size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------- cache index (Sec. 4.1.1, Sec. 4.2.2, App. B.2)
  * Host-side prefix tree over knowledge chunks that hands out slot ids of the K/V store; no device work.  A node is
  * one chunk (keyed by its text), a path from the root the chunk list of one query.  The same slot id is meant to

@@ -34,6 +34,8 @@ EXPORTS = [
     "percache_prefill_reuse_table", "percache_stack_reuse_table",
     "percache_draft_workspace_bytes", "percache_qkv_rope_draft", "percache_attention_draft", "percache_attention_weights",
     "percache_kv_append_path", "percache_kv_keep_workspace_bytes", "percache_kv_keep",
+    "percache_qkv_norm_rope", "percache_packed_workspace_bytes", "percache_packed_max_splits", "percache_attention_packed", "percache_kv_fork",
+    "percache_beam_select_workspace_bytes", "percache_beam_select",
     "percache_profile_enable", "percache_profile_read",
     "percache_peak_scratch_bytes", "percache_peak_mfma_bf16", "percache_peak_stream_read", "percache_peak_attention_tile_loop",
 ]
@@ -113,6 +115,13 @@ def load_library() -> ctypes.CDLL:
         "percache_kv_append_path": (_i32, [_vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]),
         "percache_kv_keep_workspace_bytes": (_sz, [_vp, _i32, _i32]),
         "percache_kv_keep": (_i32, [_vp, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
+        "percache_qkv_norm_rope": (_i32, [_vp, _vp, ctypes.c_int64, _i32, _vp, _i32, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+        "percache_packed_workspace_bytes": (_sz, [_vp, _i32, _i32, _i32]),
+        "percache_packed_max_splits": (_i32, [_vp, _i32, _i32]),
+        "percache_attention_packed": (_i32, [_vp, _i32, _vp, _vp, _vp, _i32, _vp, _i32, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _sz, _vp]),
+        "percache_kv_fork": (_i32, [_vp, _i32, _i32, _vp, _vp, _vp, _i32, _vp]),
+        "percache_beam_select_workspace_bytes": (_sz, [_vp, _i32, _i32, _i32, _i32]),
+        "percache_beam_select": (_i32, [_vp, _vp, _i32, ctypes.c_int64, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
         "percache_kv_slice": (_i32, [_vp, _i32, _vp, _vp, _i32, _pi32, _pi32, _i32, _vp]),
         "percache_kv_append": (_i32, [_vp, _i32, _i32, _vp, _vp, _i32, _vp]),
         "percache_stack_decode": (_i32, [_vp, ctypes.POINTER(BlockWeights), _i32, _i32, ctypes.c_float, _vp, _i32, _i32,
@@ -660,6 +669,108 @@ class Percache:
                                        stream)
         self._check(st)
         return idx_out
+
+    # ------------------------------------------------------------------ prompts of different lengths in one call
+    def percache_qkv_norm_rope(self, qkv, pos, axis=None, qkv_bias=None, q_norm=None, k_norm=None, eps: float = 1e-6, q_out=None, k_out=None, v_out=None):
+        """Rows of a QKV projection [N, (Hq + 2 Hkv) * D] (rows may be strided) with positions pos [axes, N] (int32, on the device; [N]: one axis) finished to
+        q [Hq, N, D], k, v [Hkv, N, D].  axis: of every one of the D/2 pairs (None with one axis)."""
+        import torch
+        bf16 = torch.bfloat16
+        c = self.cfg
+        Hq, Hkv, D = c.n_q_heads, c.n_kv_heads, c.head_dim
+        F = (Hq + 2 * Hkv) * D
+        if qkv.dim() != 2 or qkv.dtype != bf16 or qkv.shape[1] != F or not qkv.is_cuda or qkv.stride(1) != 1:
+            raise ValueError(f"qkv: a {bf16} tensor [N, {F}] on the GPU with dense rows is wanted, got {qkv.dtype} {tuple(qkv.shape)} strides {qkv.stride()}")
+        n = qkv.shape[0]
+        if pos.dim() == 1:
+            pos = pos[None]
+        self._want("pos", pos, (pos.shape[0], n), torch.int32)
+        if axis is not None:
+            axis = np.ascontiguousarray(axis, np.uint8).reshape(-1)
+            if axis.size != D // 2:
+                raise ValueError(f"axis: {axis.size} entries for {D // 2} pairs")
+        self._want("qkv_bias", qkv_bias, (F,), bf16)
+        self._want("q_norm", q_norm, (D,), bf16)
+        self._want("k_norm", k_norm, (D,), bf16)
+        outs = []
+        for name, t, h in (("q_out", q_out, Hq), ("k_out", k_out, Hkv), ("v_out", v_out, Hkv)):
+            if t is None:
+                t = torch.empty((h, n, D), dtype=bf16, device=self.device)
+            else:
+                self._want(name, t, (h, n, D), bf16)
+            outs.append(t)
+        # (a single row has no stride of its own)
+        st = self.lib.percache_qkv_norm_rope(self.ctx, qkv.data_ptr(), qkv.stride(0) if n > 1 else F, n, pos.data_ptr(), pos.shape[0],
+                                             None if axis is None else axis.ctypes.data, _ptr(qkv_bias), _ptr(q_norm), _ptr(k_norm), eps, outs[0].data_ptr(),
+                                             outs[1].data_ptr(), outs[2].data_ptr(), self._raw_stream())
+        self._check(st)
+        return tuple(outs)
+
+    def percache_attention_packed(self, layer, q, k, v, start, slot_ids=None, used_len=None, n_chunks=None, n_splits: int = 0, attn_out=None, lse_out=None):
+        """(attn_out [N, Hq * D], lse [Hq, N] or None) of packed rows q [Hq, N, D], k, v [Hkv, N, D]; start: the requests' first rows and the end of the
+        last one.  lse_out: a float32 tensor, True for a new one, None for none.  Rows of no request are left as they are (new tensors: unset)."""
+        import torch
+        bf16 = torch.bfloat16
+        c = self.cfg
+        Hq, Hkv, D = c.n_q_heads, c.n_kv_heads, c.head_dim
+        n = q.shape[1]
+        self._want("q", q, (Hq, n, D), bf16)
+        self._want("k", k, (Hkv, n, D), bf16)
+        self._want("v", v, (Hkv, n, D), bf16)
+        start, start_p = _i32_list(start)
+        n_seq = start.size - 1
+        if n_seq < 1:
+            raise ValueError("start: the first row of every request and the end of the last one are wanted")
+        keep, ids_p, ul_p, nc_p, max_chunks = self._draft_chunks(n_seq, slot_ids, used_len, n_chunks)
+        if attn_out is None:
+            attn_out = torch.empty((n, Hq * D), dtype=bf16, device=self.device)
+        else:
+            self._want("attn_out", attn_out, (n, Hq * D), bf16)
+        if lse_out is True:
+            lse_out = torch.empty((Hq, n), dtype=torch.float32, device=self.device)
+        else:
+            self._want("lse_out", lse_out, (Hq, n), torch.float32)
+        stream = self._raw_stream()
+        key = ("packed", n_seq, n, max_chunks)
+        need = self._draft_bytes.get(key)
+        if need is None:
+            need = self._draft_bytes[key] = self.lib.percache_packed_workspace_bytes(self.ctx, n_seq, n, max_chunks)
+        st = self.lib.percache_attention_packed(self.ctx, layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), n, start_p, n_seq, ids_p, ul_p, nc_p, max_chunks, n_splits,
+                                                attn_out.data_ptr(), _ptr(lse_out), self._draft_workspace(need, stream), need, stream)
+        self._check(st)
+        return attn_out, lse_out
+
+    # ------------------------------------------------------------------ several continuations of a prompt
+    def percache_kv_fork(self, src_slots, dst_slots, n_tokens=None, layer0: int = 0, n_layers=None):
+        """Slot dst_slots[i] becomes a copy of the first n_tokens[i] tokens (None: all) of slot src_slots[i], in every layer or n_layers from layer0 on."""
+        src, src_p = _i32_list(src_slots)
+        dst, dst_p = _i32_list(dst_slots, (src.size,))
+        nt, nt_p = _i32_list(n_tokens, (src.size,))
+        self._check(self.lib.percache_kv_fork(self.ctx, layer0, self.cfg.n_layers - layer0 if n_layers is None else n_layers, src_p, dst_p, nt_p, src.size,
+                                              self._raw_stream()))
+
+    def percache_beam_select(self, logits, scores, best: int):
+        """(parent, token, score), each [B, best], of logits [B, beams, vocab] (bf16 or float32, dense rows, beams evenly strided) and scores [B, beams]."""
+        import torch
+        if logits.dim() != 3 or logits.dtype not in (torch.bfloat16, torch.float32) or not logits.is_cuda or logits.stride(2) != 1:
+            raise ValueError(f"logits: a bfloat16 or float32 tensor [B, beams, vocab] on the GPU with dense rows is wanted, got {logits.dtype} {tuple(logits.shape)}")
+        batch, beams, vocab = logits.shape
+        stride = logits.stride(1) if beams > 1 else logits.stride(0) if batch > 1 else vocab
+        if batch > 1 and beams > 1 and logits.stride(0) != beams * stride:
+            raise ValueError(f"logits: rows at an even distance are wanted, got strides {logits.stride()}")
+        self._want("scores", scores, (batch, beams), torch.float32)
+        parent = torch.empty((batch, best), dtype=torch.int32, device=self.device)
+        token = torch.empty((batch, best), dtype=torch.int32, device=self.device)
+        score = torch.empty((batch, best), dtype=torch.float32, device=self.device)
+        stream = self._raw_stream()
+        key = ("beams", batch, beams, vocab, best)
+        need = self._draft_bytes.get(key)
+        if need is None:
+            need = self._draft_bytes[key] = self.lib.percache_beam_select_workspace_bytes(self.ctx, batch, beams, vocab, best)
+        st = self.lib.percache_beam_select(self.ctx, logits.data_ptr(), int(logits.dtype == torch.float32), stride, scores.data_ptr(), batch, beams, vocab, best,
+                                           parent.data_ptr(), token.data_ptr(), score.data_ptr(), self._draft_workspace(need, stream), need, stream)
+        self._check(st)
+        return parent, token, score
 
     # ------------------------------------------------------------------ stack of layers on the retained rows
     def percache_stack_workspace_bytes(self, batch, t_fresh, max_chunks, ffn) -> int:

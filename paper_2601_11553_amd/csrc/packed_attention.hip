@@ -1,0 +1,1104 @@
+// Attention of packed rows: request s has T_s fresh rows, one request behind the other, and attends over [its cached chunks ; its own rows up to each]:
+//   o_i = sum_j e^(s_ij - lse_i) v_j,   s_ij = q_i.k_j / sqrt(D),   lse_i = log sum_j e^s_ij.
+// The arithmetic is that of reuse_attention.hip (transposed scores, bf16 matrix instructions, fp32 softmax state against a lazily refreshed reference
+// exponent); what differs is how the work is cut and where the fresh keys come from:
+//   - the host cuts every request into blocks of rows and, where the launch would be short of workgroups, the blocks' keys into partitions, and lists
+//     them longest first.  A workgroup reads its item from the list; a call of prompts of any lengths and of single tokens is one launch.
+//   - the G query heads of a kv head are stacked token by token (row = i G + g), so a block of 256 rows spans 256 / G tokens, all its wavefronts see
+//     nearly the same keys, and a token's heads share the rows of a tile;
+//   - a fresh tile is taken as it was projected, K and V row by row; V is turned by the LDS transpose reads on its way to the matrix instruction, so
+//     there is no launch that lays it out first, and no workspace for it.
+// Blocks of up to 32 rows (single tokens, short questions) share a tile by keys instead of rows: eight wavefronts, two tiles, 16 keys each.
+//
+// What a row does not see takes no part, whatever stands there: K by the mask on the scores; V behind the end of a chunk or a request by clearing the
+// operand; V of a later token of the same tile, where it is not finite, by computing the rows that it made NaN once more, key by key.
+#include <algorithm>
+
+#include "decode_common.hpp"
+
+namespace {
+using pc::bf16x4;
+using pc::bf16x8;
+using pc::f32x16;
+using pc::f32x4;
+using pc::kKvTile;
+using pc::u32x4;
+using pc::dec::codes4;
+using pc::dec::codes8;
+using pc::dec::fast_exp2;
+using pc::dec::row_max;
+using pc::dec::row_sum;
+
+constexpr int TK = kKvTile, NW = 8;
+constexpr int kWide = 0, kNarrow = 1;      // kinds of items
+constexpr int kWideRows = 256, kNarrowRows = 32;
+constexpr float kSumLimit = 32.f * 256.f;  // 32 probabilities of a lane and tile, each at most 2^8 against the reference
+constexpr float kSumLimit4 = 4.f * 256.f;  // 4 of them
+constexpr int kMaxPackedSplits = 64;
+constexpr int kMoreItems = 16;             // items beyond one a block, per CU
+
+// A workgroup's work, for every kv head: rows [r_first, r_first + rows) of a request (stacked) over n_cached cached tiles from tile tile0 of chunk entry
+// ent on, then over the fresh tiles [f0, f1).
+struct Item {
+  int32_t row0, T, r_first, rows, kind, n_cached, ent, n_ents, tile0, f0, f1;
+  int32_t part;   // first row of its partial results, -1: it is the block's only partition
+};
+constexpr int kItemWords = sizeof(Item) / 4;
+struct Merge { int32_t row0, r_first, rows, part, n; };   // partition p of the block has its partial rows from part + p * rows on
+constexpr int kMergeWords = sizeof(Merge) / 4;
+
+struct Args {
+  const __bf16 *q, *k, *v;   // [heads][N][D]
+  const __bf16 *k16, *v16;
+  const uint8_t *k8, *v8;
+  const float *k_scale, *v_scale;
+  const int32_t *words;      // items, merges, chunk entries (slot, used length > 0)
+  __bf16 *out;               // [N][Hq * D]
+  float *lse;                // [Hq][N] or null
+  float *part_o, *part_ml;   // [part_rows of every kv head][D], [...][2]
+  long N, part_rows;
+  int n_items, ents_at, Hq, Hkv, C, n_slots16;
+  float scale_log2e;
+};
+
+// A stage of LDS: a K tile [64][D], rows swizzled by 16-byte chunks, then V: a block [D][64] of the store or, fresh, rows [64][D].
+template <int D>
+struct Lds {
+  static constexpr int K_ROW = D * 2, VB_ROW = TK * 2;
+  static constexpr int HALF = TK * D * 2, STAGE = 2 * HALF, NSTAGE = 4;
+  static constexpr int O_ROW = D + 4;                                                        // narrow: floats per output row of a wavefront
+  static constexpr int MERGE = NW * kNarrowRows * (O_ROW + 2) * 4;
+  static constexpr int BYTES = NSTAGE * STAGE > MERGE ? NSTAGE * STAGE : MERGE;
+};
+__device__ __forceinline__ int swz(int row_bytes, int row) { return row_bytes == 256 ? (row & 15) : row_bytes == 128 ? ((row >> 1) & 7) : ((row >> 2) & 3); }
+// fresh V rows: pairs of chunks stay together, so that the four rows of a transpose read lie in different banks
+__device__ __forceinline__ int swz_tr(int row_bytes, int row) { return row_bytes == 256 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
+
+#define PC_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 0xf) | (7 << 4) | (15 << 8) | ((((n) >> 4) & 3) << 14))
+
+__device__ __forceinline__ float pair_max(float x) { return fmaxf(x, __shfl_xor(x, 32, 64)); }
+__device__ __forceinline__ float pair_sum(float x) { return x + __shfl_xor(x, 32, 64); }
+
+__device__ __forceinline__ bf16x8 codes16(unsigned w0, unsigned w1, float scale) { return codes8(make_uint2(w0, w1), scale); }
+
+// four keys of one head-dim index for every lane, from four rows of 16 lanes' 4 x 16 elements (lane i of 16 names row i / 4, elements 4 (i % 4) .. +3,
+// and gets element i of the four rows)
+__device__ __forceinline__ bf16x4 read_turned(const char *p) {
+  typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p));
+}
+// what is left of four bf16 numbers when only the first `left` stay
+__device__ __forceinline__ uint2 keep_first(int left) {
+  return make_uint2((left > 0 ? 0xffffu : 0u) | (left > 1 ? 0xffff0000u : 0u), (left > 2 ? 0xffffu : 0u) | (left > 3 ? 0xffff0000u : 0u));
+}
+__device__ __forceinline__ bf16x4 cleared(bf16x4 v, uint2 keep) {
+  const uint2 w = __builtin_bit_cast(uint2, v);
+  return __builtin_bit_cast(bf16x4, make_uint2(w.x & keep.x, w.y & keep.y));
+}
+__device__ __forceinline__ bf16x8 cleared(bf16x8 v, uint2 lo, uint2 hi) {
+  const u32x4 w = __builtin_bit_cast(u32x4, v);
+  return __builtin_bit_cast(bf16x8, (u32x4){w[0] & lo.x, w[1] & lo.y, w[2] & hi.x, w[3] & hi.y});
+}
+// acc + 0 * v: NaN if one of them is not finite
+__device__ __forceinline__ float taint(unsigned two, float acc) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), bf16x2{(__bf16)0.f, (__bf16)0.f}, acc, false);
+}
+
+struct Tile { const char *k, *v; int valid, t0; bool is8; float ks, vs; };   // t0: first fresh token, -1 for a cached tile
+
+// The walk over an item's tiles; every wavefront steps its own, in scalar registers.  Lane c keeps (slot, used length) of entry c of the 64 at hand.
+template <int D, bool KV8>
+struct Walk {
+  const Args &a;
+  const Item &it;
+  int gkv, lane, my_slot = 0, my_used = 0, ent = 0, left = 0, at = 0, idx = 0;
+  const char *ck = nullptr, *cv = nullptr;
+  bool c8 = false;
+  size_t sc = 0;
+  __device__ __forceinline__ Walk(const Args &a_, const Item &it_, int gkv_, int lane_) : a(a_), it(it_), gkv(gkv_), lane(lane_) {
+    load();
+    if (it.n_cached > 0) {
+      enter();
+      skip(it.tile0);
+    }
+  }
+  __device__ __forceinline__ void load() {   // the 64 entries from ent on
+    my_slot = my_used = 0;
+    if (ent + lane < it.n_ents) {
+      const int2 e = *(const int2 *)(a.words + a.ents_at + 2 * (it.ent + ent + lane));
+      my_slot = e.x;
+      my_used = e.y;
+    }
+  }
+  __device__ __forceinline__ void enter() {
+    const int slot = __builtin_amdgcn_readlane(my_slot, ent & 63);
+    left = __builtin_amdgcn_readlane(my_used, ent & 63);
+    at = 0;
+    c8 = KV8 && slot >= a.n_slots16;
+    const size_t sh = (size_t)(c8 ? slot - a.n_slots16 : slot) * a.Hkv + gkv, base = sh * a.C * D;
+    ck = c8 ? (const char *)a.k8 + base : (const char *)a.k16 + base * 2;
+    cv = c8 ? (const char *)a.v8 + base : (const char *)a.v16 + base * 2;
+    sc = sh * (a.C / TK);
+  }
+  __device__ __forceinline__ void skip(int n) {
+    const size_t bytes = (size_t)n * TK * D * (c8 ? 1 : 2);
+    ck += bytes;
+    cv += bytes;
+    at += n;
+    left -= n * TK;
+  }
+  __device__ __forceinline__ int n() const { return it.n_cached + it.f1 - it.f0; }
+  __device__ __forceinline__ Tile next() {
+    Tile t;
+    t.ks = t.vs = 1.f;
+    if (idx < it.n_cached) {
+      t.k = ck;
+      t.v = cv;
+      t.valid = min(TK, left);
+      t.t0 = -1;
+      t.is8 = c8;
+      if (KV8 && c8) {
+        t.ks = a.k_scale[sc + at];
+        t.vs = a.v_scale[sc + at];
+      }
+      skip(1);
+      if (left <= 0 && idx + 1 < it.n_cached) {
+        ++ent;
+        if ((ent & 63) == 0) load();
+        enter();
+      }
+    } else {
+      const int f = it.f0 + idx - it.n_cached;
+      const size_t at_row = ((size_t)gkv * a.N + it.row0 + (size_t)f * TK) * (D * 2);
+      t.k = (const char *)a.k + at_row;
+      t.v = (const char *)a.v + at_row;
+      t.valid = min(TK, it.T - f * TK);
+      t.t0 = f * TK;
+      t.is8 = false;
+    }
+    ++idx;
+    return t;
+  }
+};
+
+// One row of an item once more, key by key, by one wavefront: what the row does not see is not touched.  Rows that need it are those of a tile in which a
+// later token's V is not finite.
+template <int D, bool KV8>
+__device__ __forceinline__ void redo_row(const Args &a, const Item &it, int gkv, int lane, int local, float &m_out, float &l_out, float (&o)[D / 64]) {
+  constexpr int E = D / 64;
+  const int G = a.Hq / a.Hkv, r = it.r_first + local, i = r / G, head = gkv * G + r % G;
+  float q[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    q[e] = (float)a.q[((size_t)head * a.N + it.row0 + i) * D + e * 64 + lane];
+    o[e] = 0.f;
+  }
+  float m = -INFINITY, l = 0.f;
+  Walk<D, KV8> walk(a, it, gkv, lane);
+  for (int t = 0; t < walk.n(); ++t) {
+    const Tile x = walk.next();
+    const int n = x.t0 < 0 ? x.valid : min(x.valid, i - x.t0 + 1);
+    for (int key = 0; key < n; ++key) {
+      float kx[E], vx[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int d = e * 64 + lane;
+        if (KV8 && x.is8) {
+          kx[e] = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)x.k)[key * D + d], 0) * x.ks;
+          vx[e] = __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t *)x.v)[d * TK + pc::blocked_pos8(key)], 0) * x.vs;
+        } else {
+          kx[e] = (float)((const __bf16 *)x.k)[key * D + d];
+          vx[e] = (float)((const __bf16 *)x.v)[x.t0 < 0 ? d * TK + (key & ~15) + pc::blocked_key(key & 15) : key * D + d];
+        }
+      }
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += q[e] * kx[e];
+      s = pc::dec::wave_sum(s) * a.scale_log2e;
+      const float top = fmaxf(m, s), w = m == -INFINITY ? 0.f : fast_exp2(m - top), p = s == -INFINITY ? 0.f : fast_exp2(s - top);
+      m = top;
+      l = l * w + p;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] = o[e] * w + p * vx[e];
+    }
+  }
+  m_out = m;
+  l_out = l;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] *= inv;
+}
+template <int D, bool KV8>
+__device__ __forceinline__ void redo_and_write(const Args &a, const Item &it, int gkv, int lane, int local) {
+  float m, l, o[D / 64];
+  redo_row<D, KV8>(a, it, gkv, lane, local, m, l, o);
+  const int G = a.Hq / a.Hkv, r = it.r_first + local, i = r / G, head = gkv * G + r % G;
+  if (it.part < 0) {
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) a.out[((size_t)it.row0 + i) * ((size_t)a.Hq * D) + (size_t)head * D + e * 64 + lane] = (__bf16)o[e];
+    if (a.lse && lane == 0) a.lse[(size_t)head * a.N + it.row0 + i] = pc::lse_of(m, l);
+  } else {
+    const size_t prow = (size_t)gkv * a.part_rows + it.part + local;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) a.part_o[prow * D + e * 64 + lane] = o[e];
+    if (lane == 0) *(float2 *)(a.part_ml + prow * 2) = make_float2(m, l);
+  }
+}
+
+// ---- up to 256 rows: a wavefront 32 of them, all wavefronts every tile
+template <int D, bool KV8>
+__device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv, char *lds) {
+  using L = Lds<D>;
+  constexpr int NLD = 4, NSTAGE = 3, KS = D / 16, DB = D / 32, INSTR = L::HALF / 1024 / NLD;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g2 = lane >> 5;
+  const int G = a.Hq / a.Hkv;
+
+  const int local = wave * 32 + l32;
+  const bool row_ok = local < it.rows;
+  const int r = it.r_first + min(local, it.rows - 1), my_i = r / G, head = gkv * G + r - my_i * G;
+  // first and last token among this wavefront's rows: a fresh tile that reaches past the first is masked, one that starts behind the last skipped
+  const bool wave_live = wave * 32 < it.rows;
+  const int i_lo = (it.r_first + wave * 32) / G, i_hi = (it.r_first + min(wave * 32 + 32, it.rows) - 1) / G;
+
+  bf16x8 qf[KS];
+  {
+    const __bf16 *qrow = a.q + ((size_t)head * a.N + it.row0 + my_i) * D;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *(const bf16x8 *)(qrow + ks * 16 + g2 * 8);
+  }
+  f32x16 o_acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) o_acc[db][x] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f, tainted = 0.f;
+  bool all_started = false;
+
+  Walk<D, KV8> walk(a, it, gkv, lane);
+  const int n = walk.n();
+
+  // ---- requests: wavefronts 0..3 bring in a bf16 tile, instruction i of a half its bytes [1024 i, +1024)
+  unsigned k_off[INSTR], vb_off[INSTR], vf_off[INSTR];
+#pragma unroll
+  for (int j = 0; j < INSTR; ++j) {
+    const int byte = ((wave & (NLD - 1)) + j * NLD) * 1024 + lane * 16;
+    const int row = byte / L::K_ROW, pc = byte % L::K_ROW / 16, d = byte / L::VB_ROW, pd = byte % L::VB_ROW / 16;
+    k_off[j] = row * L::K_ROW + (pc ^ swz(L::K_ROW, row)) * 16;
+    vf_off[j] = row * L::K_ROW + (pc ^ swz_tr(L::K_ROW, row)) * 16;
+    vb_off[j] = d * L::VB_ROW + (pd ^ swz(L::VB_ROW, d)) * 16;
+  }
+  auto request = [&](const Tile &t, int st) __attribute__((always_inline)) {
+    char *kb = lds + st * L::STAGE;
+    const bool ragged = t.valid < TK;   // rows past the end repeat the last valid one (masked later); a block of the store is there as a whole
+#pragma unroll
+    for (int j = 0; j < INSTR; ++j) {
+      unsigned ko = k_off[j];
+      if (__builtin_expect(ragged, 0)) ko = min((int)(ko / L::K_ROW), t.valid - 1) * L::K_ROW + ko % L::K_ROW;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(t.k + ko),
+                                       (__attribute__((address_space(3))) void *)(kb + ((wave & (NLD - 1)) + j * NLD) * 1024), 16, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < INSTR; ++j) {
+      unsigned vo = t.t0 < 0 ? vb_off[j] : vf_off[j];
+      if (__builtin_expect(ragged, 0)) {
+        if (t.t0 >= 0) vo = min((int)(vo / L::K_ROW), t.valid - 1) * L::K_ROW + vo % L::K_ROW;
+      }
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(t.v + vo),
+                                       (__attribute__((address_space(3))) void *)(kb + L::HALF + ((wave & (NLD - 1)) + j * NLD) * 1024), 16, 0, 0);
+    }
+  };
+  // 8-bit tiles: codes through registers, 16 of K and of V a thread (D = 64: of the first half of the threads), turned into a bf16 tile one tile
+  // ahead of the arithmetic.  The stores are ones that the compiler does not see, for which it would wait for every request in flight.
+  constexpr bool ALL = TK * D / 16 == 64 * NW;
+  const bool conv = KV8 && (ALL || tid < TK * D / 16);
+  const int ck_row = tid * 16 / D, ck_c = tid * 16 % D / 16, cv_row = tid >> 2, cv_m = tid & 3;
+  u32x4 kc = {0, 0, 0, 0}, vc = {0, 0, 0, 0};
+  auto load_codes = [&](const Tile &t) __attribute__((always_inline)) {
+    if (!conv) return;
+    kc = *(const u32x4 *)(t.k + min(ck_row, t.valid - 1) * D + ck_c * 16);
+    vc = *(const u32x4 *)(t.v + cv_row * TK + cv_m * 16);
+  };
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
+  auto store16 = [&](int off, bf16x8 x) __attribute__((always_inline)) {
+    const unsigned addr = lds_base + (unsigned)off;
+    asm volatile("ds_write_b128 %0, %1" : : "v"(addr), "v"(x) : "memory");
+  };
+  auto land_codes = [&](const Tile &t, int st) __attribute__((always_inline)) {
+    if (!conv) return;
+    const int kb = st * L::STAGE + ck_row * L::K_ROW, vb = st * L::STAGE + L::HALF + cv_row * L::VB_ROW, sk = swz(L::K_ROW, ck_row), sv = swz(L::VB_ROW, cv_row);
+    store16(kb + ((2 * ck_c) ^ sk) * 16, codes16(kc[0], kc[1], t.ks));
+    store16(kb + ((2 * ck_c + 1) ^ sk) * 16, codes16(kc[2], kc[3], t.ks));
+    // (bytes 32 J + 16 a + .. of a row of codes: its first 8 are the keys of bf16 chunk 4 J + a, its last 8 those of chunk 4 J + 2 + a)
+    store16(vb + ((4 * (cv_m >> 1) + (cv_m & 1)) ^ sv) * 16, codes16(vc[0], vc[1], t.vs));
+    store16(vb + ((4 * (cv_m >> 1) + 2 + (cv_m & 1)) ^ sv) * 16, codes16(vc[2], vc[3], t.vs));
+  };
+
+  int k_rd[KS], vb_rd[4], vf_rd[DB];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) k_rd[ks] = ((2 * ks + g2) ^ swz(L::K_ROW, l32)) * 16 + l32 * L::K_ROW;
+#pragma unroll
+  for (int c4 = 0; c4 < 4; ++c4) vb_rd[c4] = ((2 * c4 + g2) ^ swz(L::VB_ROW, l32)) * 16 + l32 * L::VB_ROW;
+  {
+    const int key = 4 * g2 + ((l32 & 15) >> 2);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) vf_rd[db] = key * L::K_ROW + ((db * 4 + (l32 >> 4) * 2 + ((l32 >> 1) & 1)) ^ swz_tr(L::K_ROW, key)) * 16 + (l32 & 1) * 8;
+  }
+
+  auto tile = [&](int st, const Tile &t, auto fresh_c) __attribute__((always_inline)) {
+    constexpr bool FRESH = decltype(fresh_c)::value;
+    const char *kb = lds + st * L::STAGE, *vb = kb + L::HALF;
+    f32x16 s_acc[2];
+#pragma unroll
+    for (int kbk = 0; kbk < 2; ++kbk)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s_acc[kbk][x] = 0.f;
+#pragma unroll
+    for (int h = 0; h < KS / 4; ++h) {
+      bf16x8 kop[2][4];
+#pragma unroll
+      for (int k4 = 0; k4 < 4; ++k4)
+#pragma unroll
+        for (int kbk = 0; kbk < 2; ++kbk) kop[kbk][k4] = *(const bf16x8 *)(kb + kbk * 32 * L::K_ROW + k_rd[4 * h + k4]);
+#pragma unroll
+      for (int k4 = 0; k4 < 4; ++k4)
+#pragma unroll
+        for (int kbk = 0; kbk < 2; ++kbk) s_acc[kbk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop[kbk][k4], qf[4 * h + k4], s_acc[kbk], 0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+    }
+    // V operands of 16 keys: of the first 32-key block now, so that their latency runs under the softmax
+    bf16x8 vop[2][DB][2];
+    auto v_operands = [&](int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const int c4 = 2 * half + c2;
+          if constexpr (FRESH) {
+            union { bf16x4 p[2]; bf16x8 v; } u;
+            u.p[0] = read_turned(vb + 16 * c4 * L::K_ROW + vf_rd[db]);
+            u.p[1] = read_turned(vb + (16 * c4 + 8) * L::K_ROW + vf_rd[db]);
+            vop[half][db][c2] = u.v;
+          } else {
+            vop[half][db][c2] = *(const bf16x8 *)(vb + db * 32 * L::VB_ROW + vb_rd[c4]);
+          }
+        }
+    };
+    v_operands(0);
+    const bool ragged = t.valid < TK, causal = FRESH && t.t0 + TK - 1 > i_lo;
+    if (__builtin_expect(ragged || causal, 0)) {
+      int t_lane = g2 * 4;
+      asm volatile("" : "+v"(t_lane));   // (keeps the per-element key indices out of loop-invariant registers)
+      const int lim = min(t.valid - 1, FRESH ? my_i - t.t0 : TK) - t_lane;
+#pragma unroll
+      for (int kbk = 0; kbk < 2; ++kbk)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) s_acc[kbk][x] = kbk * 32 + (x >> 2) * 8 + (x & 3) <= lim ? s_acc[kbk][x] : -INFINITY;
+    }
+    bf16x8 pf[2][2];
+    auto exponentials = [&](float neg_m) __attribute__((always_inline)) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      float sum = 0.f, sum2 = 0.f;
+#pragma unroll
+      for (int kbk = 0; kbk < 2; ++kbk)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) {
+            const float p0 = fast_exp2(__builtin_fmaf(s_acc[kbk][j * 8 + e], a.scale_log2e, neg_m));
+            const float p1 = fast_exp2(__builtin_fmaf(s_acc[kbk][j * 8 + e + 1], a.scale_log2e, neg_m));
+            const bf16x2 pr = {(__bf16)p0, (__bf16)p1};
+            pf[kbk][j][e] = pr[0];
+            pf[kbk][j][e + 1] = pr[1];
+            sum += p0;
+            sum2 += p1;
+          }
+      return sum + sum2;
+    };
+    float psum = 0.f;
+    bool refresh = !all_started;
+    if (__builtin_expect(!refresh, 1)) {
+      psum = exponentials(-m_ref);
+      refresh = __builtin_amdgcn_ballot_w64(!(psum <= kSumLimit)) != 0;   // also catches inf / nan
+    }
+    if (__builtin_expect(refresh, 0)) {
+      float mx = s_acc[0][0];
+#pragma unroll
+      for (int kbk = 0; kbk < 2; ++kbk)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) mx = fmaxf(mx, s_acc[kbk][x]);
+      const float mc = pair_max(mx) * a.scale_log2e;
+      const bool upd = mc > m_ref;
+      const float alpha = upd ? fast_exp2(m_ref - mc) : 1.0f;
+      m_ref = upd ? mc : m_ref;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o_acc[db][x] *= alpha;
+      psum = exponentials(m_ref == -INFINITY ? 0.f : -m_ref);
+      all_started = __builtin_amdgcn_ballot_w64(m_ref == -INFINITY) == 0;
+    }
+    l_run += psum;
+    v_operands(1);
+    if (__builtin_expect(ragged || causal, 0)) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int c2 = 0; c2 < 2; ++c2) {
+          const int left = t.valid - (16 * (2 * half + c2) + 4 * g2);
+          const uint2 lo = keep_first(left), hi = keep_first(left - 8);
+#pragma unroll
+          for (int db = 0; db < DB; ++db) {
+            vop[half][db][c2] = cleared(vop[half][db][c2], lo, hi);
+            if (FRESH) {
+              const u32x4 w = __builtin_bit_cast(u32x4, vop[half][db][c2]);
+              tainted = taint(w[0], taint(w[1], taint(w[2], taint(w[3], tainted))));
+            }
+          }
+        }
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o_acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop[half][db][c2], pf[half][c2], o_acc[db], 0, 0, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, (FRESH ? 4 : 2) * DB, 1);
+    __builtin_amdgcn_sched_group_barrier(0x008, 4 * DB, 1);
+  };
+
+  // ---- pipeline: tile t is computed from stage t % 3 while tiles t+1 and t+2 are on their way.  At the end of iteration t every wavefront waits for
+  // what it has in flight (its share of tile t+1; codes of t+1, which it then turns into their stage), and tile t+2 is requested into the stage
+  // that iteration t-1 read; the barrier publishes tile t+1.
+  Tile cur = {}, nxt = {}, aft = {};
+  auto bring = [&](Tile &t, int st) __attribute__((always_inline)) {
+    t = walk.next();
+    if (KV8 && t.is8) load_codes(t);
+    else if (wave < NLD) request(t, st);
+  };
+  bring(cur, 0);
+  if (KV8 && cur.is8) land_codes(cur, 0);
+  if (n > 1) bring(nxt, 1);
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
+  __builtin_amdgcn_s_waitcnt(0);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  int st = 0;
+  for (int t = 0; t < n; ++t) {
+    const int s1 = st + 1 == NSTAGE ? 0 : st + 1, s2 = s1 + 1 == NSTAGE ? 0 : s1 + 1;
+    if (wave_live) {
+      if (cur.t0 < 0) tile(st, cur, std::false_type{});
+      else if (cur.t0 <= i_hi) tile(st, cur, std::true_type{});
+    }
+    PC_WAIT_VMCNT(0);
+    if (KV8 && t + 1 < n && nxt.is8) {
+      land_codes(nxt, s1);
+      __builtin_amdgcn_s_waitcnt(0xc07f);   // (lgkmcnt 0)
+    }
+    if (t + 2 < n) bring(aft, s2);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    cur = nxt;
+    nxt = aft;
+    st = s1;
+  }
+  if (!wave_live) return;
+
+  const float l_tot = pair_sum(l_run), inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
+  unsigned again = 0;   // rows whose sums a later token's V has spoilt
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(tainted == 0.f)) != 0, 0)) {
+    float bad = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) bad += o_acc[db][x] * 0.f;
+    const unsigned long long b = __builtin_amdgcn_ballot_w64(row_ok && !(bad == 0.f));
+    again = (unsigned)b | (unsigned)(b >> 32);
+  }
+  if (row_ok && !(again >> l32 & 1)) {
+    if (it.part < 0) {
+      __bf16 *orow = a.out + ((size_t)it.row0 + my_i) * ((size_t)a.Hq * D) + (size_t)head * D;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *(bf16x4 *)(orow + db * 32 + q4 * 8 + g2 * 4) = bf16x4{(__bf16)(o_acc[db][q4 * 4] * inv), (__bf16)(o_acc[db][q4 * 4 + 1] * inv),
+                                                                 (__bf16)(o_acc[db][q4 * 4 + 2] * inv), (__bf16)(o_acc[db][q4 * 4 + 3] * inv)};
+      if (a.lse && g2 == 0) a.lse[(size_t)head * a.N + it.row0 + my_i] = pc::lse_of(m_ref, l_tot);
+    } else {
+      const size_t prow = (size_t)gkv * a.part_rows + it.part + local;
+      float *po = a.part_o + prow * D;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          *(f32x4 *)(po + db * 32 + q4 * 8 + g2 * 4) = f32x4{o_acc[db][q4 * 4] * inv, o_acc[db][q4 * 4 + 1] * inv, o_acc[db][q4 * 4 + 2] * inv, o_acc[db][q4 * 4 + 3] * inv};
+      if (g2 == 0) *(float2 *)(a.part_ml + prow * 2) = make_float2(m_ref, l_tot);
+    }
+  }
+  while (again) {
+    const int x = __builtin_ctz(again);
+    again &= again - 1;
+    redo_and_write<D, KV8>(a, it, gkv, lane, wave * 32 + x);
+  }
+}
+
+// ---- up to 16 NR rows: two tiles at a time, wavefronts 0..3 share the first by keys, 4..7 the second; each has its own running maximum, sum and output
+template <int D, bool KV8, int NR>
+__device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int gkv, char *lds) {
+  using L = Lds<D>;
+  constexpr int KS = D / 32, DB = D / 16, I16 = L::HALF / 1024 / 4, I8 = I16 / 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
+  const int odd = wave >> 2, kq = wave & 3, G = a.Hq / a.Hkv;
+
+  int my_i[NR];
+  bf16x8 q[NR][KS];
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    const int r = it.r_first + min(x * 16 + l16, it.rows - 1);
+    my_i[x] = r / G;
+    const __bf16 *p = a.q + ((size_t)(gkv * G + r - my_i[x] * G) * a.N + it.row0 + my_i[x]) * D + g * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) q[x][ks] = *(const bf16x8 *)(p + ks * 32);
+  }
+  const int i_lo = it.r_first / G;
+  f32x4 o[DB][NR];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < NR; ++x) o[db][x] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m_ref[NR], l_run[NR], tainted = 0.f;
+#pragma unroll
+  for (int x = 0; x < NR; ++x) { m_ref[x] = -INFINITY; l_run[x] = 0.f; }
+
+  Walk<D, KV8> walk(a, it, gkv, lane);
+  const int n = walk.n(), pairs = (n + 1) / 2;
+
+  // requests: four wavefronts a tile; 8-bit tiles stay codes (K rows of D bytes, V rows of 64)
+  auto half = [&](const char *src, char *dst, auto row_bytes_c, int instr, int last_row, bool turned) __attribute__((always_inline)) {
+    constexpr int RB = decltype(row_bytes_c)::value;
+#pragma unroll
+    for (int j = 0; j < I16; ++j) {
+      if (j >= instr) break;
+      const int byte = (kq + j * 4) * 1024 + lane * 16, row = byte / RB, pc = byte % RB / 16;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void *)(src + (unsigned)(min(row, last_row) * RB + (pc ^ (turned ? swz_tr(RB, row) : swz(RB, row))) * 16)),
+          (__attribute__((address_space(3))) void *)(dst + (kq + j * 4) * 1024), 16, 0, 2);
+    }
+  };
+  auto request = [&](const Tile &t, int st) __attribute__((always_inline)) {
+    char *dst = lds + st * L::STAGE;
+    if (KV8 && t.is8) {
+      half(t.k, dst, std::integral_constant<int, D>{}, I8, t.valid - 1, false);
+      half(t.v, dst + L::HALF / 2, std::integral_constant<int, TK>{}, I8, D - 1, false);
+    } else {
+      half(t.k, dst, std::integral_constant<int, D * 2>{}, I16, t.valid - 1, false);
+      if (t.t0 < 0) half(t.v, dst + L::HALF, std::integral_constant<int, TK * 2>{}, I16, D - 1, false);
+      else half(t.v, dst + L::HALF, std::integral_constant<int, D * 2>{}, I16, t.valid - 1, true);
+    }
+  };
+  // this wavefront's tile of the next pair; valid 0: there is none
+  auto bring = [&](int pair) __attribute__((always_inline)) {
+    Tile t = {}, u;
+    t.valid = 0;
+    if (2 * pair < n) {
+      u = walk.next();
+      if (!odd) t = u;
+    }
+    if (2 * pair + 1 < n) {
+      u = walk.next();
+      if (odd) t = u;
+    }
+    if (t.valid > 0) request(t, 2 * (pair & 1) + odd);
+    return t;
+  };
+
+  auto soften = [&](f32x4 &s, int x) __attribute__((always_inline)) {
+    f32x4 p;
+    auto exponentials = [&](float neg_m) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = fast_exp2(__builtin_fmaf(s[e], a.scale_log2e, neg_m));
+      return (p[0] + p[1]) + (p[2] + p[3]);
+    };
+    float sum = 0.f;
+    bool refresh = __builtin_amdgcn_ballot_w64(m_ref[x] == -INFINITY) != 0;
+    if (!refresh) {
+      sum = exponentials(-m_ref[x]);
+      refresh = __builtin_amdgcn_ballot_w64(!(sum <= kSumLimit4)) != 0;
+    }
+    if (refresh) {
+      const float mc = row_max(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]))) * a.scale_log2e;
+      const bool upd = mc > m_ref[x];
+      const float alpha = upd ? fast_exp2(m_ref[x] - mc) : 1.0f;
+      m_ref[x] = upd ? mc : m_ref[x];
+      l_run[x] *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db][x] *= alpha;
+      sum = exponentials(m_ref[x] == -INFINITY ? 0.f : -m_ref[x]);
+    }
+    l_run[x] += sum;
+    return p;
+  };
+
+  const int k_row = kq * 16 + l16;
+  auto compute = [&](int st, const Tile &t) __attribute__((always_inline)) {
+    if (kq * 16 >= t.valid) return;
+    const char *kb = lds + st * L::STAGE;
+    f32x4 s[NR];
+#pragma unroll
+    for (int x = 0; x < NR; ++x) s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+    bf16x4 vop[DB];
+    if (KV8 && t.is8) {
+      const char *vb = kb + L::HALF / 2;
+      uint2 raw[KS];
+      unsigned vraw[DB];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) raw[ks] = *(const uint2 *)(kb + k_row * D + (((2 * ks + (g >> 1)) ^ swz(D, k_row)) * 16) + (g & 1) * 8);
+      // byte p = 32 J + 16 a + 8 j + 4 c + e of a V row holds key 32 J + 16 j + 8 c + 4 a + e
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const int row = db * 16 + l16;
+        vraw[db] = *(const unsigned *)(vb + row * TK + (((2 * (kq >> 1) + (g & 1)) ^ swz(TK, row)) * 16) + 8 * (kq & 1) + 4 * (g >> 1));
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 k = codes8(raw[ks], t.ks);
+#pragma unroll
+        for (int x = 0; x < NR; ++x) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[x][ks], s[x], 0, 0, 0);
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) vop[db] = codes4(vraw[db], t.vs);
+    } else {
+      const char *vb = kb + L::HALF;
+      bf16x8 kop[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kop[ks] = *(const bf16x8 *)(kb + k_row * L::K_ROW + (((4 * ks + g) ^ swz(L::K_ROW, k_row)) * 16));
+      if (t.t0 < 0) {
+        // (keys 4 g .. 4 g + 3 of a group of 16 sit at 8 (g & 1) + 4 (g >> 1))
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const int row = db * 16 + l16;
+          vop[db] = *(const bf16x4 *)(vb + row * L::VB_ROW + (((2 * kq + (g & 1)) ^ swz(L::VB_ROW, row)) * 16) + 8 * (g >> 1));
+        }
+      } else {
+        const int key = kq * 16 + 4 * g + (l16 >> 2);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) vop[db] = read_turned(vb + key * L::K_ROW + ((db * 2 + ((l16 >> 1) & 1)) ^ swz_tr(L::K_ROW, key)) * 16 + (l16 & 1) * 8);
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int x = 0; x < NR; ++x) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[ks], q[x][ks], s[x], 0, 0, 0);
+    }
+    if (t.valid < TK || (t.t0 >= 0 && t.t0 + TK - 1 > i_lo)) {
+#pragma unroll
+      for (int x = 0; x < NR; ++x) {
+        const int lim = min(t.valid - 1, t.t0 >= 0 ? my_i[x] - t.t0 : TK) - (kq * 16 + g * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[x][e] = e <= lim ? s[x][e] : -INFINITY;
+      }
+      const uint2 keep = keep_first(t.valid - kq * 16 - g * 4);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        vop[db] = cleared(vop[db], keep);
+        if (t.t0 >= 0) {
+          const uint2 w = __builtin_bit_cast(uint2, vop[db]);
+          tainted = taint(w.x, taint(w.y, tainted));
+        }
+      }
+    }
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int x = 0; x < NR; ++x) {
+      const f32x4 p = soften(s[x], x);
+      const bf16x4 pb = {(__bf16)p[0], (__bf16)p[1], (__bf16)p[2], (__bf16)p[3]};
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        o[db][x] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, vop[db]), __builtin_bit_cast(s16x4, pb), o[db][x], 0, 0, 0);
+    }
+  };
+
+  // ---- pipeline: pair p sits in stages 2 (p & 1) and the next; the barrier says that it has landed and that the pair before it has been read, so its
+  // stages take pair p + 1
+  Tile cur = bring(0), nxt = {};
+#pragma unroll
+  for (int x = 0; x < NR; ++x)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[x][ks]));
+  for (int p = 0; p < pairs; ++p) {
+    PC_WAIT_VMCNT(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (p + 1 < pairs) nxt = bring(p + 1);
+    compute(2 * (p & 1) + odd, cur);
+    cur = nxt;
+  }
+
+  // ---- merge of the eight wavefronts through LDS
+  __syncthreads();
+  float *om = (float *)lds, *ml = om + NW * kNarrowRows * L::O_ROW;   // [wave][row][O_ROW], [wave][row][2]
+  constexpr int VPR = D / 8;
+#pragma unroll
+  for (int x = 0; x < NR; ++x) {
+    const int row = x * 16 + l16;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *(f32x4 *)(om + (wave * kNarrowRows + row) * L::O_ROW + db * 16 + g * 4) = o[db][x];
+    const float l = row_sum(l_run[x]);
+    if (g == 0) *(float2 *)(ml + (wave * kNarrowRows + row) * 2) = make_float2(m_ref[x], l);
+  }
+  const bool any_tainted = __syncthreads_or(!(tainted == 0.f)) != 0;
+  for (int u0 = wave * 64; u0 < it.rows * VPR; u0 += 64 * NW) {
+    const int u = u0 + lane, row = min(u / VPR, it.rows - 1), dv = u % VPR;
+    const bool live = u < it.rows * VPR;
+    float mw[NW], lw[NW], m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float2 e = *(const float2 *)(ml + (w * kNarrowRows + row) * 2);
+      mw[w] = e.x;
+      lw[w] = e.y;
+      m = fmaxf(m, e.x);
+    }
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float f = mw[w] == -INFINITY ? (lw[w] == 0.f ? 0.f : 1.f) : fast_exp2(mw[w] - m);   // (a sum that is NaN without a maximum stays)
+      l += lw[w] * f;
+      if (lw[w] == 0.f && mw[w] == -INFINITY) continue;   // (a wavefront that saw no key of the row)
+      const float *src = om + (w * kNarrowRows + row) * L::O_ROW + dv * 8;
+      const f32x4 lo = *(const f32x4 *)src, hi = *(const f32x4 *)(src + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { acc[e] += lo[e] * f; acc[4 + e] += hi[e] * f; }
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    float bad = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      bad += acc[e] * 0.f;
+      acc[e] *= inv;
+    }
+    const int r = it.r_first + row, i = r / G, head = gkv * G + r - i * G;
+    // rows whose sums a later token's V has spoilt (a row's lanes are all in this wavefront)
+    unsigned long long redo = __builtin_expect(any_tainted, 0) ? __builtin_amdgcn_ballot_w64(live && !(bad == 0.f)) : 0ull;
+    const unsigned long long row_lanes = (1ull << VPR) - 1;
+    if (live && !(redo >> (lane / VPR * VPR) & row_lanes)) {
+      if (it.part < 0) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (__bf16)acc[e];
+        *(bf16x8 *)(a.out + ((size_t)it.row0 + i) * ((size_t)a.Hq * D) + (size_t)head * D + dv * 8) = v;
+        if (a.lse && dv == 0) a.lse[(size_t)head * a.N + it.row0 + i] = pc::lse_of(m, l);
+      } else {
+        const size_t prow = (size_t)gkv * a.part_rows + it.part + row;
+        *(f32x4 *)(a.part_o + prow * D + dv * 8) = f32x4{acc[0], acc[1], acc[2], acc[3]};
+        *(f32x4 *)(a.part_o + prow * D + dv * 8 + 4) = f32x4{acc[4], acc[5], acc[6], acc[7]};
+        if (dv == 0) *(float2 *)(a.part_ml + prow * 2) = make_float2(m, l);
+      }
+    }
+    while (redo) {
+      const int first = __builtin_ctzll(redo) / VPR;
+      redo &= ~(row_lanes << (first * VPR));
+      redo_and_write<D, KV8>(a, it, gkv, lane, u0 / VPR + first);
+    }
+  }
+}
+
+template <int D, bool KV8>
+__global__ __launch_bounds__(64 * NW, 2) void packed_attention_kernel(const Args a) {
+  __shared__ __align__(16) char lds[Lds<D>::BYTES];
+  // (workgroup ids go round-robin over the XCDs: a kv head's items share one where there are eight heads)
+  const int gkv = blockIdx.x % a.Hkv;
+  Item it;   // (in scalar registers: every branch on it is the wavefront's)
+  {
+    int32_t w[kItemWords];
+    const int32_t *src = a.words + (size_t)(blockIdx.x / a.Hkv) * kItemWords;
+#pragma unroll
+    for (int i = 0; i < kItemWords; ++i) w[i] = __builtin_amdgcn_readfirstlane(src[i]);
+    it = __builtin_bit_cast(Item, w);
+  }
+  if (it.kind == kWide) wide_item<D, KV8>(a, it, gkv, lds);
+  else if (it.rows <= 16) narrow_item<D, KV8, 1>(a, it, gkv, lds);
+  else narrow_item<D, KV8, 2>(a, it, gkv, lds);
+}
+
+// The partitions of split blocks: D/8 lanes have a row, 8 elements each, and take its partitions four at a time.
+template <int D>
+__global__ __launch_bounds__(256) void packed_merge_kernel(const Args a, int merges_at) {
+  constexpr int VPR = D / 8, ROWS = 256 / VPR;
+  const Merge m = *(const Merge *)(a.words + merges_at + blockIdx.x * kMergeWords);
+  const int gkv = blockIdx.z, row = blockIdx.y * ROWS + threadIdx.x / VPR, dv = threadIdx.x % VPR, G = a.Hq / a.Hkv;
+  if (row >= m.rows) return;
+  const size_t first = (size_t)gkv * a.part_rows + m.part + row;
+  float top = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int p0 = 0; p0 < m.n; p0 += 4) {
+    float2 e[4];
+    f32x4 x[4][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const size_t at = first + (size_t)min(p0 + j, m.n - 1) * m.rows;
+      e[j] = *(const float2 *)(a.part_ml + at * 2);
+      x[j][0] = *(const f32x4 *)(a.part_o + at * D + dv * 8);
+      x[j][1] = *(const f32x4 *)(a.part_o + at * D + dv * 8 + 4);
+      if (p0 + j >= m.n) e[j] = make_float2(-INFINITY, 0.f);
+    }
+    float t = top;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) t = fmaxf(t, e[j].x);
+    const float shrink = top == -INFINITY ? (l == 0.f ? 0.f : 1.f) : fast_exp2(top - t);
+    top = t;
+    l *= shrink;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) acc[d] *= shrink;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (e[j].y == 0.f) continue;   // (no key of the row in that partition)
+      const float w = e[j].x == -INFINITY ? e[j].y : e[j].y * fast_exp2(e[j].x - top);
+      l += w;
+#pragma unroll
+      for (int d = 0; d < 8; ++d) acc[d] += w * x[j][d >> 2][d & 3];
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const int r = m.r_first + row, i = r / G, head = gkv * G + r - i * G;
+  bf16x8 v;
+#pragma unroll
+  for (int d = 0; d < 8; ++d) v[d] = (__bf16)(acc[d] * inv);
+  *(bf16x8 *)(a.out + ((size_t)m.row0 + i) * ((size_t)a.Hq * D) + (size_t)head * D + dv * 8) = v;
+  if (a.lse && dv == 0) a.lse[(size_t)head * a.N + m.row0 + i] = pc::lse_of(top, l);
+}
+
+// ---------------------------------------------------------------- host side
+struct PackedWs {
+  int32_t *words;
+  float *part_o, *part_ml;
+  long most_items, part_rows;   // of one kv head
+  size_t total;
+};
+long most_blocks(const percache_config &c, int n_seq, int n_rows) { return (long)(c.n_q_heads / c.n_kv_heads) * n_rows / kNarrowRows + n_seq; }
+long most_part_rows(const percache_config &c, int n_cu, int n_rows) {   // of one kv head
+  const long rows = (long)(c.n_q_heads / c.n_kv_heads) * n_rows;
+  return std::max(rows, std::min(rows * kMaxPackedSplits, 2L * n_cu * kWideRows / c.n_kv_heads));
+}
+PackedWs carve(const percache_config &c, int n_cu, void *base, int n_seq, int n_rows, int max_chunks) {
+  PackedWs w;
+  char *p = (char *)base;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { char *r = p ? p + off : nullptr; off += pc::align_up(bytes); return r; };
+  const long blocks = most_blocks(c, n_seq, n_rows);
+  w.most_items = blocks + (long)kMoreItems * n_cu;
+  w.part_rows = most_part_rows(c, n_cu, n_rows);
+  w.words = (int32_t *)take(((size_t)w.most_items * kItemWords + (size_t)blocks * kMergeWords + (size_t)n_seq * max_chunks * 2 + 4) * sizeof(int32_t));
+  w.part_o = (float *)take((size_t)w.part_rows * c.n_kv_heads * c.head_dim * sizeof(float));
+  w.part_ml = (float *)take((size_t)w.part_rows * c.n_kv_heads * 2 * sizeof(float));
+  w.total = off;
+  return w;
+}
+int max_splits(const percache_config &c, int n_cu, int n_seq, int n_rows) {
+  const long rows = (long)(c.n_q_heads / c.n_kv_heads) * std::max(n_rows, 1), blocks = std::max(most_blocks(c, n_seq, n_rows), 1L);
+  const long by_rows = most_part_rows(c, n_cu, n_rows) / rows, by_items = 1 + (long)kMoreItems * n_cu / blocks;
+  return (int)std::max(1L, std::min((long)kMaxPackedSplits, std::min(by_rows, by_items)));
+}
+
+// The list of a call: items, longest first; merges; chunk entries.
+struct Plan {
+  std::vector<int32_t> words;
+  int n_items = 0, n_merges = 0, merges_at = 0, ents_at = 0, tallest = 0;
+};
+void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int stride, const int32_t *start, int n_seq, int n_splits, const PackedWs &ws, Plan &plan) {
+  const percache_config &c = ctx->cfg;
+  const int G = c.n_q_heads / c.n_kv_heads;
+  struct Block { int seq, r_first, rows, kind, tiles; float cost; };
+  std::vector<Block> blocks;
+  std::vector<int32_t> ents, first_ent(n_seq + 1), tiles_before;   // entries with keys; cached tiles before each
+  std::vector<int> cached(n_seq);
+  for (int s = 0; s < n_seq; ++s) {
+    first_ent[s] = (int)ents.size() / 2;
+    int tiles = 0;
+    if (start[s + 1] > start[s])
+      for (int ci = 0; ci < table[(size_t)s * stride]; ++ci) {
+        const int slot = table[(size_t)s * stride + pc::kTblHeader + 2 * ci], used = table[(size_t)s * stride + pc::kTblHeader + 2 * ci + 1];
+        if (used <= 0) continue;
+        ents.push_back(slot);
+        ents.push_back(used);
+        tiles_before.push_back(tiles);
+        tiles += (used + TK - 1) / TK;
+      }
+    cached[s] = tiles;
+  }
+  first_ent[n_seq] = (int)ents.size() / 2;
+  // Blocks of 256 rows, the last of a request narrow where 32 rows are left; all of them narrow while the whole call would leave half of the CUs idle.
+  auto cut = [&](int height) {
+    blocks.clear();
+    for (int s = 0; s < n_seq; ++s) {
+      const int R = G * (start[s + 1] - start[s]);
+      for (int r = 0; r < R;) {
+        const int rows = std::min(R - r, R - r <= kNarrowRows ? kNarrowRows : height), kind = rows <= kNarrowRows ? kNarrow : kWide;
+        const int tiles = cached[s] + ((r + rows - 1) / G) / TK + 1;
+        blocks.push_back({s, r, rows, kind, tiles, (kind == kWide ? 1.f : 0.4f) * (float)tiles + 2.f});
+        r += rows;
+      }
+    }
+  };
+  long narrow = 0, wide = 0;
+  for (int s = 0; s < n_seq; ++s) {
+    const long R = (long)G * (start[s + 1] - start[s]);
+    narrow += (R + kNarrowRows - 1) / kNarrowRows;
+    wide += (R + kWideRows - 1) / kWideRows;
+  }
+  cut(wide * c.n_kv_heads * 2 <= ctx->n_cu && narrow * c.n_kv_heads <= 2L * ctx->n_cu ? kNarrowRows : kWideRows);
+
+  float work = 0.f, longest = 0.f;
+  for (const Block &b : blocks) {
+    work += b.cost;
+    longest = std::max(longest, b.cost);
+  }
+  const float share = work * c.n_kv_heads / ctx->n_cu;   // of a CU
+  const float limit = longest <= 0.6f * share ? longest : 0.6f * share;
+  struct Unit { int block, begin, end; float cost; int part; };
+  std::vector<Unit> units;
+  long part_rows = 0, more = ws.most_items - (long)blocks.size();
+  for (int b = 0; b < (int)blocks.size(); ++b) {
+    const Block &x = blocks[b];
+    const int least = x.kind == kWide ? 8 : 4;   // tiles of a partition
+    int n = n_splits > 0 ? std::min(n_splits, x.tiles) : std::max(1, std::min({(int)(x.cost / limit + 0.999f), x.tiles / least, kMaxPackedSplits}));
+    if (n - 1 > more || part_rows + (long)n * x.rows > ws.part_rows) n = 1;
+    if (n > 1) {
+      const Merge m = {start[x.seq], x.r_first, x.rows, (int32_t)part_rows, n};
+      plan.words.insert(plan.words.end(), (const int32_t *)&m, (const int32_t *)&m + kMergeWords);
+      ++plan.n_merges;
+      plan.tallest = std::max(plan.tallest, x.rows);
+    }
+    for (int p = 0; p < n; ++p) {
+      const int begin = (int)((long)p * x.tiles / n), end = (int)((long)(p + 1) * x.tiles / n);
+      units.push_back({b, begin, end, x.cost * (float)(end - begin) / (float)x.tiles, n > 1 ? (int)part_rows + p * x.rows : -1});
+    }
+    if (n > 1) part_rows += (long)n * x.rows;
+    more -= n - 1;
+  }
+  std::stable_sort(units.begin(), units.end(), [](const Unit &x, const Unit &y) { return x.cost > y.cost; });
+  std::vector<int32_t> items;
+  items.reserve(units.size() * kItemWords);
+  for (const Unit &u : units) {
+    const Block &x = blocks[u.block];
+    const int s = x.seq, e0 = first_ent[s], e1 = first_ent[s + 1];
+    Item it = {};
+    it.row0 = start[s];
+    it.T = start[s + 1] - start[s];
+    it.r_first = x.r_first;
+    it.rows = x.rows;
+    it.kind = x.kind;
+    it.n_cached = std::max(0, std::min(u.end, cached[s]) - u.begin);
+    it.f0 = std::max(0, u.begin - cached[s]);
+    it.f1 = std::max(it.f0, u.end - cached[s]);
+    it.part = u.part;
+    if (it.n_cached > 0) {
+      const int first = (int)(std::upper_bound(tiles_before.begin() + e0, tiles_before.begin() + e1, u.begin) - tiles_before.begin()) - 1;
+      const int last = (int)(std::upper_bound(tiles_before.begin() + e0, tiles_before.begin() + e1, u.begin + it.n_cached - 1) - tiles_before.begin()) - 1;
+      it.ent = first;
+      it.n_ents = last - first + 1;
+      it.tile0 = u.begin - tiles_before[first];
+    }
+    items.insert(items.end(), (const int32_t *)&it, (const int32_t *)&it + kItemWords);
+  }
+  plan.n_items = (int)units.size();
+  plan.merges_at = (int)items.size();
+  items.insert(items.end(), plan.words.begin(), plan.words.end());
+  if (items.size() & 1) items.push_back(0);   // (entries are read two words at a time)
+  plan.ents_at = (int)items.size();
+  items.insert(items.end(), ents.begin(), ents.end());
+  plan.words = std::move(items);
+}
+}  // namespace
+
+extern "C" {
+
+size_t percache_packed_workspace_bytes(const percache_ctx *ctx, int32_t n_seq, int32_t n_rows, int32_t max_chunks) {
+  if (!ctx || n_seq < 1 || n_rows < 0 || max_chunks < 0) return 0;
+  return carve(ctx->cfg, ctx->n_cu, nullptr, n_seq, n_rows, max_chunks).total;
+}
+
+int32_t percache_packed_max_splits(const percache_ctx *ctx, int32_t n_seq, int32_t n_rows) {
+  if (!ctx || n_seq < 1 || n_rows < 0) return PC_EINVAL;
+  return max_splits(ctx->cfg, ctx->n_cu, n_seq, n_rows);
+}
+
+pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void *q_dev, const void *k_dev, const void *v_dev, int32_t n_rows,
+                                    const int32_t *start_host, int32_t n_seq, const int32_t *slot_ids_host, const int32_t *used_len_host,
+                                    const int32_t *n_chunks_host, int32_t max_chunks, int32_t n_splits, void *attn_out_dev, float *lse_out_dev,
+                                    void *workspace_dev, size_t workspace_bytes, void *stream) {
+  if (!ctx) return PC_EINVAL;
+  const percache_config &c = ctx->cfg;
+  if (n_seq < 1 || n_rows < 0) return pc::fail(ctx, PC_EINVAL, "n_seq must be positive and n_rows not negative");
+  if (!start_host) return pc::fail(ctx, PC_EINVAL, "start_host is NULL");
+  if (start_host[0] < 0) return pc::fail(ctx, PC_EINVAL, "start[0]=%d is negative", start_host[0]);
+  for (int s = 0; s < n_seq; ++s)
+    if (start_host[s + 1] < start_host[s]) return pc::fail(ctx, PC_EINVAL, "start[%d]=%d lies before start[%d]=%d", s + 1, start_host[s + 1], s, start_host[s]);
+  if (start_host[n_seq] > n_rows) return pc::fail(ctx, PC_EINVAL, "start[%d]=%d lies behind the last of %d rows", n_seq, start_host[n_seq], n_rows);
+  // (stacked rows of a request, and partial rows, are counted in 32 bits)
+  if ((long)n_rows * c.n_q_heads >= (1L << 31)) return pc::fail(ctx, PC_ESHAPE, "%d rows of %d heads are 2^31 or more", n_rows, c.n_q_heads);
+  const int cap = max_splits(c, ctx->n_cu, n_seq, n_rows);
+  if (n_splits < 0 || n_splits > cap) return pc::fail(ctx, PC_EINVAL, "n_splits %d outside [0,%d] for this shape", n_splits, cap);
+  std::vector<int32_t> table;
+  pc_status st = pc::build_chunk_table(ctx, layer, n_seq, 1, slot_ids_host, used_len_host, n_chunks_host, max_chunks, table);
+  if (st != PC_OK) return st;
+  const size_t need = percache_packed_workspace_bytes(ctx, n_seq, n_rows, max_chunks);
+  if (!workspace_dev || workspace_bytes < need) return pc::fail(ctx, PC_ENOMEM, "packed workspace has %zu bytes, need %zu", workspace_bytes, need);
+  if ((uintptr_t)workspace_dev % pc::kAlign) return pc::fail(ctx, PC_EINVAL, "workspace must be 256-byte aligned");
+  if (start_host[n_seq] == start_host[0]) return PC_OK;   // (no rows at all)
+  if (!q_dev || !k_dev || !v_dev || !attn_out_dev) return pc::fail(ctx, PC_EINVAL, "NULL tensor pointer");
+  if (((uintptr_t)q_dev | (uintptr_t)k_dev | (uintptr_t)v_dev | (uintptr_t)attn_out_dev) % 16) return pc::fail(ctx, PC_EINVAL, "tensor pointers must be 16-byte aligned");
+  if ((uintptr_t)lse_out_dev % sizeof(float)) return pc::fail(ctx, PC_EINVAL, "lse_out_dev must be 4-byte aligned");
+  const int stride = pc::tbl_stride(max_chunks), formats = pc::table_formats(table, stride, n_seq);
+  const PackedWs ws = carve(c, ctx->n_cu, workspace_dev, n_seq, n_rows, max_chunks);
+  Plan plan;
+  plan_items(ctx, table, stride, start_host, n_seq, n_splits, ws, plan);
+  hipStream_t s = (hipStream_t)stream;
+  st = pc::upload_table(ctx, plan.words, ws.words, s);
+  if (st != PC_OK) return st;
+  Args a = {};
+  a.q = (const __bf16 *)q_dev;
+  a.k = (const __bf16 *)k_dev;
+  a.v = (const __bf16 *)v_dev;
+  a.k16 = ctx->k_store + (size_t)layer * ctx->layer_stride;
+  a.v16 = ctx->v_store + (size_t)layer * ctx->layer_stride;
+  a.k8 = ctx->k8_store + (size_t)layer * ctx->layer_stride8;
+  a.v8 = ctx->v8_store + (size_t)layer * ctx->layer_stride8;
+  const size_t sc = (size_t)layer * ctx->n_slots8 * c.n_kv_heads * (c.slot_capacity / TK);
+  a.k_scale = ctx->k_scale + sc;
+  a.v_scale = ctx->v_scale + sc;
+  a.words = ws.words;
+  a.out = (__bf16 *)attn_out_dev;
+  a.lse = lse_out_dev;
+  a.part_o = ws.part_o;
+  a.part_ml = ws.part_ml;
+  a.N = n_rows;
+  a.part_rows = ws.part_rows;
+  a.n_items = plan.n_items;
+  a.ents_at = plan.ents_at;
+  a.Hq = c.n_q_heads;
+  a.Hkv = c.n_kv_heads;
+  a.C = c.slot_capacity;
+  a.n_slots16 = ctx->n_slots16;
+  a.scale_log2e = 1.4426950408889634f / sqrtf((float)c.head_dim);
+  const dim3 grid((unsigned)((long)plan.n_items * c.n_kv_heads));
+  pc::prof_begin(ctx, PC_KERNEL_ATTENTION, s);
+#define PC_PACKED(DD, EE) hipLaunchKernelGGL((packed_attention_kernel<DD, EE>), grid, dim3(64 * NW), 0, s, a)
+  if (c.head_dim == 128) { if (formats & 1) PC_PACKED(128, true); else PC_PACKED(128, false); }
+  else { if (formats & 1) PC_PACKED(64, true); else PC_PACKED(64, false); }
+#undef PC_PACKED
+  PC_HIP(ctx, hipGetLastError());
+  pc::prof_end(ctx, PC_KERNEL_ATTENTION, s);
+  if (plan.n_merges) {
+    const int per = 256 / (c.head_dim / 8);
+    const dim3 mgrid((unsigned)plan.n_merges, (unsigned)((plan.tallest + per - 1) / per), (unsigned)c.n_kv_heads);
+    if (c.head_dim == 128) hipLaunchKernelGGL(packed_merge_kernel<128>, mgrid, dim3(256), 0, s, a, plan.merges_at);
+    else hipLaunchKernelGGL(packed_merge_kernel<64>, mgrid, dim3(256), 0, s, a, plan.merges_at);
+    PC_HIP(ctx, hipGetLastError());
+  }
+  return PC_OK;
+}
+
+}  // extern "C"
