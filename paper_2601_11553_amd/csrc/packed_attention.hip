@@ -67,7 +67,7 @@ struct Lds {
   static constexpr int K_ROW = D * 2, VB_ROW = TK * 2;
   static constexpr int HALF = TK * D * 2, STAGE = 2 * HALF, NSTAGE = 4;
   static constexpr int O_ROW = D + 4;                                                        // narrow: floats per output row of a wavefront
-  static constexpr int MERGE = NW * kNarrowRows * (O_ROW + 2) * 4;
+  static constexpr int MERGE = NW * kNarrowRows * (O_ROW + 2) * 4 + NW * 4;
   static constexpr int BYTES = NSTAGE * STAGE > MERGE ? NSTAGE * STAGE : MERGE;
 };
 __device__ __forceinline__ int swz(int row_bytes, int row) { return row_bytes == 256 ? (row & 15) : row_bytes == 128 ? ((row >> 1) & 7) : ((row >> 2) & 3); }
@@ -103,6 +103,16 @@ __device__ __forceinline__ bf16x8 cleared(bf16x8 v, uint2 lo, uint2 hi) {
 __device__ __forceinline__ float taint(unsigned two, float acc) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, two), bf16x2{(__bf16)0.f, (__bf16)0.f}, acc, false);
+}
+
+// 16 bytes a lane from src + off to LDS: lane l's to address to + 16 l.  Written out because the compiler would make every transpose read behind it wait
+// for all requests in flight; what is read from LDS is waited for where the stages change hands (PC_WAIT_VMCNT).  (m0 is the compiler's own only around
+// instructions that need it, of which this file has no others; the wait states are those between a vector instruction that writes a scalar register and
+// a memory instruction that reads it.)
+template <bool ONCE>   // ONCE: read by this workgroup only, not kept in the caches
+__device__ __forceinline__ void to_lds(const char *src, unsigned off, unsigned to) {
+  if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(to), "v"(off), "s"(src) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(src) : "memory");
 }
 
 struct Tile { const char *k, *v; int valid, t0; bool is8; float ks, vs; };   // t0: first fresh token, -1 for a cached tile
@@ -278,35 +288,36 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
   Walk<D, KV8> walk(a, it, gkv, lane);
   const int n = walk.n();
 
-  // ---- requests: wavefronts 0..3 bring in a bf16 tile, instruction i of a half its bytes [1024 i, +1024)
-  unsigned k_off[INSTR], vb_off[INSTR], vf_off[INSTR];
-#pragma unroll
-  for (int j = 0; j < INSTR; ++j) {
-    const int byte = ((wave & (NLD - 1)) + j * NLD) * 1024 + lane * 16;
+  // ---- requests: wavefronts 0..3 bring in a bf16 tile, instruction i of a half its bytes [1024 i, +1024).  The rows of a wavefront's instructions are 16 (of
+  // 256 bytes; of 128 bytes 32) apart and swizzled alike: one offset for all of them, the distance goes into the scalar base.
+  constexpr int APART = NLD * 1024;
+  static_assert(APART % (16 * 256) == 0, "the instructions' rows are swizzled alike");
+  unsigned k_off, vb_off, vf_off;
+  {
+    const int byte = (wave & (NLD - 1)) * 1024 + lane * 16;
     const int row = byte / L::K_ROW, pc = byte % L::K_ROW / 16, d = byte / L::VB_ROW, pd = byte % L::VB_ROW / 16;
-    k_off[j] = row * L::K_ROW + (pc ^ swz(L::K_ROW, row)) * 16;
-    vf_off[j] = row * L::K_ROW + (pc ^ swz_tr(L::K_ROW, row)) * 16;
-    vb_off[j] = d * L::VB_ROW + (pd ^ swz(L::VB_ROW, d)) * 16;
+    k_off = row * L::K_ROW + (pc ^ swz(L::K_ROW, row)) * 16;
+    vf_off = row * L::K_ROW + (pc ^ swz_tr(L::K_ROW, row)) * 16;
+    vb_off = d * L::VB_ROW + (pd ^ swz(L::VB_ROW, d)) * 16;
   }
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
   auto request = [&](const Tile &t, int st) __attribute__((always_inline)) {
-    char *kb = lds + st * L::STAGE;
-    const bool ragged = t.valid < TK;   // rows past the end repeat the last valid one (masked later); a block of the store is there as a whole
+    const unsigned kb = lds_base + st * L::STAGE + (wave & (NLD - 1)) * 1024, vb = kb + L::HALF;
+    if (__builtin_expect(t.valid < TK, 0)) {   // rows past the end repeat the last valid one (masked later); a block of the store is there as a whole
+      const int last = t.valid - 1;
 #pragma unroll
-    for (int j = 0; j < INSTR; ++j) {
-      unsigned ko = k_off[j];
-      if (__builtin_expect(ragged, 0)) ko = min((int)(ko / L::K_ROW), t.valid - 1) * L::K_ROW + ko % L::K_ROW;
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(t.k + ko),
-                                       (__attribute__((address_space(3))) void *)(kb + ((wave & (NLD - 1)) + j * NLD) * 1024), 16, 0, 0);
-    }
-#pragma unroll
-    for (int j = 0; j < INSTR; ++j) {
-      unsigned vo = t.t0 < 0 ? vb_off[j] : vf_off[j];
-      if (__builtin_expect(ragged, 0)) {
-        if (t.t0 >= 0) vo = min((int)(vo / L::K_ROW), t.valid - 1) * L::K_ROW + vo % L::K_ROW;
+      for (int j = 0; j < INSTR; ++j) {
+        const unsigned ko = k_off + j * APART, vo = vf_off + j * APART;
+        to_lds<false>(t.k, min((int)(ko / L::K_ROW), last) * L::K_ROW + ko % L::K_ROW, kb + j * APART);
+        to_lds<false>(t.v, t.t0 < 0 ? vb_off + j * APART : min((int)(vo / L::K_ROW), last) * L::K_ROW + vo % L::K_ROW, vb + j * APART);
       }
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(t.v + vo),
-                                       (__attribute__((address_space(3))) void *)(kb + L::HALF + ((wave & (NLD - 1)) + j * NLD) * 1024), 16, 0, 0);
+      return;
     }
+    const unsigned v_off = t.t0 < 0 ? vb_off : vf_off;
+#pragma unroll
+    for (int j = 0; j < INSTR; ++j) to_lds<false>(t.k + j * APART, k_off, kb + j * APART);
+#pragma unroll
+    for (int j = 0; j < INSTR; ++j) to_lds<false>(t.v + j * APART, v_off, vb + j * APART);
   };
   // 8-bit tiles: codes through registers, 16 of K and of V a thread (D = 64: of the first half of the threads), turned into a bf16 tile one tile
   // ahead of the arithmetic.  The stores are ones that the compiler does not see, for which it would wait for every request in flight.
@@ -319,7 +330,6 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
     kc = *(const u32x4 *)(t.k + min(ck_row, t.valid - 1) * D + ck_c * 16);
     vc = *(const u32x4 *)(t.v + cv_row * TK + cv_m * 16);
   };
-  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
   auto store16 = [&](int off, bf16x8 x) __attribute__((always_inline)) {
     const unsigned addr = lds_base + (unsigned)off;
     asm volatile("ds_write_b128 %0, %1" : : "v"(addr), "v"(x) : "memory");
@@ -385,9 +395,26 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
           }
         }
     };
+    // what stands behind the last key is cleared; whether what is left is finite matters where later rows are among it
+    auto clear = [&](int half) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c2 = 0; c2 < 2; ++c2) {
+        const int left = t.valid - (16 * (2 * half + c2) + 4 * g2);
+        const uint2 lo = keep_first(left), hi = keep_first(left - 8);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          vop[half][db][c2] = cleared(vop[half][db][c2], lo, hi);
+          if (FRESH) {
+            const u32x4 w = __builtin_bit_cast(u32x4, vop[half][db][c2]);
+            tainted = taint(w[0], taint(w[1], taint(w[2], taint(w[3], tainted))));
+          }
+        }
+      }
+    };
     v_operands(0);
     const bool ragged = t.valid < TK, causal = FRESH && t.t0 + TK - 1 > i_lo;
     if (__builtin_expect(ragged || causal, 0)) {
+      clear(0);
       int t_lane = g2 * 4;
       asm volatile("" : "+v"(t_lane));   // (keeps the per-element key indices out of loop-invariant registers)
       const int lim = min(t.valid - 1, FRESH ? my_i - t.t0 : TK) - t_lane;
@@ -442,23 +469,7 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
     }
     l_run += psum;
     v_operands(1);
-    if (__builtin_expect(ragged || causal, 0)) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int c2 = 0; c2 < 2; ++c2) {
-          const int left = t.valid - (16 * (2 * half + c2) + 4 * g2);
-          const uint2 lo = keep_first(left), hi = keep_first(left - 8);
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            vop[half][db][c2] = cleared(vop[half][db][c2], lo, hi);
-            if (FRESH) {
-              const u32x4 w = __builtin_bit_cast(u32x4, vop[half][db][c2]);
-              tainted = taint(w[0], taint(w[1], taint(w[2], taint(w[3], tainted))));
-            }
-          }
-        }
-    }
+    if (__builtin_expect(ragged || causal, 0)) clear(1);
 #pragma unroll
     for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -473,38 +484,44 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
   // what it has in flight (its share of tile t+1; codes of t+1, which it then turns into their stage), and tile t+2 is requested into the stage
   // that iteration t-1 read; the barrier publishes tile t+1.
   Tile cur = {}, nxt = {}, aft = {};
-  auto bring = [&](Tile &t, int st) __attribute__((always_inline)) {
+  auto bring = [&](Tile &t, int st, auto codes_c) __attribute__((always_inline)) {
     t = walk.next();
-    if (KV8 && t.is8) load_codes(t);
+    if (decltype(codes_c)::value && t.is8) load_codes(t);
     else if (wave < NLD) request(t, st);
   };
-  bring(cur, 0);
+  const std::bool_constant<KV8> codes;
+  bring(cur, 0, codes);
   if (KV8 && cur.is8) land_codes(cur, 0);
-  if (n > 1) bring(nxt, 1);
+  if (n > 1) bring(nxt, 1, codes);
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
   __builtin_amdgcn_s_waitcnt(0);
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  int st = 0;
-  for (int t = 0; t < n; ++t) {
+  // (two loops, one after the other: with both kinds of tiles in one the compiler runs out of registers)
+  int st = 0, t = 0;
+  auto step = [&](auto codes_c) __attribute__((always_inline)) {
     const int s1 = st + 1 == NSTAGE ? 0 : st + 1, s2 = s1 + 1 == NSTAGE ? 0 : s1 + 1;
-    if (wave_live) {
-      if (cur.t0 < 0) tile(st, cur, std::false_type{});
-      else if (cur.t0 <= i_hi) tile(st, cur, std::true_type{});
-    }
     PC_WAIT_VMCNT(0);
-    if (KV8 && t + 1 < n && nxt.is8) {
+    if (decltype(codes_c)::value && t + 1 < n && nxt.is8) {
       land_codes(nxt, s1);
       __builtin_amdgcn_s_waitcnt(0xc07f);   // (lgkmcnt 0)
     }
-    if (t + 2 < n) bring(aft, s2);
+    if (t + 2 < n) bring(aft, s2, codes_c);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     cur = nxt;
     nxt = aft;
     st = s1;
+  };
+  for (; t < it.n_cached; ++t) {
+    if (wave_live) tile(st, cur, std::false_type{});
+    step(codes);
+  }
+  for (; t < n; ++t) {
+    if (wave_live && cur.t0 <= i_hi) tile(st, cur, std::true_type{});
+    step(std::false_type{});
   }
   if (!wave_live) return;
 
@@ -579,19 +596,18 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
   const int n = walk.n(), pairs = (n + 1) / 2;
 
   // requests: four wavefronts a tile; 8-bit tiles stay codes (K rows of D bytes, V rows of 64)
-  auto half = [&](const char *src, char *dst, auto row_bytes_c, int instr, int last_row, bool turned) __attribute__((always_inline)) {
+  const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
+  auto half = [&](const char *src, unsigned dst, auto row_bytes_c, int instr, int last_row, bool turned) __attribute__((always_inline)) {
     constexpr int RB = decltype(row_bytes_c)::value;
 #pragma unroll
     for (int j = 0; j < I16; ++j) {
       if (j >= instr) break;
       const int byte = (kq + j * 4) * 1024 + lane * 16, row = byte / RB, pc = byte % RB / 16;
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void *)(src + (unsigned)(min(row, last_row) * RB + (pc ^ (turned ? swz_tr(RB, row) : swz(RB, row))) * 16)),
-          (__attribute__((address_space(3))) void *)(dst + (kq + j * 4) * 1024), 16, 0, 2);
+      to_lds<true>(src, (unsigned)(min(row, last_row) * RB + (pc ^ (turned ? swz_tr(RB, row) : swz(RB, row))) * 16), dst + (kq + j * 4) * 1024);
     }
   };
   auto request = [&](const Tile &t, int st) __attribute__((always_inline)) {
-    char *dst = lds + st * L::STAGE;
+    const unsigned dst = lds_base + st * L::STAGE;
     if (KV8 && t.is8) {
       half(t.k, dst, std::integral_constant<int, D>{}, I8, t.valid - 1, false);
       half(t.v, dst + L::HALF / 2, std::integral_constant<int, TK>{}, I8, D - 1, false);
@@ -739,19 +755,31 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
     cur = nxt;
   }
 
-  // ---- merge of the eight wavefronts through LDS
+  // ---- merge of the eight wavefronts through LDS (by stores that the compiler does not see: it would make every operand read of this kernel wait for all
+  // requests in flight)
   __syncthreads();
-  float *om = (float *)lds, *ml = om + NW * kNarrowRows * L::O_ROW;   // [wave][row][O_ROW], [wave][row][2]
+  const float *om = (const float *)lds, *ml = om + NW * kNarrowRows * L::O_ROW, *tl = ml + NW * kNarrowRows * 2;   // [wave][row][O_ROW], [wave][row][2], [wave]
   constexpr int VPR = D / 8;
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
-    const int row = x * 16 + l16;
+    const int row = wave * kNarrowRows + x * 16 + l16;
+    const unsigned to = lds_base + (unsigned)((row * L::O_ROW + g * 4) * 4);
 #pragma unroll
-    for (int db = 0; db < DB; ++db) *(f32x4 *)(om + (wave * kNarrowRows + row) * L::O_ROW + db * 16 + g * 4) = o[db][x];
+    for (int db = 0; db < DB; ++db) asm volatile("ds_write_b128 %0, %1 offset:%2" : : "v"(to), "v"(o[db][x]), "n"(db * 64) : "memory");
     const float l = row_sum(l_run[x]);
-    if (g == 0) *(float2 *)(ml + (wave * kNarrowRows + row) * 2) = make_float2(m_ref[x], l);
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    if (g == 0) asm volatile("ds_write_b64 %0, %1" : : "v"(lds_base + (unsigned)((NW * kNarrowRows * L::O_ROW + row * 2) * 4)), "v"(f32x2{m_ref[x], l}) : "memory");
   }
-  const bool any_tainted = __syncthreads_or(!(tainted == 0.f)) != 0;
+  {
+    const float any = __builtin_amdgcn_ballot_w64(!(tainted == 0.f)) ? 1.f : 0.f;
+    if (lane == 0) asm volatile("ds_write_b32 %0, %1" : : "v"(lds_base + (unsigned)((NW * kNarrowRows * (L::O_ROW + 2) + wave) * 4)), "v"(any) : "memory");
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  float spoilt = 0.f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) spoilt += tl[w];
+  const bool any_tainted = __builtin_amdgcn_ballot_w64(spoilt != 0.f) != 0;
   for (int u0 = wave * 64; u0 < it.rows * VPR; u0 += 64 * NW) {
     const int u = u0 + lane, row = min(u / VPR, it.rows - 1), dv = u % VPR;
     const bool live = u < it.rows * VPR;
