@@ -13,6 +13,10 @@
 // What a row does not see takes no part, whatever stands there: K by the mask on the scores; V behind the end of a chunk or a request by clearing the
 // operand; V of a later token of the same tile, where it is not finite, by computing the rows that it made NaN once more, key by key.
 #include <algorithm>
+#include <cmath>
+#include <cstddef>
+#include <cstring>
+#include <functional>
 
 #include "decode_common.hpp"
 
@@ -37,14 +41,14 @@ constexpr float kSumLimit4 = 4.f * 256.f;  // 4 of them
 constexpr int kMaxPackedSplits = 64;
 constexpr int kMoreItems = 16;             // items beyond one a block, per CU
 
-// A workgroup's work, for every kv head: rows [r_first, r_first + rows) of a request (stacked) over n_cached cached tiles from tile tile0 of chunk entry
-// ent on, then over the fresh tiles [f0, f1).
+// A workgroup's work, for every kv head: `rows` stacked rows from head rem0 of token i0 of a request on, over n_cached cached tiles from tile tile0 of
+// chunk entry ent on, then over the fresh tiles [f0, f1).
 struct Item {
-  int32_t row0, T, r_first, rows, kind, n_cached, ent, n_ents, tile0, f0, f1;
+  int32_t row0, T, i0, rem0, rows, kind, n_cached, ent, n_ents, tile0, f0, f1;
   int32_t part;   // first row of its partial results, -1: it is the block's only partition
 };
 constexpr int kItemWords = sizeof(Item) / 4;
-struct Merge { int32_t row0, r_first, rows, part, n; };   // partition p of the block has its partial rows from part + p * rows on
+struct Merge { int32_t row0, i0, rem0, rows, part, n; };   // partition p of the block has its partial rows from part + p * rows on
 constexpr int kMergeWords = sizeof(Merge) / 4;
 
 struct Args {
@@ -57,9 +61,28 @@ struct Args {
   float *lse;                // [Hq][N] or null
   float *part_o, *part_ml;   // [part_rows of every kv head][D], [...][2]
   long N, part_rows;
-  int n_items, ents_at, Hq, Hkv, C, n_slots16;
+  int merges_at, ents_at, Hq, Hkv, C, n_slots16;
+  unsigned per_group;        // 2^32 / G, rounded up: x / G = the upper half of x times it for the small x of a block
   float scale_log2e;
 };
+
+// Lists that fit a launch's arguments are read from there: no launch in front that copies them.
+struct ArgsAndWords {
+  Args a;
+  int32_t words[pc::kListWords];
+};
+static_assert(sizeof(ArgsAndWords) <= 4096, "the arguments of a launch");
+__device__ __forceinline__ const int32_t *words_of_launch() {
+  return (const int32_t *)((const char *)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(ArgsAndWords, words));
+}
+
+// token (of its request) and query head of a block's row
+struct RowAt { int i, head; };
+template <class Block>
+__device__ __forceinline__ RowAt row_at(const Args &a, const Block &b, int gkv, int local) {
+  const int G = a.Hq / a.Hkv, x = b.rem0 + local, q = G == 1 ? x : (int)__umulhi((unsigned)x, a.per_group);
+  return {b.i0 + q, gkv * G + x - q * G};
+}
 
 // A stage of LDS: a K tile [64][D], rows swizzled by 16-byte chunks, then V: a block [D][64] of the store or, fresh, rows [64][D].
 template <int D>
@@ -169,8 +192,10 @@ struct Walk {
       t.t0 = -1;
       t.is8 = c8;
       if (KV8 && c8) {
-        t.ks = a.k_scale[sc + at];
-        t.vs = a.v_scale[sc + at];
+        // (scalar loads: vector ones would be waited for together with the tiles requested behind them)
+        typedef const __attribute__((address_space(4))) float *scalar;
+        t.ks = ((scalar)a.k_scale)[sc + at];
+        t.vs = ((scalar)a.v_scale)[sc + at];
       }
       skip(1);
       if (left <= 0 && idx + 1 < it.n_cached) {
@@ -197,7 +222,7 @@ struct Walk {
 template <int D, bool KV8>
 __device__ __forceinline__ void redo_row(const Args &a, const Item &it, int gkv, int lane, int local, float &m_out, float &l_out, float (&o)[D / 64]) {
   constexpr int E = D / 64;
-  const int G = a.Hq / a.Hkv, r = it.r_first + local, i = r / G, head = gkv * G + r % G;
+  const auto [i, head] = row_at(a, it, gkv, local);
   float q[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -243,7 +268,7 @@ template <int D, bool KV8>
 __device__ __forceinline__ void redo_and_write(const Args &a, const Item &it, int gkv, int lane, int local) {
   float m, l, o[D / 64];
   redo_row<D, KV8>(a, it, gkv, lane, local, m, l, o);
-  const int G = a.Hq / a.Hkv, r = it.r_first + local, i = r / G, head = gkv * G + r % G;
+  const auto [i, head] = row_at(a, it, gkv, local);
   if (it.part < 0) {
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) a.out[((size_t)it.row0 + i) * ((size_t)a.Hq * D) + (size_t)head * D + e * 64 + lane] = (__bf16)o[e];
@@ -262,14 +287,14 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
   using L = Lds<D>;
   constexpr int NLD = 4, NSTAGE = 3, KS = D / 16, DB = D / 32, INSTR = L::HALF / 1024 / NLD;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g2 = lane >> 5;
-  const int G = a.Hq / a.Hkv;
 
   const int local = wave * 32 + l32;
   const bool row_ok = local < it.rows;
-  const int r = it.r_first + min(local, it.rows - 1), my_i = r / G, head = gkv * G + r - my_i * G;
+  const RowAt mine = row_at(a, it, gkv, min(local, it.rows - 1));
+  const int my_i = mine.i, head = mine.head;
   // first and last token among this wavefront's rows: a fresh tile that reaches past the first is masked, one that starts behind the last skipped
   const bool wave_live = wave * 32 < it.rows;
-  const int i_lo = (it.r_first + wave * 32) / G, i_hi = (it.r_first + min(wave * 32 + 32, it.rows) - 1) / G;
+  const int i_lo = __builtin_amdgcn_readlane(my_i, 0), i_hi = __builtin_amdgcn_readlane(my_i, 31);
 
   bf16x8 qf[KS];
   {
@@ -570,19 +595,18 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
   using L = Lds<D>;
   constexpr int KS = D / 32, DB = D / 16, I16 = L::HALF / 1024 / 4, I8 = I16 / 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4;
-  const int odd = wave >> 2, kq = wave & 3, G = a.Hq / a.Hkv;
+  const int odd = wave >> 2, kq = wave & 3;
 
   int my_i[NR];
   bf16x8 q[NR][KS];
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
-    const int r = it.r_first + min(x * 16 + l16, it.rows - 1);
-    my_i[x] = r / G;
-    const __bf16 *p = a.q + ((size_t)(gkv * G + r - my_i[x] * G) * a.N + it.row0 + my_i[x]) * D + g * 8;
+    const RowAt r = row_at(a, it, gkv, min(x * 16 + l16, it.rows - 1));
+    my_i[x] = r.i;
+    const __bf16 *p = a.q + ((size_t)r.head * a.N + it.row0 + r.i) * D + g * 8;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) q[x][ks] = *(const bf16x8 *)(p + ks * 32);
   }
-  const int i_lo = it.r_first / G;
   f32x4 o[DB][NR];
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -595,15 +619,17 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
   Walk<D, KV8> walk(a, it, gkv, lane);
   const int n = walk.n(), pairs = (n + 1) / 2;
 
-  // requests: four wavefronts a tile; 8-bit tiles stay codes (K rows of D bytes, V rows of 64)
+  // requests: four wavefronts a tile; 8-bit tiles stay codes (K rows of D bytes, V rows of 64).  The rows of a wavefront's instructions are 4096 bytes apart
+  // and swizzled alike; rows past the end repeat the last valid one (masked later).
   const unsigned lds_base = (unsigned)(size_t)(__attribute__((address_space(3))) char *)lds;
+  const int byte0 = kq * 1024 + lane * 16;
   auto half = [&](const char *src, unsigned dst, auto row_bytes_c, int instr, int last_row, bool turned) __attribute__((always_inline)) {
     constexpr int RB = decltype(row_bytes_c)::value;
+    const int row = byte0 / RB, c = (byte0 % RB / 16 ^ (turned ? swz_tr(RB, row) : swz(RB, row))) * 16;
 #pragma unroll
     for (int j = 0; j < I16; ++j) {
       if (j >= instr) break;
-      const int byte = (kq + j * 4) * 1024 + lane * 16, row = byte / RB, pc = byte % RB / 16;
-      to_lds<true>(src, (unsigned)(min(row, last_row) * RB + (pc ^ (turned ? swz_tr(RB, row) : swz(RB, row))) * 16), dst + (kq + j * 4) * 1024);
+      to_lds<true>(src, (unsigned)(min(row + j * (4096 / RB), last_row) * RB + c), dst + kq * 1024 + j * 4096);
     }
   };
   auto request = [&](const Tile &t, int st) __attribute__((always_inline)) {
@@ -710,7 +736,7 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
 #pragma unroll
         for (int x = 0; x < NR; ++x) s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[ks], q[x][ks], s[x], 0, 0, 0);
     }
-    if (t.valid < TK || (t.t0 >= 0 && t.t0 + TK - 1 > i_lo)) {
+    if (t.valid < TK || (t.t0 >= 0 && t.t0 + TK - 1 > it.i0)) {
 #pragma unroll
       for (int x = 0; x < NR; ++x) {
         const int lim = min(t.valid - 1, t.t0 >= 0 ? my_i[x] - t.t0 : TK) - (kq * 16 + g * 4);
@@ -738,21 +764,30 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
     }
   };
 
-  // ---- pipeline: pair p sits in stages 2 (p & 1) and the next; the barrier says that it has landed and that the pair before it has been read, so its
-  // stages take pair p + 1
+  // ---- pipeline: pair p sits in stages 2 (p & 1) and the next.  The first barrier of an iteration says that it has landed, the second that it has been
+  // read, so that its stages take pair p + 2: one to two pairs are on their way while this one is worked on.
   Tile cur = bring(0), nxt = {};
+  if (pairs > 1) nxt = bring(1);
 #pragma unroll
   for (int x = 0; x < NR; ++x)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(q[x][ks]));
   for (int p = 0; p < pairs; ++p) {
-    PC_WAIT_VMCNT(0);
+    // (behind this pair's requests are those of the next: of this wavefront 2 I16, 2 I8 of a tile of codes, none past the end)
+    if (p + 1 >= pairs || nxt.valid == 0) PC_WAIT_VMCNT(0);
+    else if (KV8 && nxt.is8) PC_WAIT_VMCNT(2 * I8);
+    else PC_WAIT_VMCNT(2 * I16);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (p + 1 < pairs) nxt = bring(p + 1);
     compute(2 * (p & 1) + odd, cur);
     cur = nxt;
+    if (p + 2 < pairs) {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      nxt = bring(p + 2);
+    }
   }
 
   // ---- merge of the eight wavefronts through LDS (by stores that the compiler does not see: it would make every operand read of this kernel wait for all
@@ -760,6 +795,12 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
   __syncthreads();
   const float *om = (const float *)lds, *ml = om + NW * kNarrowRows * L::O_ROW, *tl = ml + NW * kNarrowRows * 2;   // [wave][row][O_ROW], [wave][row][2], [wave]
   constexpr int VPR = D / 8;
+  // (the matrix instructions' results are not waited for by what the compiler does not see)
+#pragma unroll
+  for (int x = 0; x < NR; ++x)
+#pragma unroll
+    for (int db = 0; db < DB; ++db) asm volatile("" : "+v"(o[db][x]));
+  asm volatile("s_nop 15\n\ts_nop 15");
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
     const int row = wave * kNarrowRows + x * 16 + l16;
@@ -783,23 +824,21 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
   for (int u0 = wave * 64; u0 < it.rows * VPR; u0 += 64 * NW) {
     const int u = u0 + lane, row = min(u / VPR, it.rows - 1), dv = u % VPR;
     const bool live = u < it.rows * VPR;
-    float mw[NW], lw[NW], m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float2 *const mlr = (const float2 *)ml + row;
 #pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, mlr[w * kNarrowRows].x);
+    // (little code: it runs once a workgroup, from memory rather than from the instruction cache)
+#pragma unroll 2
     for (int w = 0; w < NW; ++w) {
-      const float2 e = *(const float2 *)(ml + (w * kNarrowRows + row) * 2);
-      mw[w] = e.x;
-      lw[w] = e.y;
-      m = fmaxf(m, e.x);
-    }
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float f = mw[w] == -INFINITY ? (lw[w] == 0.f ? 0.f : 1.f) : fast_exp2(mw[w] - m);   // (a sum that is NaN without a maximum stays)
-      l += lw[w] * f;
-      if (lw[w] == 0.f && mw[w] == -INFINITY) continue;   // (a wavefront that saw no key of the row)
+      const float2 e = mlr[w * kNarrowRows];
       const float *src = om + (w * kNarrowRows + row) * L::O_ROW + dv * 8;
       const f32x4 lo = *(const f32x4 *)src, hi = *(const f32x4 *)(src + 4);
+      if (e.y == 0.f && e.x == -INFINITY) continue;   // (a wavefront that saw no key of the row)
+      const float f = e.x == -INFINITY ? 1.f : fast_exp2(e.x - m);   // (a sum that is NaN without a maximum stays)
+      l += e.y * f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { acc[e] += lo[e] * f; acc[4 + e] += hi[e] * f; }
+      for (int x = 0; x < 4; ++x) { acc[x] += lo[x] * f; acc[4 + x] += hi[x] * f; }
     }
     const float inv = l == 0.f ? 0.f : 1.0f / l;
     float bad = 0.f;
@@ -808,7 +847,7 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
       bad += acc[e] * 0.f;
       acc[e] *= inv;
     }
-    const int r = it.r_first + row, i = r / G, head = gkv * G + r - i * G;
+    const auto [i, head] = row_at(a, it, gkv, row);
     // rows whose sums a later token's V has spoilt (a row's lanes are all in this wavefront)
     unsigned long long redo = __builtin_expect(any_tainted, 0) ? __builtin_amdgcn_ballot_w64(live && !(bad == 0.f)) : 0ull;
     const unsigned long long row_lanes = (1ull << VPR) - 1;
@@ -835,7 +874,7 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
 }
 
 template <int D, bool KV8>
-__global__ __launch_bounds__(64 * NW, 2) void packed_attention_kernel(const Args a) {
+__device__ __forceinline__ void packed_item(const Args &a) {
   __shared__ __align__(16) char lds[Lds<D>::BYTES];
   // (workgroup ids go round-robin over the XCDs: a kv head's items share one where there are eight heads)
   const int gkv = blockIdx.x % a.Hkv;
@@ -851,13 +890,21 @@ __global__ __launch_bounds__(64 * NW, 2) void packed_attention_kernel(const Args
   else if (it.rows <= 16) narrow_item<D, KV8, 1>(a, it, gkv, lds);
   else narrow_item<D, KV8, 2>(a, it, gkv, lds);
 }
+template <int D, bool KV8>
+__global__ __launch_bounds__(64 * NW, 2) void packed_attention_kernel(const Args a) { packed_item<D, KV8>(a); }
+template <int D, bool KV8>
+__global__ __launch_bounds__(64 * NW, 2) void packed_attention_words_kernel(const ArgsAndWords w) {
+  Args a = w.a;
+  a.words = words_of_launch();
+  packed_item<D, KV8>(a);
+}
 
 // The partitions of split blocks: D/8 lanes have a row, 8 elements each, and take its partitions four at a time.
 template <int D>
-__global__ __launch_bounds__(256) void packed_merge_kernel(const Args a, int merges_at) {
+__device__ __forceinline__ void packed_merge(const Args &a) {
   constexpr int VPR = D / 8, ROWS = 256 / VPR;
-  const Merge m = *(const Merge *)(a.words + merges_at + blockIdx.x * kMergeWords);
-  const int gkv = blockIdx.z, row = blockIdx.y * ROWS + threadIdx.x / VPR, dv = threadIdx.x % VPR, G = a.Hq / a.Hkv;
+  const Merge m = *(const Merge *)(a.words + a.merges_at + blockIdx.x * kMergeWords);
+  const int gkv = blockIdx.z, row = blockIdx.y * ROWS + threadIdx.x / VPR, dv = threadIdx.x % VPR;
   if (row >= m.rows) return;
   const size_t first = (size_t)gkv * a.part_rows + m.part + row;
   float top = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -890,12 +937,21 @@ __global__ __launch_bounds__(256) void packed_merge_kernel(const Args a, int mer
     }
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int r = m.r_first + row, i = r / G, head = gkv * G + r - i * G;
+  const auto [i, head] = row_at(a, m, gkv, row);
   bf16x8 v;
 #pragma unroll
   for (int d = 0; d < 8; ++d) v[d] = (__bf16)(acc[d] * inv);
   *(bf16x8 *)(a.out + ((size_t)m.row0 + i) * ((size_t)a.Hq * D) + (size_t)head * D + dv * 8) = v;
   if (a.lse && dv == 0) a.lse[(size_t)head * a.N + m.row0 + i] = pc::lse_of(top, l);
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void packed_merge_kernel(const Args a) { packed_merge<D>(a); }
+template <int D>
+__global__ __launch_bounds__(256) void packed_merge_words_kernel(const ArgsAndWords w) {
+  Args a = w.a;
+  a.words = words_of_launch();
+  packed_merge<D>(a);
 }
 
 // ---------------------------------------------------------------- host side
@@ -938,7 +994,11 @@ struct Plan {
 void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int stride, const int32_t *start, int n_seq, int n_splits, const PackedWs &ws, Plan &plan) {
   const percache_config &c = ctx->cfg;
   const int G = c.n_q_heads / c.n_kv_heads;
-  struct Block { int seq, r_first, rows, kind, tiles; float cost; };
+  struct Block { int seq, r_first, rows, kind, tiles, n; };   // n: partitions
+  // us of a workgroup's start and end, and of a tile (most of the chip at work; wide ones alone 1.45 at head size 128), us of a MB from memory
+  constexpr float kStart = 6.f, kPerMb = 1.f / 5.4f;
+  const float tile_us[2] = {c.head_dim == 128 ? 1.85f : 1.28f, c.head_dim == 128 ? 0.72f : 0.5f};
+  auto cost_of = [&](const Block &b, int tiles) { return kStart + tile_us[b.kind] * (float)tiles; };
   std::vector<Block> blocks;
   std::vector<int32_t> ents, first_ent(n_seq + 1), tiles_before;   // entries with keys; cached tiles before each
   std::vector<int> cached(n_seq);
@@ -965,7 +1025,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
       for (int r = 0; r < R;) {
         const int rows = std::min(R - r, R - r <= kNarrowRows ? kNarrowRows : height), kind = rows <= kNarrowRows ? kNarrow : kWide;
         const int tiles = cached[s] + ((r + rows - 1) / G) / TK + 1;
-        blocks.push_back({s, r, rows, kind, tiles, (kind == kWide ? 1.f : 0.4f) * (float)tiles + 2.f});
+        blocks.push_back({s, r, rows, kind, tiles, 1});
         r += rows;
       }
     }
@@ -978,30 +1038,80 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   }
   cut(wide * c.n_kv_heads * 2 <= ctx->n_cu && narrow * c.n_kv_heads <= 2L * ctx->n_cu ? kNarrowRows : kWideRows);
 
-  float work = 0.f, longest = 0.f;
-  for (const Block &b : blocks) {
-    work += b.cost;
-    longest = std::max(longest, b.cost);
+  // Partitions: blocks that take longer than a limit, one for each kind, are cut evenly.  A launch is dealt out longest first to the CUs, of which every kv head
+  // gets its share; that is played through for limits from the longest block's time down (while there are few workgroups a CU: many even out by themselves),
+  // and a limit that promises 3 % is taken.  Nothing is faster than its keys come from memory; a merge is a launch and the partial rows.  us at 1, 2, 3, 4
+  // partitions, measured: 72 wide blocks of 60 tiles 95, 64, 53, 60; head size 64, 152 of 36 to 60 tiles 84, 80, 70; 144 narrow ones of 52 tiles 53, 62, 53,
+  // 59, 32 of them 48, 32, 24, 22, 200 wide ones of 50 to 60 tiles beside the 144 134 (cut evenly into 712 workgroups 151).
+  auto parts_of = [&](const Block &x, const float (&limit)[2]) {
+    const int least = x.kind == kWide ? 6 : 4;   // tiles of a partition
+    return std::max(1, std::min({(int)(tile_us[x.kind] * (float)x.tiles / std::max(limit[x.kind] - kStart, 1.f) + 0.99f), x.tiles / least, kMaxPackedSplits}));
+  };
+  const int cus = std::max(1, ctx->n_cu / c.n_kv_heads);
+  if (n_splits > 0) {
+    for (Block &x : blocks) x.n = std::min(n_splits, x.tiles);
+  } else if ((long)blocks.size() <= 8L * cus) {
+    float longest[2] = {0.f, 0.f}, mb = 0.f;
+    for (const Block &x : blocks) longest[x.kind] = std::max(longest[x.kind], cost_of(x, x.tiles));
+    for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
+    std::vector<float> costs, free_at(cus);
+    float best = 1e30f, best_limit[2] = {longest[kWide], longest[kNarrow]};
+    const float top = std::max(longest[kWide], longest[kNarrow]);
+    const bool both = longest[kWide] > 0.f && longest[kNarrow] > 0.f;
+    bool any = false, open = true;   // whether a block can be cut; whether finer limits can still be better: their workgroups' time only grows
+    for (const Block &x : blocks) any |= x.tiles >= (x.kind == kWide ? 12 : 8);
+    for (float cut = 1.f; any && open && cut <= (float)kMaxPackedSplits; cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
+      for (float cut2 = 1.f; cut2 <= (both ? 2.f : 1.f); cut2 *= 2.f) {
+        const float wide = kStart + (top - kStart) / cut, limit[2] = {wide, std::min(wide, kStart + (longest[kNarrow] - kStart) / cut2)};
+        float rows = 0.f, sum = 0.f;
+        costs.clear();
+        for (const Block &x : blocks) {
+          const int n = parts_of(x, limit);
+          const float each = kStart + tile_us[x.kind] * (float)x.tiles / (float)n;
+          costs.insert(costs.end(), n, each);
+          sum += each * (float)n;
+          if (n > 1) rows += (float)(n * x.rows);
+        }
+        const float more = rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f;
+        if (std::max(sum / (float)cus, mb * kPerMb) + more >= 0.97f * best) {
+          open = cut2 > 1.f && open;
+          continue;
+        }
+        std::sort(costs.begin(), costs.end(), [](float x, float y) { return x > y; });
+        std::fill(free_at.begin(), free_at.end(), 0.f);   // (a heap, the CU that is free first at its head)
+        float end = 0.f;
+        for (const float us : costs) {
+          std::pop_heap(free_at.begin(), free_at.end(), std::greater<float>());
+          free_at.back() += us;
+          end = std::max(end, free_at.back());
+          std::push_heap(free_at.begin(), free_at.end(), std::greater<float>());
+        }
+        const float us = std::max(end, mb * kPerMb) + more;
+        if (us < 0.97f * best) {
+          best = us;
+          best_limit[kWide] = limit[kWide];
+          best_limit[kNarrow] = limit[kNarrow];
+        }
+      }
+    if (any)
+      for (Block &x : blocks) x.n = parts_of(x, best_limit);
   }
-  const float share = work * c.n_kv_heads / ctx->n_cu;   // of a CU
-  const float limit = longest <= 0.6f * share ? longest : 0.6f * share;
   struct Unit { int block, begin, end; float cost; int part; };
   std::vector<Unit> units;
   long part_rows = 0, more = ws.most_items - (long)blocks.size();
   for (int b = 0; b < (int)blocks.size(); ++b) {
     const Block &x = blocks[b];
-    const int least = x.kind == kWide ? 8 : 4;   // tiles of a partition
-    int n = n_splits > 0 ? std::min(n_splits, x.tiles) : std::max(1, std::min({(int)(x.cost / limit + 0.999f), x.tiles / least, kMaxPackedSplits}));
+    int n = x.n;
     if (n - 1 > more || part_rows + (long)n * x.rows > ws.part_rows) n = 1;
     if (n > 1) {
-      const Merge m = {start[x.seq], x.r_first, x.rows, (int32_t)part_rows, n};
+      const Merge m = {start[x.seq], x.r_first / G, x.r_first % G, x.rows, (int32_t)part_rows, n};
       plan.words.insert(plan.words.end(), (const int32_t *)&m, (const int32_t *)&m + kMergeWords);
       ++plan.n_merges;
       plan.tallest = std::max(plan.tallest, x.rows);
     }
     for (int p = 0; p < n; ++p) {
       const int begin = (int)((long)p * x.tiles / n), end = (int)((long)(p + 1) * x.tiles / n);
-      units.push_back({b, begin, end, x.cost * (float)(end - begin) / (float)x.tiles, n > 1 ? (int)part_rows + p * x.rows : -1});
+      units.push_back({b, begin, end, cost_of(x, end - begin), n > 1 ? (int)part_rows + p * x.rows : -1});
     }
     if (n > 1) part_rows += (long)n * x.rows;
     more -= n - 1;
@@ -1015,7 +1125,8 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     Item it = {};
     it.row0 = start[s];
     it.T = start[s + 1] - start[s];
-    it.r_first = x.r_first;
+    it.i0 = x.r_first / G;
+    it.rem0 = x.r_first % G;
     it.rows = x.rows;
     it.kind = x.kind;
     it.n_cached = std::max(0, std::min(u.end, cached[s]) - u.begin);
@@ -1084,9 +1195,13 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   Plan plan;
   plan_items(ctx, table, stride, start_host, n_seq, n_splits, ws, plan);
   hipStream_t s = (hipStream_t)stream;
-  st = pc::upload_table(ctx, plan.words, ws.words, s);
-  if (st != PC_OK) return st;
-  Args a = {};
+  const bool in_args = plan.words.size() <= (size_t)pc::kListWords;
+  if (!in_args) {
+    st = pc::upload_table(ctx, plan.words, ws.words, s);
+    if (st != PC_OK) return st;
+  }
+  ArgsAndWords aw;
+  Args &a = aw.a;
   a.q = (const __bf16 *)q_dev;
   a.k = (const __bf16 *)k_dev;
   a.v = (const __bf16 *)v_dev;
@@ -1104,16 +1219,22 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   a.part_ml = ws.part_ml;
   a.N = n_rows;
   a.part_rows = ws.part_rows;
-  a.n_items = plan.n_items;
+  a.merges_at = plan.merges_at;
   a.ents_at = plan.ents_at;
   a.Hq = c.n_q_heads;
   a.Hkv = c.n_kv_heads;
   a.C = c.slot_capacity;
   a.n_slots16 = ctx->n_slots16;
+  a.per_group = (unsigned)((0xffffffffull + c.n_q_heads / c.n_kv_heads) / (c.n_q_heads / c.n_kv_heads));
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)c.head_dim);
   const dim3 grid((unsigned)((long)plan.n_items * c.n_kv_heads));
   pc::prof_begin(ctx, PC_KERNEL_ATTENTION, s);
-#define PC_PACKED(DD, EE) hipLaunchKernelGGL((packed_attention_kernel<DD, EE>), grid, dim3(64 * NW), 0, s, a)
+  if (in_args) memcpy(aw.words, plan.words.data(), plan.words.size() * sizeof(int32_t));
+#define PC_PACKED(DD, EE)                                                                                                        \
+  do {                                                                                                                           \
+    if (in_args) hipLaunchKernelGGL((packed_attention_words_kernel<DD, EE>), grid, dim3(64 * NW), 0, s, aw);                      \
+    else hipLaunchKernelGGL((packed_attention_kernel<DD, EE>), grid, dim3(64 * NW), 0, s, a);                                     \
+  } while (0)
   if (c.head_dim == 128) { if (formats & 1) PC_PACKED(128, true); else PC_PACKED(128, false); }
   else { if (formats & 1) PC_PACKED(64, true); else PC_PACKED(64, false); }
 #undef PC_PACKED
@@ -1122,8 +1243,13 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   if (plan.n_merges) {
     const int per = 256 / (c.head_dim / 8);
     const dim3 mgrid((unsigned)plan.n_merges, (unsigned)((plan.tallest + per - 1) / per), (unsigned)c.n_kv_heads);
-    if (c.head_dim == 128) hipLaunchKernelGGL(packed_merge_kernel<128>, mgrid, dim3(256), 0, s, a, plan.merges_at);
-    else hipLaunchKernelGGL(packed_merge_kernel<64>, mgrid, dim3(256), 0, s, a, plan.merges_at);
+#define PC_MERGE(DD)                                                                                          \
+  do {                                                                                                        \
+    if (in_args) hipLaunchKernelGGL(packed_merge_words_kernel<DD>, mgrid, dim3(256), 0, s, aw);                \
+    else hipLaunchKernelGGL(packed_merge_kernel<DD>, mgrid, dim3(256), 0, s, a);                               \
+  } while (0)
+    if (c.head_dim == 128) PC_MERGE(128); else PC_MERGE(64);
+#undef PC_MERGE
     PC_HIP(ctx, hipGetLastError());
   }
   return PC_OK;
