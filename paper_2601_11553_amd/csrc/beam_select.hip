@@ -30,6 +30,31 @@ __device__ __forceinline__ float from_ordered(unsigned u) { return __uint_as_flo
 // larger logits first, equal ones by the lower token; 0 is below every logit that is one
 __device__ __forceinline__ u64 key_of(float x, unsigned token) { return ((u64)ordered(x + 0.f) << 32) | (0xffffffffu - token); }
 
+// over the 64 lanes: data-parallel moves inside 16 of them, then the rows change places
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true)); }
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {
+  const u64 u = (u64)__double_as_longlong(x);
+  const unsigned lo = __builtin_amdgcn_update_dpp(0, (unsigned)u, CTRL, 0xf, 0xf, true), hi = __builtin_amdgcn_update_dpp(0, (unsigned)(u >> 32), CTRL, 0xf, 0xf, true);
+  return __longlong_as_double((long long)(((u64)hi << 32) | lo));
+}
+template <class X, class Op>
+__device__ __forceinline__ X over_lanes(X x, Op op) {
+  x = op(x, moved<0xB1>(x));     // lane ^ 1
+  x = op(x, moved<0x4E>(x));     // lane ^ 2
+  x = op(x, moved<0x141>(x));    // mirrored inside 8
+  x = op(x, moved<0x140>(x));    // mirrored inside 16
+  x = op(x, __shfl_xor(x, 16, 64));
+  return op(x, __shfl_xor(x, 32, 64));
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return over_lanes(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ double wave_sum(double x) {
+  return over_lanes(x, [](double a, double b) { return a + b; });
+}
+
 // e^d for d <= 0.  The difference is taken before the product with log2(e): the sum of a row is compared to the last places of 32 bits, and a reference
 // multiplied beforehand would move every term of it by the same 2^-24 of the reference.
 __device__ __forceinline__ float exp_below(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
@@ -44,7 +69,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
   __shared__ float tops[kWaves];
   __shared__ double sums[kWaves];
   __shared__ u64 bound, next_best;
-  __shared__ int n_again, n_found;
+  __shared__ int n_found;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int row = blockIdx.x / n_stretch, stretch = blockIdx.x - row * n_stretch;
   const T *x = logits + (long)row * row_stride;
@@ -110,19 +135,8 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
   }
   least_of[tid] = least;
   if (tid == 0) {
-    n_again = n_found = 0;
+    n_found = 0;
     bound = ~0ull;
-  }
-  // the wavefront's maximum and sum, then the workgroup's
-  float top = m;
-#pragma unroll
-  for (int sh = 1; sh < 64; sh <<= 1) top = fmaxf(top, __shfl_xor(top, sh, 64));
-  double sum = m == -INFINITY ? (l == l ? 0.0 : (double)NAN) : (double)l * (double)exp_below(m - top);
-#pragma unroll
-  for (int sh = 1; sh < 64; sh <<= 1) sum += __shfl_xor(sum, sh, 64);
-  if (lane == 0) {
-    tops[wave] = top;
-    sums[wave] = sum;
   }
   __syncthreads();
   if (wave == 0) {
@@ -134,12 +148,6 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
 #pragma unroll 16
     for (int j = 0; j < 64; ++j) rank += found[j] > own;
     if (rank < best) atomicMin(&bound, own ? own : 1ull);   // (fewer than `best` groups with a token: every one of theirs reaches it)
-  } else if (tid == 64) {
-    float t = tops[0];
-    for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
-    double s = 0.0;
-    for (int w = 0; w < kWaves; ++w) s += tops[w] == -INFINITY ? (sums[w] == sums[w] ? 0.0 : sums[w]) : sums[w] * exp((double)tops[w] - (double)t);
-    st_out[blockIdx.x] = Stretch{s, t, 0};
   }
   __syncthreads();
   const u64 reach = bound;
@@ -147,25 +155,47 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
     const int at = atomicAdd(&n_found, 1);   // (in any order: they are counted against each other)
     if (at < kFound) found[at] = key;
   };
-  if (most >= reach) again[atomicAdd(&n_again, 1)] = (uint16_t)tid;
   const u64 tail_key = tail > -INFINITY ? key_of(tail, (unsigned)(tail0 + lane)) : 0ull;
-  __syncthreads();
-  // vector `item` of the lanes that are read again
-  const int each = (vecs / parts + 64) / 64, items = n_again * each;
-  auto reread = [&](int item, auto use) __attribute__((always_inline)) {
-    const int who = again[item / each], w = who >> 6, v = part_begin(w) + (who & 63) + item % each * 64;
-    if (v >= part_begin(w + 1)) return;
-    const u32x4_ raw = *(const vec_at *)(x + (long)v * PER);
-#pragma unroll
-    for (int e = 0; e < PER; ++e) {
-      const float y = value(raw, e);
-      if (y > -INFINITY) use(key_of(y, (unsigned)(v * PER + e)));
-    }
-  };
   if (tail_key >= reach) put(tail_key);
-  for (int item = tid; item < items; item += kThreads)
+  // this wavefront's lanes that are read again, vector by vector
+  const u64 mask = __builtin_amdgcn_ballot_w64(most >= reach);
+  if (most >= reach) again[wave * 64 + __popcll(mask & ((1ull << lane) - 1))] = (uint16_t)lane;
+  __builtin_amdgcn_wave_barrier();
+  const int each = (v1 - v0 + 63) / 64, items = __popcll(mask) * each;
+  auto reread = [&](int item0, auto use) __attribute__((always_inline)) {   // two of them
+    u32x4_ raw[2];
+    int v[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int item = item0 + 64 * j, i = item / each;
+      v[j] = item < items ? v0 + again[wave * 64 + i] + (item - i * each) * 64 : v1;
+      raw[j] = *(const vec_at *)(x + (long)min(v[j], v1 - 1) * PER);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        const float y = value(raw[j], e);
+        if (v[j] < v1 && y > -INFINITY) use(key_of(y, (unsigned)(v[j] * PER + e)));
+      }
+  };
+  for (int item = lane; item < items; item += 128)
     reread(item, [&](u64 key) __attribute__((always_inline)) { if (key >= reach) put(key); });
+  // the wavefront's maximum and sum
+  const float top = wave_max(m);
+  const double sum = wave_sum(m == -INFINITY ? (l == l ? 0.0 : (double)NAN) : (double)l * (double)exp_below(m - top));
+  if (lane == 0) {
+    tops[wave] = top;
+    sums[wave] = sum;
+  }
   __syncthreads();
+  if (tid == kThreads - 1) {
+    float t = tops[0];
+    for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
+    double s = 0.0;
+    for (int w = 0; w < kWaves; ++w) s += tops[w] == -INFINITY ? (sums[w] == sums[w] ? 0.0 : sums[w]) : sums[w] * exp((double)tops[w] - (double)t);
+    st_out[blockIdx.x] = Stretch{s, t, 0};
+  }
   const int count = n_found;
   u64 *out = list_out + (size_t)blockIdx.x * best;
   if (count <= kFound) {
@@ -184,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
     if (tid == 0) next_best = 0;
     __syncthreads();
     u64 own = tail_key < before ? tail_key : 0ull;
-    for (int item = tid; item < items; item += kThreads)
+    for (int item = lane; item < items; item += 128)
       reread(item, [&](u64 key) __attribute__((always_inline)) { own = key < before && key > own ? key : own; });
     atomicMax(&next_best, own);
     __syncthreads();
@@ -230,12 +260,9 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(const Stretch *
       top = t;
     }
     if (n_stretch > 1) {
-      float t = top;
-#pragma unroll
-      for (int sh = 1; sh < 64; sh <<= 1) t = fmaxf(t, __shfl_xor(t, sh, 64));
+      const float t = wave_max(top);
       if (top != -INFINITY) sum *= exp((double)top - (double)t);
-#pragma unroll
-      for (int sh = 1; sh < 64; sh <<= 1) sum += __shfl_xor(sum, sh, 64);
+      sum = wave_sum(sum);
       top = t;
     }
     if (lane == 0) {
