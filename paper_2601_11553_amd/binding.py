@@ -685,26 +685,32 @@ class Percache:
         if pos.dim() == 1:
             pos = pos[None]
         self._want("pos", pos, (pos.shape[0], n), torch.int32)
+        axis_p = None
         if axis is not None:
-            axis = np.ascontiguousarray(axis, np.uint8).reshape(-1)
+            if type(axis) is not np.ndarray or axis.dtype != np.uint8 or not axis.flags.c_contiguous:
+                axis = np.ascontiguousarray(axis, np.uint8)
             if axis.size != D // 2:
                 raise ValueError(f"axis: {axis.size} entries for {D // 2} pairs")
+            axis_p = axis.__array_interface__["data"][0]
         self._want("qkv_bias", qkv_bias, (F,), bf16)
         self._want("q_norm", q_norm, (D,), bf16)
         self._want("k_norm", k_norm, (D,), bf16)
-        outs = []
-        for name, t, h in (("q_out", q_out, Hq), ("k_out", k_out, Hkv), ("v_out", v_out, Hkv)):
-            if t is None:
-                t = torch.empty((h, n, D), dtype=bf16, device=self.device)
-            else:
-                self._want(name, t, (h, n, D), bf16)
-            outs.append(t)
+        if q_out is None:
+            q_out = qkv.new_empty((Hq, n, D))
+        else:
+            self._want("q_out", q_out, (Hq, n, D), bf16)
+        if k_out is None:
+            k_out = qkv.new_empty((Hkv, n, D))
+        else:
+            self._want("k_out", k_out, (Hkv, n, D), bf16)
+        if v_out is None:
+            v_out = qkv.new_empty((Hkv, n, D))
+        else:
+            self._want("v_out", v_out, (Hkv, n, D), bf16)
         # (a single row has no stride of its own)
-        st = self.lib.percache_qkv_norm_rope(self.ctx, qkv.data_ptr(), qkv.stride(0) if n > 1 else F, n, pos.data_ptr(), pos.shape[0],
-                                             None if axis is None else axis.ctypes.data, _ptr(qkv_bias), _ptr(q_norm), _ptr(k_norm), eps, outs[0].data_ptr(),
-                                             outs[1].data_ptr(), outs[2].data_ptr(), self._raw_stream())
-        self._check(st)
-        return tuple(outs)
+        self._check(self.lib.percache_qkv_norm_rope(self.ctx, qkv.data_ptr(), qkv.stride(0) if n > 1 else F, n, pos.data_ptr(), pos.shape[0], axis_p, _ptr(qkv_bias),
+                                                    _ptr(q_norm), _ptr(k_norm), eps, q_out.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), self._raw_stream()))
+        return q_out, k_out, v_out
 
     def percache_attention_packed(self, layer, q, k, v, start, slot_ids=None, used_len=None, n_chunks=None, n_splits: int = 0, attn_out=None, lse_out=None):
         """(attn_out [N, Hq * D], lse [Hq, N] or None) of packed rows q [Hq, N, D], k, v [Hkv, N, D]; start: the requests' first rows and the end of the
@@ -723,7 +729,7 @@ class Percache:
             raise ValueError("start: the first row of every request and the end of the last one are wanted")
         keep, ids_p, ul_p, nc_p, max_chunks = self._draft_chunks(n_seq, slot_ids, used_len, n_chunks)
         if attn_out is None:
-            attn_out = torch.empty((n, Hq * D), dtype=bf16, device=self.device)
+            attn_out = q.new_empty((n, Hq * D))
         else:
             self._want("attn_out", attn_out, (n, Hq * D), bf16)
         if lse_out is True:
@@ -759,9 +765,8 @@ class Percache:
         if batch > 1 and beams > 1 and logits.stride(0) != beams * stride:
             raise ValueError(f"logits: rows at an even distance are wanted, got strides {logits.stride()}")
         self._want("scores", scores, (batch, beams), torch.float32)
-        parent = torch.empty((batch, best), dtype=torch.int32, device=self.device)
-        token = torch.empty((batch, best), dtype=torch.int32, device=self.device)
-        score = torch.empty((batch, best), dtype=torch.float32, device=self.device)
+        score = scores.new_empty((batch, best))
+        parent, token = (torch.empty((batch, best), dtype=torch.int32, device=self.device) for _ in range(2))
         stream = self._raw_stream()
         key = ("beams", batch, beams, vocab, best)
         need = self._draft_bytes.get(key)
