@@ -41,11 +41,15 @@ constexpr float kSumLimit4 = 4.f * 256.f;  // 4 of them
 constexpr int kMaxPackedSplits = 64;
 constexpr int kMoreItems = 16;             // items beyond one a block, per CU
 
-// A workgroup's work, for every kv head: `rows` stacked rows from head rem0 of token i0 of a request on, over n_cached cached tiles from tile tile0 of
+// A workgroup's work, for every kv head: rows() stacked rows from head rem0 of token i0 of a request on, over n_cached cached tiles from tile tile0 of
 // chunk entry ent on, then over the fresh tiles [f0, f1).
 struct Item {
-  int32_t row0, T, i0, rem0, rows, kind, n_cached, ent, n_ents, tile0, f0, f1;
-  int32_t part;   // first row of its partial results, -1: it is the block's only partition
+  int32_t row0, T, i0, n_cached, ent, tile0, f0, f1;
+  int32_t slot0, used0;     // entry ent: a workgroup's first tiles are asked for before its entries are there
+  int32_t part;             // first row of its partial results, -1: it is the block's only partition
+  uint16_t rem0, rows_kind; // rows * 2 + kind
+  __host__ __device__ int rows() const { return rows_kind >> 1; }
+  __host__ __device__ int kind() const { return rows_kind & 1; }
 };
 constexpr int kItemWords = sizeof(Item) / 4;
 struct Merge { int32_t row0, i0, rem0, rows, part, n; };   // partition p of the block has its partial rows from part + p * rows on
@@ -61,15 +65,16 @@ struct Args {
   float *lse;                // [Hq][N] or null
   float *part_o, *part_ml;   // [part_rows of every kv head][D], [...][2]
   long N, part_rows;
-  int merges_at, ents_at, Hq, Hkv, C, n_slots16;
+  int merges_at, ents_at, n_ents, Hq, Hkv, C, n_slots16;
   unsigned per_group;        // 2^32 / G, rounded up: x / G = the upper half of x times it for the small x of a block
   float scale_log2e;
 };
 
 // Lists that fit a launch's arguments are read from there: no launch in front that copies them.
+constexpr int kArgWords = (4096 - (int)sizeof(Args)) / 4;
 struct ArgsAndWords {
   Args a;
-  int32_t words[pc::kListWords];
+  int32_t words[kArgWords];
 };
 static_assert(sizeof(ArgsAndWords) <= 4096, "the arguments of a launch");
 __device__ __forceinline__ const int32_t *words_of_launch() {
@@ -152,21 +157,20 @@ struct Walk {
   __device__ __forceinline__ Walk(const Args &a_, const Item &it_, int gkv_, int lane_) : a(a_), it(it_), gkv(gkv_), lane(lane_) {
     load();
     if (it.n_cached > 0) {
-      enter();
+      enter(it.slot0, it.used0);
       skip(it.tile0);
     }
   }
-  __device__ __forceinline__ void load() {   // the 64 entries from ent on
+  __device__ __forceinline__ void load() {   // the 64 entries from ent on (of other requests behind the last one's)
     my_slot = my_used = 0;
-    if (ent + lane < it.n_ents) {
+    if (it.ent + ent + lane < a.n_ents) {
       const int2 e = *(const int2 *)(a.words + a.ents_at + 2 * (it.ent + ent + lane));
       my_slot = e.x;
       my_used = e.y;
     }
   }
-  __device__ __forceinline__ void enter() {
-    const int slot = __builtin_amdgcn_readlane(my_slot, ent & 63);
-    left = __builtin_amdgcn_readlane(my_used, ent & 63);
+  __device__ __forceinline__ void enter(int slot, int used) {
+    left = used;
     at = 0;
     c8 = KV8 && slot >= a.n_slots16;
     const size_t sh = (size_t)(c8 ? slot - a.n_slots16 : slot) * a.Hkv + gkv, base = sh * a.C * D;
@@ -201,7 +205,7 @@ struct Walk {
       if (left <= 0 && idx + 1 < it.n_cached) {
         ++ent;
         if ((ent & 63) == 0) load();
-        enter();
+        enter(__builtin_amdgcn_readlane(my_slot, ent & 63), __builtin_amdgcn_readlane(my_used, ent & 63));
       }
     } else {
       const int f = it.f0 + idx - it.n_cached;
@@ -289,11 +293,11 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, g2 = lane >> 5;
 
   const int local = wave * 32 + l32;
-  const bool row_ok = local < it.rows;
-  const RowAt mine = row_at(a, it, gkv, min(local, it.rows - 1));
+  const bool row_ok = local < it.rows();
+  const RowAt mine = row_at(a, it, gkv, min(local, it.rows() - 1));
   const int my_i = mine.i, head = mine.head;
   // first and last token among this wavefront's rows: a fresh tile that reaches past the first is masked, one that starts behind the last skipped
-  const bool wave_live = wave * 32 < it.rows;
+  const bool wave_live = wave * 32 < it.rows();
   const int i_lo = __builtin_amdgcn_readlane(my_i, 0), i_hi = __builtin_amdgcn_readlane(my_i, 31);
 
   bf16x8 qf[KS];
@@ -369,11 +373,10 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
     store16(vb + ((4 * (cv_m >> 1) + 2 + (cv_m & 1)) ^ sv) * 16, codes16(vc[2], vc[3], t.vs));
   };
 
-  int k_rd[KS], vb_rd[4], vf_rd[DB];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) k_rd[ks] = ((2 * ks + g2) ^ swz(L::K_ROW, l32)) * 16 + l32 * L::K_ROW;
-#pragma unroll
-  for (int c4 = 0; c4 < 4; ++c4) vb_rd[c4] = ((2 * c4 + g2) ^ swz(L::VB_ROW, l32)) * 16 + l32 * L::VB_ROW;
+  // Operand reads: chunk 2 j + g2 of row l32, swizzled, for j = 0, 1, ...: the first one's address with j in bits 5 and up the other way round.  Kept, or, where
+  // registers are short (a tile of codes in flight), formed at each read.
+  const int k_rd0 = (g2 ^ swz(L::K_ROW, l32)) * 16 + l32 * L::K_ROW, vb_rd0 = (g2 ^ swz(L::VB_ROW, l32)) * 16 + l32 * L::VB_ROW;
+  int vf_rd[DB];
   {
     const int key = 4 * g2 + ((l32 & 15) >> 2);
 #pragma unroll
@@ -383,6 +386,8 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
   auto tile = [&](int st, const Tile &t, auto fresh_c) __attribute__((always_inline)) {
     constexpr bool FRESH = decltype(fresh_c)::value;
     const char *kb = lds + st * L::STAGE, *vb = kb + L::HALF;
+    int k_rd = k_rd0, vb_rd = vb_rd0;
+    if (KV8) asm volatile("" : "+v"(k_rd), "+v"(vb_rd));
     f32x16 s_acc[2];
 #pragma unroll
     for (int kbk = 0; kbk < 2; ++kbk)
@@ -394,7 +399,7 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
 #pragma unroll
       for (int k4 = 0; k4 < 4; ++k4)
 #pragma unroll
-        for (int kbk = 0; kbk < 2; ++kbk) kop[kbk][k4] = *(const bf16x8 *)(kb + kbk * 32 * L::K_ROW + k_rd[4 * h + k4]);
+        for (int kbk = 0; kbk < 2; ++kbk) kop[kbk][k4] = *(const bf16x8 *)(kb + kbk * 32 * L::K_ROW + (k_rd ^ (4 * h + k4) * 32));
 #pragma unroll
       for (int k4 = 0; k4 < 4; ++k4)
 #pragma unroll
@@ -416,7 +421,7 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
             u.p[1] = read_turned(vb + (16 * c4 + 8) * L::K_ROW + vf_rd[db]);
             vop[half][db][c2] = u.v;
           } else {
-            vop[half][db][c2] = *(const bf16x8 *)(vb + db * 32 * L::VB_ROW + vb_rd[c4]);
+            vop[half][db][c2] = *(const bf16x8 *)(vb + db * 32 * L::VB_ROW + (vb_rd ^ c4 * 32));
           }
         }
     };
@@ -564,12 +569,21 @@ __device__ __forceinline__ void wide_item(const Args &a, const Item &it, int gkv
   if (row_ok && !(again >> l32 & 1)) {
     if (it.part < 0) {
       __bf16 *orow = a.out + ((size_t)it.row0 + my_i) * ((size_t)a.Hq * D) + (size_t)head * D;
+      // (lane l has elements 8 x + 0..3, lane l + 32 elements 8 x + 4..7: for every two x they change halves and store 16 bytes each)
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4)
-          *(bf16x4 *)(orow + db * 32 + q4 * 8 + g2 * 4) = bf16x4{(__bf16)(o_acc[db][q4 * 4] * inv), (__bf16)(o_acc[db][q4 * 4 + 1] * inv),
-                                                                 (__bf16)(o_acc[db][q4 * 4 + 2] * inv), (__bf16)(o_acc[db][q4 * 4 + 3] * inv)};
+        for (int h = 0; h < 2; ++h) {
+          typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+          uint2 w[2];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int at = (2 * h + x) * 4;
+            w[x] = __builtin_bit_cast(uint2, bf16x4{(__bf16)(o_acc[db][at] * inv), (__bf16)(o_acc[db][at + 1] * inv), (__bf16)(o_acc[db][at + 2] * inv), (__bf16)(o_acc[db][at + 3] * inv)});
+          }
+          const u32x2 lo = __builtin_amdgcn_permlane32_swap(w[0].x, w[1].x, false, false), hi = __builtin_amdgcn_permlane32_swap(w[0].y, w[1].y, false, false);
+          *(u32x4 *)(orow + db * 32 + h * 16 + g2 * 8) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+        }
       if (a.lse && g2 == 0) a.lse[(size_t)head * a.N + it.row0 + my_i] = pc::lse_of(m_ref, l_tot);
     } else {
       const size_t prow = (size_t)gkv * a.part_rows + it.part + local;
@@ -601,7 +615,7 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
   bf16x8 q[NR][KS];
 #pragma unroll
   for (int x = 0; x < NR; ++x) {
-    const RowAt r = row_at(a, it, gkv, min(x * 16 + l16, it.rows - 1));
+    const RowAt r = row_at(a, it, gkv, min(x * 16 + l16, it.rows() - 1));
     my_i[x] = r.i;
     const __bf16 *p = a.q + ((size_t)r.head * a.N + it.row0 + r.i) * D + g * 8;
 #pragma unroll
@@ -821,9 +835,9 @@ __device__ __forceinline__ void narrow_item(const Args &a, const Item &it, int g
 #pragma unroll
   for (int w = 0; w < NW; ++w) spoilt += tl[w];
   const bool any_tainted = __builtin_amdgcn_ballot_w64(spoilt != 0.f) != 0;
-  for (int u0 = wave * 64; u0 < it.rows * VPR; u0 += 64 * NW) {
-    const int u = u0 + lane, row = min(u / VPR, it.rows - 1), dv = u % VPR;
-    const bool live = u < it.rows * VPR;
+  for (int u0 = wave * 64; u0 < it.rows() * VPR; u0 += 64 * NW) {
+    const int u = u0 + lane, row = min(u / VPR, it.rows() - 1), dv = u % VPR;
+    const bool live = u < it.rows() * VPR;
     float m = -INFINITY, l = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     const float2 *const mlr = (const float2 *)ml + row;
 #pragma unroll
@@ -886,8 +900,8 @@ __device__ __forceinline__ void packed_item(const Args &a) {
     for (int i = 0; i < kItemWords; ++i) w[i] = __builtin_amdgcn_readfirstlane(src[i]);
     it = __builtin_bit_cast(Item, w);
   }
-  if (it.kind == kWide) wide_item<D, KV8>(a, it, gkv, lds);
-  else if (it.rows <= 16) narrow_item<D, KV8, 1>(a, it, gkv, lds);
+  if (it.kind() == kWide) wide_item<D, KV8>(a, it, gkv, lds);
+  else if (it.rows() <= 16) narrow_item<D, KV8, 1>(a, it, gkv, lds);
   else narrow_item<D, KV8, 2>(a, it, gkv, lds);
 }
 template <int D, bool KV8>
@@ -1054,7 +1068,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     float longest[2] = {0.f, 0.f}, mb = 0.f;
     for (const Block &x : blocks) longest[x.kind] = std::max(longest[x.kind], cost_of(x, x.tiles));
     for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
-    std::vector<float> costs, free_at(cus);
+    std::vector<float> costs, free_at;
     float best = 1e30f, best_limit[2] = {longest[kWide], longest[kNarrow]};
     const float top = std::max(longest[kWide], longest[kNarrow]);
     const bool both = longest[kWide] > 0.f && longest[kNarrow] > 0.f;
@@ -1063,13 +1077,14 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     for (float cut = 1.f; any && open && cut <= (float)kMaxPackedSplits; cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
       for (float cut2 = 1.f; cut2 <= (both ? 2.f : 1.f); cut2 *= 2.f) {
         const float wide = kStart + (top - kStart) / cut, limit[2] = {wide, std::min(wide, kStart + (longest[kNarrow] - kStart) / cut2)};
-        float rows = 0.f, sum = 0.f;
+        float rows = 0.f, sum = 0.f, end = 0.f;
         costs.clear();
         for (const Block &x : blocks) {
           const int n = parts_of(x, limit);
           const float each = kStart + tile_us[x.kind] * (float)x.tiles / (float)n;
           costs.insert(costs.end(), n, each);
           sum += each * (float)n;
+          end = std::max(end, each);
           if (n > 1) rows += (float)(n * x.rows);
         }
         const float more = rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f;
@@ -1077,14 +1092,16 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
           open = cut2 > 1.f && open;
           continue;
         }
-        std::sort(costs.begin(), costs.end(), [](float x, float y) { return x > y; });
-        std::fill(free_at.begin(), free_at.end(), 0.f);   // (a heap, the CU that is free first at its head)
-        float end = 0.f;
-        for (const float us : costs) {
-          std::pop_heap(free_at.begin(), free_at.end(), std::greater<float>());
-          free_at.back() += us;
-          end = std::max(end, free_at.back());
-          std::push_heap(free_at.begin(), free_at.end(), std::greater<float>());
+        if ((int)costs.size() > cus) {
+          std::sort(costs.begin(), costs.end(), std::greater<float>());
+          free_at.assign(costs.begin(), costs.begin() + cus);   // (a heap, the CU that is free first at its head)
+          std::make_heap(free_at.begin(), free_at.end(), std::greater<float>());
+          for (size_t i = cus; i < costs.size(); ++i) {
+            std::pop_heap(free_at.begin(), free_at.end(), std::greater<float>());
+            free_at.back() += costs[i];
+            end = std::max(end, free_at.back());
+            std::push_heap(free_at.begin(), free_at.end(), std::greater<float>());
+          }
         }
         const float us = std::max(end, mb * kPerMb) + more;
         if (us < 0.97f * best) {
@@ -1126,19 +1143,18 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     it.row0 = start[s];
     it.T = start[s + 1] - start[s];
     it.i0 = x.r_first / G;
-    it.rem0 = x.r_first % G;
-    it.rows = x.rows;
-    it.kind = x.kind;
+    it.rem0 = (uint16_t)(x.r_first % G);
+    it.rows_kind = (uint16_t)(x.rows * 2 + x.kind);
     it.n_cached = std::max(0, std::min(u.end, cached[s]) - u.begin);
     it.f0 = std::max(0, u.begin - cached[s]);
     it.f1 = std::max(it.f0, u.end - cached[s]);
     it.part = u.part;
     if (it.n_cached > 0) {
       const int first = (int)(std::upper_bound(tiles_before.begin() + e0, tiles_before.begin() + e1, u.begin) - tiles_before.begin()) - 1;
-      const int last = (int)(std::upper_bound(tiles_before.begin() + e0, tiles_before.begin() + e1, u.begin + it.n_cached - 1) - tiles_before.begin()) - 1;
       it.ent = first;
-      it.n_ents = last - first + 1;
       it.tile0 = u.begin - tiles_before[first];
+      it.slot0 = ents[2 * first];
+      it.used0 = ents[2 * first + 1];
     }
     items.insert(items.end(), (const int32_t *)&it, (const int32_t *)&it + kItemWords);
   }
@@ -1176,6 +1192,7 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   for (int s = 0; s < n_seq; ++s)
     if (start_host[s + 1] < start_host[s]) return pc::fail(ctx, PC_EINVAL, "start[%d]=%d lies before start[%d]=%d", s + 1, start_host[s + 1], s, start_host[s]);
   if (start_host[n_seq] > n_rows) return pc::fail(ctx, PC_EINVAL, "start[%d]=%d lies behind the last of %d rows", n_seq, start_host[n_seq], n_rows);
+  if (c.n_q_heads / c.n_kv_heads > 65535) return pc::fail(ctx, PC_ESHAPE, "more than 65535 query heads a kv head");
   // (stacked rows of a request, and partial rows, are counted in 32 bits)
   if ((long)n_rows * c.n_q_heads >= (1L << 31)) return pc::fail(ctx, PC_ESHAPE, "%d rows of %d heads are 2^31 or more", n_rows, c.n_q_heads);
   const int cap = max_splits(c, ctx->n_cu, n_seq, n_rows);
@@ -1195,7 +1212,7 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   Plan plan;
   plan_items(ctx, table, stride, start_host, n_seq, n_splits, ws, plan);
   hipStream_t s = (hipStream_t)stream;
-  const bool in_args = plan.words.size() <= (size_t)pc::kListWords;
+  const bool in_args = plan.words.size() <= (size_t)kArgWords;
   if (!in_args) {
     st = pc::upload_table(ctx, plan.words, ws.words, s);
     if (st != PC_OK) return st;
@@ -1221,6 +1238,7 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   a.part_rows = ws.part_rows;
   a.merges_at = plan.merges_at;
   a.ents_at = plan.ents_at;
+  a.n_ents = (int)(plan.words.size() - plan.ents_at) / 2;
   a.Hq = c.n_q_heads;
   a.Hkv = c.n_kv_heads;
   a.C = c.slot_capacity;
