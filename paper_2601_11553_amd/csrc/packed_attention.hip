@@ -1009,11 +1009,11 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   const percache_config &c = ctx->cfg;
   const int G = c.n_q_heads / c.n_kv_heads;
   struct Block { int seq, r_first, rows, kind, tiles, n; };   // n: partitions
-  // us of a workgroup's start and end, and of a tile (most of the chip at work; wide ones alone 1.45 at head size 128), us of a MB from memory
+  // us of a workgroup's start and end, and of a tile (most of the chip at work: the clock falls; alone 1.45 at head size 128), us of a MB from memory
   constexpr float kStart = 6.f, kPerMb = 1.f / 5.4f;
-  const float tile_us[2] = {c.head_dim == 128 ? 1.85f : 1.28f, c.head_dim == 128 ? 0.72f : 0.5f};
-  auto cost_of = [&](const Block &b, int tiles) { return kStart + tile_us[b.kind] * (float)tiles; };
-  std::vector<Block> blocks;
+  const bool d128 = c.head_dim == 128;
+  auto tile_us = [&](const Block &b) { return b.kind == kWide ? (d128 ? 1.85f : 1.28f) : b.rows > 16 ? (d128 ? 0.88f : 0.52f) : d128 ? 0.72f : 0.45f; };
+  auto cost_of = [&](const Block &b, int tiles) { return kStart + tile_us(b) * (float)tiles; };
   std::vector<int32_t> ents, first_ent(n_seq + 1), tiles_before;   // entries with keys; cached tiles before each
   std::vector<int> cached(n_seq);
   for (int s = 0; s < n_seq; ++s) {
@@ -1031,9 +1031,8 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     cached[s] = tiles;
   }
   first_ent[n_seq] = (int)ents.size() / 2;
-  // Blocks of 256 rows, the last of a request narrow where 32 rows are left; all of them narrow while the whole call would leave half of the CUs idle.
-  auto cut = [&](int height) {
-    blocks.clear();
+  auto cut = [&](int height) {   // blocks of so many rows, the last of a request narrow where 32 rows are left
+    std::vector<Block> blocks;
     for (int s = 0; s < n_seq; ++s) {
       const int R = G * (start[s + 1] - start[s]);
       for (int r = 0; r < R;) {
@@ -1043,15 +1042,8 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
         r += rows;
       }
     }
+    return blocks;
   };
-  long narrow = 0, wide = 0;
-  for (int s = 0; s < n_seq; ++s) {
-    const long R = (long)G * (start[s + 1] - start[s]);
-    narrow += (R + kNarrowRows - 1) / kNarrowRows;
-    wide += (R + kWideRows - 1) / kWideRows;
-  }
-  cut(wide * c.n_kv_heads * 2 <= ctx->n_cu && narrow * c.n_kv_heads <= 2L * ctx->n_cu ? kNarrowRows : kWideRows);
-
   // Partitions: blocks that take longer than a limit, one for each kind, are cut evenly.  A launch is dealt out longest first to the CUs, of which every kv head
   // gets its share; that is played through for limits from the longest block's time down (while there are few workgroups a CU: many even out by themselves),
   // and a limit that promises 3 % is taken.  Nothing is faster than its keys come from memory; a merge is a launch and the partial rows.  us at 1, 2, 3, 4
@@ -1059,29 +1051,30 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   // 59, 32 of them 48, 32, 24, 22, 200 wide ones of 50 to 60 tiles beside the 144 134 (cut evenly into 712 workgroups 151).
   auto parts_of = [&](const Block &x, const float (&limit)[2]) {
     const int least = x.kind == kWide ? 6 : 4;   // tiles of a partition
-    return std::max(1, std::min({(int)(tile_us[x.kind] * (float)x.tiles / std::max(limit[x.kind] - kStart, 1.f) + 0.99f), x.tiles / least, kMaxPackedSplits}));
+    return std::max(1, std::min({(int)(tile_us(x) * (float)x.tiles / std::max(limit[x.kind] - kStart, 1.f) + 0.99f), x.tiles / least, kMaxPackedSplits}));
   };
   const int cus = std::max(1, ctx->n_cu / c.n_kv_heads);
-  if (n_splits > 0) {
-    for (Block &x : blocks) x.n = std::min(n_splits, x.tiles);
-  } else if ((long)blocks.size() <= 8L * cus) {
-    float longest[2] = {0.f, 0.f}, mb = 0.f;
-    for (const Block &x : blocks) longest[x.kind] = std::max(longest[x.kind], cost_of(x, x.tiles));
-    for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
-    std::vector<float> costs, free_at;
+  float mb = 0.f;
+  for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
+  std::vector<float> costs, free_at;
+  auto settle = [&](std::vector<Block> &blocks) {   // chooses the partitions; us
+    float longest[2] = {0.f, 0.f};
+    bool any = false, open = true;   // whether a block can be cut; whether finer limits can still be better: their workgroups' time only grows
+    for (const Block &x : blocks) {
+      longest[x.kind] = std::max(longest[x.kind], cost_of(x, x.tiles));
+      any |= x.tiles >= (x.kind == kWide ? 12 : 8);
+    }
     float best = 1e30f, best_limit[2] = {longest[kWide], longest[kNarrow]};
     const float top = std::max(longest[kWide], longest[kNarrow]);
     const bool both = longest[kWide] > 0.f && longest[kNarrow] > 0.f;
-    bool any = false, open = true;   // whether a block can be cut; whether finer limits can still be better: their workgroups' time only grows
-    for (const Block &x : blocks) any |= x.tiles >= (x.kind == kWide ? 12 : 8);
-    for (float cut = 1.f; any && open && cut <= (float)kMaxPackedSplits; cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
-      for (float cut2 = 1.f; cut2 <= (both ? 2.f : 1.f); cut2 *= 2.f) {
+    for (float cut = 1.f; open && cut <= (any ? (float)kMaxPackedSplits : 1.f); cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
+      for (float cut2 = 1.f; cut2 <= (any && both ? 2.f : 1.f); cut2 *= 2.f) {
         const float wide = kStart + (top - kStart) / cut, limit[2] = {wide, std::min(wide, kStart + (longest[kNarrow] - kStart) / cut2)};
         float rows = 0.f, sum = 0.f, end = 0.f;
         costs.clear();
         for (const Block &x : blocks) {
           const int n = parts_of(x, limit);
-          const float each = kStart + tile_us[x.kind] * (float)x.tiles / (float)n;
+          const float each = kStart + tile_us(x) * (float)x.tiles / (float)n;
           costs.insert(costs.end(), n, each);
           sum += each * (float)n;
           end = std::max(end, each);
@@ -1110,9 +1103,20 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
           best_limit[kNarrow] = limit[kNarrow];
         }
       }
-    if (any)
-      for (Block &x : blocks) x.n = parts_of(x, best_limit);
+    for (Block &x : blocks) x.n = parts_of(x, best_limit);
+    return best;
+  };
+  // Blocks of 256 rows; where few of them would find the chip half empty, 32 rows each may be the faster ones (few keys: more workgroups, less of a walk each)
+  // or not (many keys: eight times as many are walked).
+  std::vector<Block> blocks = cut(kWideRows);
+  const bool choose = n_splits <= 0 && (long)blocks.size() <= 8L * cus;
+  const float by_wide = choose ? settle(blocks) : 0.f;
+  if ((long)blocks.size() * 2 <= cus) {
+    std::vector<Block> low = cut(kNarrowRows);
+    if ((long)low.size() <= 2L * cus && (!choose || settle(low) < by_wide)) blocks = std::move(low);
   }
+  if (n_splits > 0)
+    for (Block &x : blocks) x.n = std::min(n_splits, x.tiles);
   struct Unit { int block, begin, end; float cost; int part; };
   std::vector<Unit> units;
   long part_rows = 0, more = ws.most_items - (long)blocks.size();
