@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
     if (v < v1) take(raw, v, std::false_type{});
   }
   // keys that the lane's best token is not below, and not above (0: it has none)
-  u64 least = m > -INFINITY ? key_of(m, (unsigned)((when + ROUND - 64 + lane) * PER + PER - 1)) : 0ull;
+  u64 least = m > -INFINITY ? key_of(m, (unsigned)(when + ROUND - 64 + lane) * PER + PER - 1) : 0ull;
   u64 most = m > -INFINITY ? key_of(m, (unsigned)((when + lane) * PER)) : 0ull;
   if (has_tail) {
     const float mn = fmaxf(m, tail), ref = mn == -INFINITY ? 0.f : mn;
@@ -323,8 +323,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(const Stretch *
 }
 
 // Stretches a row is cut into: four workgroups a CU (512 rows of 131072: 35.8, 33.6, 34.7 us at two, four, eight), none shorter than 2048 logits, and no more
-// candidates of a request than
-// beam_pick_kernel holds.
+// candidates of a request than beam_pick_kernel holds.
 int stretches_for(int n_cu, long rows, int beams, int vocab, int best) {
   long s = (4L * n_cu + rows - 1) / rows;
   if (s > vocab / 2048) s = vocab / 2048;
@@ -351,6 +350,7 @@ pc_status percache_beam_select(percache_ctx *ctx, const void *logits_dev, int32_
   if (beams * best > kPickMost) return pc::fail(ctx, PC_ESHAPE, "%d beams with %d best each are more than %d candidates", beams, best, kPickMost);
   if (vocab < 1) return pc::fail(ctx, PC_ESHAPE, "vocab must be positive");
   if (row_stride < vocab) return pc::fail(ctx, PC_EINVAL, "row stride %ld is shorter than a row of %d", (long)row_stride, vocab);
+  if ((long)batch * beams >= 1L << 23) return pc::fail(ctx, PC_ESHAPE, "2^23 rows or more");   // (a grid has fewer than 2^32 threads)
   if (batch == 0) return PC_OK;
   if (!logits_dev || !scores_dev || !parent_out_dev || !token_out_dev || !score_out_dev) return pc::fail(ctx, PC_EINVAL, "NULL tensor pointer");
   if ((uintptr_t)logits_dev % (fp32 ? 4 : 2) || ((uintptr_t)scores_dev | (uintptr_t)parent_out_dev | (uintptr_t)token_out_dev | (uintptr_t)score_out_dev) % 4)
@@ -362,7 +362,6 @@ pc_status percache_beam_select(percache_ctx *ctx, const void *logits_dev, int32_
   const int ns = stretches_for(ctx->n_cu, rows, beams, vocab, best);
   Stretch *st = (Stretch *)workspace_dev;
   u64 *lists = (u64 *)((char *)workspace_dev + pc::align_up((size_t)rows * ns * sizeof(Stretch)));
-  if (rows * ns >= (1L << 31)) return pc::fail(ctx, PC_ESHAPE, "more than 2^31 rows");
   hipStream_t s = (hipStream_t)stream;
   const dim3 grid((unsigned)(rows * ns));
   if (fp32) hipLaunchKernelGGL(beam_rows_kernel<float>, grid, dim3(64 * kWaves), 0, s, (const float *)logits_dev, (long)row_stride, vocab, ns, best, st, lists);

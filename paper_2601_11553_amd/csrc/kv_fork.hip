@@ -6,19 +6,14 @@
 // registers meanwhile.  Nothing is exchanged between threads and no workspace is needed.  What bounds it: the bytes, a source read once for all of
 // its copies (they are neighbours in the list), every copy written once.
 #include <algorithm>
+#include <exception>
 
-#include "percache_internal.hpp"
+#include "launch_lists.hpp"
 
 namespace {
 using pc::kKvTile;
 using pc::u32x4;
-
-constexpr int kMoves = 240;   // moves of a launch (its arguments are at most 4096 bytes)
-struct Move { int32_t src, dst, len; };   // slots of one store; dst -1: src into the registers; src -1: from them
-struct Moves {
-  Move m[kMoves];
-  uint16_t start[kMoves + 1];   // moves start[p] .. start[p + 1] depend on each other
-};
+using namespace pc::fork;
 
 // One workgroup copies a block of 64 tokens of one layer and kv head for one list of dependent moves.  ES: bytes per element.
 template <int D, int ES>
@@ -34,7 +29,7 @@ __global__ __launch_bounds__(256) void kv_fork_kernel(const Moves moves, int blo
   for (int at = first; at < end; ++at) {
     const Move m = moves.m[at];
     const int here = m.len - block * kKvTile;   // tokens of this block that are copied
-    if (here <= 0) continue;
+    if (here <= 0 || (m.src == m.dst && here >= kKvTile)) continue;   // (a slot that is cut: zeros behind its last token)
     if (m.src >= 0 && (m.src != held || m.len > held_len)) {
       const size_t base = (size_t)layer * layer_stride + (((size_t)m.src * Hkv + h) * C + (size_t)block * kKvTile) * (D * ES);
 #pragma unroll
@@ -74,7 +69,7 @@ __global__ __launch_bounds__(256) void kv_fork_kernel(const Moves moves, int blo
   }
 }
 
-// The moves of a call in an order in which no slot is written before it is read; lists[p] are moves that depend on each other (or share their source),
+// The moves of a call in an order in which no slot is written before the others have read it; lists[p] are moves that depend on each other (or share their source),
 // cut where a launch may end: atoms, none longer than a launch.
 typedef std::vector<std::vector<Move>> Atoms;
 void order_moves(const std::vector<Move> &all, int n_slots, std::vector<Atoms> &lists) {
@@ -87,7 +82,7 @@ void order_moves(const std::vector<Move> &all, int n_slots, std::vector<Atoms> &
   };
   for (int i = 0; i < n; ++i) {
     parent[find(all[i].src)] = find(all[i].dst);
-    ++readers[all[i].src];
+    readers[all[i].src] += all[i].src != all[i].dst;   // (a slot that is cut waits for the others that read it)
     writer[all[i].dst] = i;
   }
   for (int i = n - 1; i >= 0; --i) {
@@ -109,7 +104,7 @@ void order_moves(const std::vector<Move> &all, int n_slots, std::vector<Atoms> &
       const Move &m = all[ready[at]];
       atoms.push_back({m});
       done[ready[at]] = 1;
-      if (--readers[m.src] == 0 && writer[m.src] >= 0) ready.push_back(writer[m.src]);
+      if (m.src != m.dst && --readers[m.src] == 0 && writer[m.src] >= 0) ready.push_back(writer[m.src]);
     }
     for (int i = first_of[root]; i >= 0; i = next_of[i]) {   // what is left is a ring: every slot of it is read once and written once
       if (done[i]) continue;
@@ -141,14 +136,21 @@ void order_moves(const std::vector<Move> &all, int n_slots, std::vector<Atoms> &
   }
 }
 
-pc_status launch_moves(percache_ctx *ctx, bool eight, int layer0, int n_layers, const Moves &moves, int n_lists, int longest, hipStream_t s) {
+// A launch: lists of moves of one store, in layers whose copies are equally long.
+struct Launch {
+  int eight, layer0, n_layers, n_lists, n_moves, longest;
+  Moves moves;
+  int blocks() const { return (longest + kKvTile - 1) / kKvTile; }
+};
+pc_status launch_moves(percache_ctx *ctx, const Launch &x, hipStream_t s) {
   const percache_config &c = ctx->cfg;
-  const int blocks = (longest + kKvTile - 1) / kKvTile;
-  const dim3 grid((unsigned)(blocks * c.n_kv_heads * n_lists), (unsigned)n_layers);
+  const bool eight = x.eight;
+  const int blocks = x.blocks();
+  const dim3 grid((unsigned)((long)blocks * c.n_kv_heads * x.n_lists), (unsigned)x.n_layers);
   const long layer_bytes = eight ? (long)ctx->layer_stride8 : (long)ctx->layer_stride * 2, scales = (long)ctx->n_slots8 * c.n_kv_heads * (c.slot_capacity / kKvTile);
-  char *k = (eight ? (char *)ctx->k8_store : (char *)ctx->k_store) + layer0 * layer_bytes, *v = (eight ? (char *)ctx->v8_store : (char *)ctx->v_store) + layer0 * layer_bytes;
-  float *ks = ctx->k_scale + layer0 * scales, *vs = ctx->v_scale + layer0 * scales;
-#define PC_FORK(DD, EE) hipLaunchKernelGGL((kv_fork_kernel<DD, EE>), grid, dim3(256), 0, s, moves, blocks, c.n_kv_heads, c.slot_capacity, layer_bytes, scales, k, v, ks, vs)
+  char *k = (eight ? (char *)ctx->k8_store : (char *)ctx->k_store) + x.layer0 * layer_bytes, *v = (eight ? (char *)ctx->v8_store : (char *)ctx->v_store) + x.layer0 * layer_bytes;
+  float *ks = ctx->k_scale + x.layer0 * scales, *vs = ctx->v_scale + x.layer0 * scales;
+#define PC_FORK(DD, EE) hipLaunchKernelGGL((kv_fork_kernel<DD, EE>), grid, dim3(256), 0, s, x.moves, blocks, c.n_kv_heads, c.slot_capacity, layer_bytes, scales, k, v, ks, vs)
   if (c.head_dim == 128) { if (eight) PC_FORK(128, 1); else PC_FORK(128, 2); }
   else { if (eight) PC_FORK(64, 1); else PC_FORK(64, 2); }
 #undef PC_FORK
@@ -158,7 +160,7 @@ pc_status launch_moves(percache_ctx *ctx, bool eight, int layer0, int n_layers, 
 }  // namespace
 
 extern "C" pc_status percache_kv_fork(percache_ctx *ctx, int32_t layer0, int32_t n_layers, const int32_t *src_slots_host, const int32_t *dst_slots_host,
-                                      const int32_t *n_tokens_host, int32_t n, void *stream) {
+                                      const int32_t *n_tokens_host, int32_t n, void *stream) try {
   if (!ctx) return PC_EINVAL;
   const percache_config &c = ctx->cfg;
   if (n < 0 || (n > 0 && (!src_slots_host || !dst_slots_host))) return pc::fail(ctx, PC_EINVAL, "a slot list is NULL or n is negative");
@@ -178,11 +180,14 @@ extern "C" pc_status percache_kv_fork(percache_ctx *ctx, int32_t layer0, int32_t
     }
   }
   if (n == 0) return PC_OK;
-  hipStream_t s = (hipStream_t)stream;
   auto len_of = [&](int l, int i) { return n_tokens_host ? n_tokens_host[i] : ctx->slot_len[(size_t)l * c.n_slots + src_slots_host[i]]; };
+  // (all launches are put together before the first of them)
+  constexpr long kMostBlocks = 1L << 23;   // of a launch: a grid has fewer than 2^32 threads
+  std::vector<Launch> launches;
+  std::vector<int32_t> lens(n);
   for (int l0 = layer0; l0 < layer0 + n_layers;) {
     int l1 = l0 + 1;   // layers whose copies are equally long share their launches
-    for (bool same = true; same && l1 < layer0 + n_layers;) {
+    for (bool same = true; same && l1 < layer0 + n_layers && l1 - l0 < 65535;) {
       for (int i = 0; same && i < n; ++i) same = len_of(l1, i) == len_of(l0, i);
       l1 += same;
     }
@@ -190,46 +195,44 @@ extern "C" pc_status percache_kv_fork(percache_ctx *ctx, int32_t layer0, int32_t
       std::vector<Move> all;
       const int off = eight ? ctx->n_slots16 : 0;
       for (int i = 0; i < n; ++i)
-        if ((int)ctx->is8(src_slots_host[i]) == eight && src_slots_host[i] != dst_slots_host[i])
+        if ((int)ctx->is8(src_slots_host[i]) == eight && (src_slots_host[i] != dst_slots_host[i] || (n_tokens_host && n_tokens_host[i] % kKvTile)))
           all.push_back({src_slots_host[i] - off, dst_slots_host[i] - off, len_of(l0, i)});
       if (all.empty()) continue;
       std::vector<Atoms> lists;
       order_moves(all, eight ? ctx->n_slots8 : ctx->n_slots16, lists);
-      Moves moves;
-      int n_moves = 0, n_lists = 0, longest = 0;
-      auto flush = [&]() {
-        if (!n_moves) return PC_OK;
-        moves.start[n_lists] = (uint16_t)n_moves;
-        const pc_status st = launch_moves(ctx, eight, l0, l1 - l0, moves, n_lists, longest, s);
-        n_moves = n_lists = longest = 0;
-        return st;
-      };
+      const size_t first = launches.size();
       for (const Atoms &atoms : lists) {
         bool open = false;
         for (const std::vector<Move> &atom : atoms) {
-          if (n_moves + (int)atom.size() > kMoves) {
-            const pc_status st = flush();
-            if (st != PC_OK) return st;
+          const bool fits = launches.size() > first && launches.back().n_moves + (int)atom.size() <= kMoves &&
+                            (open || (launches.back().n_lists + 1L) * ((c.slot_capacity + kKvTile - 1) / kKvTile) * c.n_kv_heads <= kMostBlocks);
+          if (!fits) {
+            launches.push_back({eight, l0, l1 - l0, 0, 0, 0, {}});
             open = false;
           }
-          if (!open) moves.start[n_lists++] = (uint16_t)n_moves;
+          Launch &x = launches.back();
+          if (!open) x.moves.start[x.n_lists++] = (uint16_t)x.n_moves;
           open = true;
           for (const Move &m : atom) {
-            moves.m[n_moves++] = m;
-            longest = std::max(longest, (int)m.len);
+            x.moves.m[x.n_moves++] = m;
+            x.longest = std::max(x.longest, (int)m.len);
           }
+          x.moves.start[x.n_lists] = (uint16_t)x.n_moves;
         }
       }
-      const pc_status st = flush();
-      if (st != PC_OK) return st;
     }
     l0 = l1;
   }
+  for (const Launch &x : launches) {
+    const pc_status st = launch_moves(ctx, x, (hipStream_t)stream);
+    if (st != PC_OK) return st;
+  }
   // (lengths all at once: a slot may be a source and a destination)
-  std::vector<int32_t> lens(n);
   for (int l = layer0; l < layer0 + n_layers; ++l) {
     for (int i = 0; i < n; ++i) lens[i] = len_of(l, i);
     for (int i = 0; i < n; ++i) ctx->slot_len[(size_t)l * c.n_slots + dst_slots_host[i]] = lens[i];
   }
   return PC_OK;
+} catch (const std::exception &) {   // (before the first launch; the text is short enough to be kept without an allocation)
+  return pc::fail(ctx, PC_ENOMEM, "no host memory");
 }

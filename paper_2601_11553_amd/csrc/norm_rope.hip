@@ -159,6 +159,7 @@ extern "C" pc_status percache_qkv_norm_rope(percache_ctx *ctx, const void *qkv_d
   // A head for every group of lanes while that fills the chip; then several; past what the last-level cache holds, loads and stores that are not kept (48 heads
   // of 128, 4000 rows 20.4 us kept, 21.6 not; 8000 rows 40.0, 38.9; 16384 rows 84.6, 75.2 and with four heads a group 78: 5.4 TB/s, what a copy of 200 MB reaches).
   const long groups = (long)n_rows * heads;
+  if (groups >= 1L << 31) return pc::fail(ctx, PC_ESHAPE, "%d rows of %d heads are 2^31 or more", n_rows, heads);   // (a grid has fewer than 2^32 threads)
 #define PC_NR(DD, HH, OO)                                                                                                   \
   hipLaunchKernelGGL((norm_rope_kernel<DD, HH, OO>), dim3((unsigned)(((long)n_rows * ((heads + HH - 1) / HH) * lanes + 255) / 256)), dim3(256), 0, s, a)
 #define PC_NR_D(DD)                                                                     \

@@ -13,12 +13,14 @@
 // What a row does not see takes no part, whatever stands there: K by the mask on the scores; V behind the end of a chunk or a request by clearing the
 // operand; V of a later token of the same tile, where it is not finite, by computing the rows that it made NaN once more, key by key.
 #include <algorithm>
+#include <exception>
 #include <cmath>
 #include <cstddef>
 #include <cstring>
 #include <functional>
 
 #include "decode_common.hpp"
+#include "launch_lists.hpp"
 
 namespace {
 using pc::bf16x4;
@@ -32,50 +34,14 @@ using pc::dec::codes8;
 using pc::dec::fast_exp2;
 using pc::dec::row_max;
 using pc::dec::row_sum;
+using namespace pc::packed;
 
 constexpr int TK = kKvTile, NW = 8;
-constexpr int kWide = 0, kNarrow = 1;      // kinds of items
-constexpr int kWideRows = 256, kNarrowRows = 32;
 constexpr float kSumLimit = 32.f * 256.f;  // 32 probabilities of a lane and tile, each at most 2^8 against the reference
 constexpr float kSumLimit4 = 4.f * 256.f;  // 4 of them
 constexpr int kMaxPackedSplits = 64;
 constexpr int kMoreItems = 16;             // items beyond one a block, per CU
 
-// A workgroup's work, for every kv head: rows() stacked rows from head rem0 of token i0 of a request on, over n_cached cached tiles from tile tile0 of
-// chunk entry ent on, then over the fresh tiles [f0, f1).
-struct Item {
-  int32_t row0, T, i0, n_cached, ent, tile0, f0, f1;
-  int32_t slot0, used0;     // entry ent: a workgroup's first tiles are asked for before its entries are there
-  int32_t part;             // first row of its partial results, -1: it is the block's only partition
-  uint16_t rem0, rows_kind; // rows * 2 + kind
-  __host__ __device__ int rows() const { return rows_kind >> 1; }
-  __host__ __device__ int kind() const { return rows_kind & 1; }
-};
-constexpr int kItemWords = sizeof(Item) / 4;
-struct Merge { int32_t row0, i0, rem0, rows, part, n; };   // partition p of the block has its partial rows from part + p * rows on
-constexpr int kMergeWords = sizeof(Merge) / 4;
-
-struct Args {
-  const __bf16 *q, *k, *v;   // [heads][N][D]
-  const __bf16 *k16, *v16;
-  const uint8_t *k8, *v8;
-  const float *k_scale, *v_scale;
-  const int32_t *words;      // items, merges, chunk entries (slot, used length > 0)
-  __bf16 *out;               // [N][Hq * D]
-  float *lse;                // [Hq][N] or null
-  float *part_o, *part_ml;   // [part_rows of every kv head][D], [...][2]
-  long N, part_rows;
-  int merges_at, ents_at, n_ents, Hq, Hkv, C, n_slots16;
-  unsigned per_group;        // 2^32 / G, rounded up: x / G = the upper half of x times it for the small x of a block
-  float scale_log2e;
-};
-
-// Lists that fit a launch's arguments are read from there: no launch in front that copies them.
-constexpr int kArgWords = (4096 - (int)sizeof(Args)) / 4;
-struct ArgsAndWords {
-  Args a;
-  int32_t words[kArgWords];
-};
 static_assert(sizeof(ArgsAndWords) <= 4096, "the arguments of a launch");
 __device__ __forceinline__ const int32_t *words_of_launch() {
   return (const int32_t *)((const char *)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(ArgsAndWords, words));
@@ -1187,7 +1153,7 @@ int32_t percache_packed_max_splits(const percache_ctx *ctx, int32_t n_seq, int32
 pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void *q_dev, const void *k_dev, const void *v_dev, int32_t n_rows,
                                     const int32_t *start_host, int32_t n_seq, const int32_t *slot_ids_host, const int32_t *used_len_host,
                                     const int32_t *n_chunks_host, int32_t max_chunks, int32_t n_splits, void *attn_out_dev, float *lse_out_dev,
-                                    void *workspace_dev, size_t workspace_bytes, void *stream) {
+                                    void *workspace_dev, size_t workspace_bytes, void *stream) try {
   if (!ctx) return PC_EINVAL;
   const percache_config &c = ctx->cfg;
   if (n_seq < 1 || n_rows < 0) return pc::fail(ctx, PC_EINVAL, "n_seq must be positive and n_rows not negative");
@@ -1215,6 +1181,7 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   const PackedWs ws = carve(c, ctx->n_cu, workspace_dev, n_seq, n_rows, max_chunks);
   Plan plan;
   plan_items(ctx, table, stride, start_host, n_seq, n_splits, ws, plan);
+  if ((long)plan.n_items * c.n_kv_heads >= 1L << 23) return pc::fail(ctx, PC_ESHAPE, "2^23 workgroups or more");   // (a grid has fewer than 2^32 threads)
   hipStream_t s = (hipStream_t)stream;
   const bool in_args = plan.words.size() <= (size_t)kArgWords;
   if (!in_args) {
@@ -1275,6 +1242,8 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
     PC_HIP(ctx, hipGetLastError());
   }
   return PC_OK;
+} catch (const std::exception &) {   // (before the first launch; the text is short enough to be kept without an allocation)
+  return pc::fail(ctx, PC_ENOMEM, "no host memory");
 }
 
 }  // extern "C"

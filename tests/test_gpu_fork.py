@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 def filled(seed, Hkv, D, C, n, n8, lengths, n_layers=2):
     g = np.random.default_rng(seed)
-    pc = Percache(n_layers=n_layers, hidden=64, n_q_heads=2 * Hkv, n_kv_heads=Hkv, head_dim=D, n_slots=n, slot_capacity=C, max_pos=64, n_slots_8bit=n8, device=DEV)
+    pc = Percache(n_layers=n_layers, hidden=64, n_q_heads=2 * Hkv, n_kv_heads=Hkv, head_dim=D, n_slots=n, slot_capacity=C, max_pos=512, n_slots_8bit=n8, device=DEV)
     for layer in range(n_layers):
         for s, m in enumerate(lengths if np.ndim(lengths) == 1 else lengths[layer]):
             if m:
@@ -116,4 +116,21 @@ def test_padding_behind_the_last_token_is_zero():
     out = pc.percache_attention_reuse(0, q, kf, vf, slot_ids=[[1]])
     torch.cuda.synchronize()
     assert torch.isfinite(out).all()
+    pc.close()
+
+
+@pytest.mark.parametrize("D,n8", [(128, 0), (64, 0), (128, 3), (64, 3)])
+def test_a_slot_cut_in_place_has_zeros_behind_its_last_token(D, n8):
+    """The tokens that are cut off are infinite (8-bit: large); another slot takes them along before."""
+    pc, g = filled(11, 2, D, 128, 3, n8, [100, 128, 7], n_layers=2)
+    for layer in range(2):
+        k, v = pc.percache_kv_get(layer, 0)
+        v[:, 70:] = 2.0 ** 100 if n8 else float("inf")
+        pc.percache_kv_put(layer, 0, k, v)
+    check(pc, [0, 0, 1], [0, 2, 1], [70, 90, 64])
+    for layer in range(2):
+        q, kf, vf = (bf16(g.standard_normal((1, h, 3, D))) for h in (4, 2, 2))
+        out = pc.percache_attention_reuse(layer, q, kf, vf, slot_ids=[[0, 1]])
+        torch.cuda.synchronize()
+        assert torch.isfinite(out).all()
     pc.close()
