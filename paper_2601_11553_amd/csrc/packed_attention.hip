@@ -974,7 +974,7 @@ struct Plan {
 void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int stride, const int32_t *start, int n_seq, int n_splits, const PackedWs &ws, Plan &plan) {
   const percache_config &c = ctx->cfg;
   const int G = c.n_q_heads / c.n_kv_heads;
-  struct Block { int seq, r_first, rows, kind, tiles, n; };   // n: partitions
+  struct Block { int seq, r_first, rows, kind, tiles, n; };   // n: partitions (0: they end where `ends` says)
   // us of a workgroup's start and end, and of a tile (most of the chip at work: the clock falls; alone 1.45 at head size 128), us of a MB from memory
   constexpr float kStart = 6.f, kPerMb = 1.f / 5.4f;
   const bool d128 = c.head_dim == 128;
@@ -1023,6 +1023,21 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   float mb = 0.f;
   for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
   std::vector<float> costs, free_at;
+  std::vector<int> ends;
+  auto play = [&]() {   // us of workgroups of these costs
+    std::sort(costs.begin(), costs.end(), std::greater<float>());
+    float end = costs[0];
+    if ((int)costs.size() <= cus) return end;
+    free_at.assign(costs.begin(), costs.begin() + cus);   // (a heap, the CU that is free first at its head)
+    std::make_heap(free_at.begin(), free_at.end(), std::greater<float>());
+    for (size_t i = cus; i < costs.size(); ++i) {
+      std::pop_heap(free_at.begin(), free_at.end(), std::greater<float>());
+      free_at.back() += costs[i];
+      end = std::max(end, free_at.back());
+      std::push_heap(free_at.begin(), free_at.end(), std::greater<float>());
+    }
+    return end;
+  };
   auto settle = [&](std::vector<Block> &blocks) {   // chooses the partitions; us
     float longest[2] = {0.f, 0.f};
     bool any = false, open = true;   // whether a block can be cut; whether finer limits can still be better: their workgroups' time only grows
@@ -1036,14 +1051,13 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     for (float cut = 1.f; open && cut <= (any ? (float)kMaxPackedSplits : 1.f); cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
       for (float cut2 = 1.f; cut2 <= (any && both ? 2.f : 1.f); cut2 *= 2.f) {
         const float wide = kStart + (top - kStart) / cut, limit[2] = {wide, std::min(wide, kStart + (longest[kNarrow] - kStart) / cut2)};
-        float rows = 0.f, sum = 0.f, end = 0.f;
+        float rows = 0.f, sum = 0.f;
         costs.clear();
         for (const Block &x : blocks) {
           const int n = parts_of(x, limit);
           const float each = kStart + tile_us(x) * (float)x.tiles / (float)n;
           costs.insert(costs.end(), n, each);
           sum += each * (float)n;
-          end = std::max(end, each);
           if (n > 1) rows += (float)(n * x.rows);
         }
         const float more = rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f;
@@ -1051,18 +1065,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
           open = cut2 > 1.f && open;
           continue;
         }
-        if ((int)costs.size() > cus) {
-          std::sort(costs.begin(), costs.end(), std::greater<float>());
-          free_at.assign(costs.begin(), costs.begin() + cus);   // (a heap, the CU that is free first at its head)
-          std::make_heap(free_at.begin(), free_at.end(), std::greater<float>());
-          for (size_t i = cus; i < costs.size(); ++i) {
-            std::pop_heap(free_at.begin(), free_at.end(), std::greater<float>());
-            free_at.back() += costs[i];
-            end = std::max(end, free_at.back());
-            std::push_heap(free_at.begin(), free_at.end(), std::greater<float>());
-          }
-        }
-        const float us = std::max(end, mb * kPerMb) + more;
+        const float us = std::max(play(), mb * kPerMb) + more;
         if (us < 0.97f * best) {
           best = us;
           best_limit[kWide] = limit[kWide];
@@ -1070,6 +1073,44 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
         }
       }
     for (Block &x : blocks) x.n = parts_of(x, best_limit);
+    // The blocks' keys laid end to end and cut where a CU's share ends, the share a little longer from try to try until it is enough: partitions are as long as
+    // a share or what is left of one on either side of a block's end, and the launch puts the latter together again, longest with shortest (the 200 wide blocks
+    // alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64 and 8-bit chunks 67, 59; with the 144 narrow ones 131 uncut, 138).
+    float sum = 0.f;
+    for (const Block &x : blocks) sum += cost_of(x, x.tiles);
+    int tries = any && (long)blocks.size() <= 4L * cus ? 8 : 0;
+    for (float share = std::max(sum / (float)cus + kStart, 2.f * kStart); tries > 0; share *= 1.05f, --tries) {
+      ends.clear();
+      costs.clear();
+      int bins = 1;
+      float left = share, rows = 0.f;
+      for (const Block &x : blocks) {
+        const int least = x.kind == kWide ? 6 : 4;
+        int n = 0;
+        for (int t = 0; t < x.tiles; ++n) {
+          int can = (int)((left - kStart) / tile_us(x));
+          if (can < std::min(least, x.tiles - t)) {
+            ++bins;
+            left = share;
+            can = std::max(least, (int)((left - kStart) / tile_us(x)));
+          }
+          if (can < x.tiles - t && x.tiles - t - can < least) can = x.tiles - t < 2 * least ? x.tiles - t : x.tiles - t - least;
+          can = std::min(can, x.tiles - t);
+          t += can;
+          left -= cost_of(x, can);
+          costs.push_back(cost_of(x, can));
+          ends.push_back(t);
+        }
+        if (n > 1) rows += (float)(n * x.rows);
+      }
+      if (bins > cus) continue;
+      const float us = std::max(play(), mb * kPerMb) + (rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f);
+      if (us < 0.97f * best) {
+        best = us;
+        for (Block &x : blocks) x.n = 0;
+      }
+      break;
+    }
     return best;
   };
   // Blocks of 256 rows; where few of them would find the chip half empty, 32 rows each may be the faster ones (few keys: more workgroups, less of a walk each)
@@ -1079,16 +1120,24 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   const float by_wide = choose ? settle(blocks) : 0.f;
   if ((long)blocks.size() * 2 <= cus) {
     std::vector<Block> low = cut(kNarrowRows);
+    const std::vector<int> of_wide = ends;
     if ((long)low.size() <= 2L * cus && (!choose || settle(low) < by_wide)) blocks = std::move(low);
+    else ends = of_wide;
   }
   if (n_splits > 0)
     for (Block &x : blocks) x.n = std::min(n_splits, x.tiles);
   struct Unit { int block, begin, end; float cost; int part; };
   std::vector<Unit> units;
   long part_rows = 0, more = ws.most_items - (long)blocks.size();
+  const int *end_of = ends.data();
   for (int b = 0; b < (int)blocks.size(); ++b) {
     const Block &x = blocks[b];
     int n = x.n;
+    const int *const mine = n ? nullptr : end_of;
+    if (mine) {
+      while (mine[n] < x.tiles) ++n;
+      end_of += ++n;
+    }
     if (n - 1 > more || part_rows + (long)n * x.rows > ws.part_rows) n = 1;
     if (n > 1) {
       const Merge m = {start[x.seq], x.r_first / G, x.r_first % G, x.rows, (int32_t)part_rows, n};
@@ -1097,7 +1146,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
       plan.tallest = std::max(plan.tallest, x.rows);
     }
     for (int p = 0; p < n; ++p) {
-      const int begin = (int)((long)p * x.tiles / n), end = (int)((long)(p + 1) * x.tiles / n);
+      const int begin = n == 1 ? 0 : mine ? (p ? mine[p - 1] : 0) : (int)((long)p * x.tiles / n), end = n == 1 ? x.tiles : mine ? mine[p] : (int)((long)(p + 1) * x.tiles / n);
       units.push_back({b, begin, end, cost_of(x, end - begin), n > 1 ? (int)part_rows + p * x.rows : -1});
     }
     if (n > 1) part_rows += (long)n * x.rows;

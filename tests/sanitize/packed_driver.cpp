@@ -42,7 +42,7 @@ std::vector<Fork> forks;
 
 long allocations_left = -1;   // -1: as many as are asked for
 int bad;
-int seen_merges, seen_long, seen_short, seen_kind[2], seen_rings, seen_store[2];   // that the calls reach all of this
+int seen_merges, seen_long, seen_short, seen_kind[2], seen_rings, seen_store[2], seen_uneven;   // that the calls reach all of this
 void expect(bool ok, const char *what) {
   if (!ok) {
     if (++bad < 20) std::printf("FAILED: %s\n", what);
@@ -258,14 +258,17 @@ void packed_call(Context &x, std::mt19937 &rng, const std::vector<int> &T, int m
       const int rows = heights[b][kv.first], tiles = cached[b] + ((kv.first + rows - 1) / G) / 64 + 1;
       auto &parts = kv.second;
       std::sort(parts.begin(), parts.end(), [](const Part &x, const Part &y) { return x.begin < y.begin; });
-      int t = 0;
+      int t = 0, shortest = tiles, longest = 0;
       for (const Part &q : parts) {
+        shortest = std::min(shortest, q.end - q.begin);
+        longest = std::max(longest, q.end - q.begin);
         expect(q.begin == t && q.rows == rows, "packed: every key in one partition");
         t = q.end;
         expect((parts.size() == 1) == (q.part < 0), "packed: partial results");
         if (q.part >= 0) rows_used.push_back({q.part, q.part + rows});
       }
       expect(t == tiles, "packed: all keys");
+      seen_uneven += longest > shortest + 1;
       if (parts.size() > 1) {
         ++merged;
         const auto m = merges.find(parts[0].part);
@@ -444,7 +447,7 @@ int main() {
   fork_calls();
   refusals();
   selection_sizes();
-  expect(seen_merges && seen_long && seen_short && seen_kind[0] && seen_kind[1] && seen_rings && seen_store[0] && seen_store[1], "calls of every kind");
+  expect(seen_merges && seen_long && seen_short && seen_kind[0] && seen_kind[1] && seen_rings && seen_store[0] && seen_store[1] && seen_uneven, "calls of every kind");
   std::printf(bad ? "packed driver: %d FAILED checks\n" : "packed driver: ok\n", bad);
   return bad ? 1 : 0;
 }
