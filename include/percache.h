@@ -360,8 +360,9 @@ pc_status percache_kv_keep(percache_ctx *ctx, int32_t layer, const int32_t *slot
  *   [Hq, n_rows], the log-sum-exp of a row's scores.  Positions are those of q and k already, so L_pre is checked as if one token were
  *   fresh.  What a row does not see takes no part, infinities and NaN included: cached tokens behind the used length, later rows, other requests.
  *   n_splits > 0 cuts every row block's keys into that many partitions (at most percache_packed_max_splits), 0: chosen by the library.
- *   workspace_dev >= percache_packed_workspace_bytes(ctx, n_seq, n_rows, max_chunks), 256-byte aligned.  The call brings its lists to the device as
- *   the calls with host chunk lists do. */
+ *   workspace_dev >= percache_packed_workspace_bytes(ctx, n_seq, n_rows, max_chunks), 256-byte aligned.  Its lists (12 words a
+ *   row block or partition, 6 a merge, 2 a chunk) travel as a launch argument up to about 980 words, beyond that as the calls with host chunk lists do;
+ *   a captured call keeps the lists it was captured with and is refused (PC_ESHAPE) where they do not fit the argument. */
 pc_status percache_qkv_norm_rope(percache_ctx *ctx, const void *qkv_dev, int64_t row_stride, int32_t n_rows, const int32_t *pos_dev,
                                  int32_t n_axes, const uint8_t *axis_host, const void *qkv_bias_dev, const void *q_norm_dev,
                                  const void *k_norm_dev, float eps, void *q_out_dev, void *k_out_dev, void *v_out_dev, void *stream);

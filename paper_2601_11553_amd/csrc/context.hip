@@ -120,6 +120,13 @@ pc_status build_chunk_table(percache_ctx *ctx, int32_t layer, int32_t batch, int
   return PC_OK;
 }
 
+bool being_captured(hipStream_t st) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(st, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return true;
+}
+
 pc_status upload_table(percache_ctx *ctx, const std::vector<int32_t> &rows, int32_t *dst_dev, hipStream_t stream) {
   // Lists that fit a launch's arguments travel as such.  The staged copy is a kernel too (2.6 us), behind a change of queues, and the host
   // waits for the events that guard its ring: one query's layer over 4 chunks, 64 tokens, 26.7 us a call with it, 22.9 without.

@@ -1681,12 +1681,7 @@ size_t list_bytes(const percache_ctx *ctx, int32_t n_probes) {
 }
 
 constexpr int kInLaunchProbes = 4;   // (one wavefront of the merging workgroup each)
-bool being_captured(hipStream_t st) {
-  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-  if (hipStreamIsCapturing(st, &status) == hipSuccess) return status != hipStreamCaptureStatusNone;
-  (void)hipGetLastError();
-  return true;
-}
+using pc::being_captured;
 // A number for the marks of a call that no other call uses (from a start that a workspace's contents will not hold by chance).
 unsigned long long next_mark() {
   static std::atomic<unsigned long long> counter{std::chrono::steady_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull | 1};

@@ -1234,6 +1234,8 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   hipStream_t s = (hipStream_t)stream;
   const bool in_args = plan.words.size() <= (size_t)kArgWords;
   if (!in_args) {
+    // (a replay would find whatever the ring of staging buffers holds by then)
+    if (pc::being_captured(s)) return pc::fail(ctx, PC_ESHAPE, "a list of %zu words is too long for a call that is captured (%d)", plan.words.size(), kArgWords);
     st = pc::upload_table(ctx, plan.words, ws.words, s);
     if (st != PC_OK) return st;
   }

@@ -146,6 +146,8 @@ pc_status fail(percache_ctx *ctx, pc_status st, const char *fmt, ...);
 pc_status build_chunk_table(percache_ctx *ctx, int32_t layer, int32_t batch, int32_t t_fresh,
                             const int32_t *slot_ids, const int32_t *used_len, const int32_t *n_chunks,
                             int32_t max_chunks, std::vector<int32_t> &rows);
+// Whether work on the stream goes into a graph (also where the runtime does not say).
+bool being_captured(hipStream_t stream);
 // Copies table rows to device memory through the pinned ring, ordered on `stream`.
 pc_status upload_table(percache_ctx *ctx, const std::vector<int32_t> &rows, int32_t *dst_dev,
                        hipStream_t stream);

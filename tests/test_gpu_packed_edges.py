@@ -197,6 +197,29 @@ def test_lists_longer_than_a_launchs_arguments():
     pc.close()
 
 
+def test_a_list_too_long_for_a_captured_call_is_refused():
+    """... without harm to the capture: what else is captured runs."""
+    pc, g, kv = make(56, 4, 2, 64, 64, "bf16", [64] * 4, max_pos=1024)
+    long, short = np.arange(0, 301), [0, 300]
+    q, k, v = packed(g, 4, 2, 64, 300)
+    out = torch.zeros((300, 256), dtype=torch.bfloat16, device=DEV)
+    for start in (long, short):
+        pc.percache_attention_packed(0, q, k, v, start, attn_out=out)
+    torch.cuda.synchronize()
+    want = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(PercacheError, match="captured"):
+            pc.percache_attention_packed(0, q, k, v, long, attn_out=out)
+        pc.percache_attention_packed(0, q, k, v, short, attn_out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    pc.close()
+
+
 def test_offsets_beyond_32_bits():
     """Slots whose elements lie beyond 2^32 bytes of the store, packed rows beyond 2^31 elements of q."""
     pc = Percache(n_layers=1, hidden=64, n_q_heads=2, n_kv_heads=1, head_dim=128, n_slots=3000, slot_capacity=8192, max_pos=16384, device=DEV)   # 6.3 GB each of K and V
