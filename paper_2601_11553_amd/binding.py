@@ -209,6 +209,7 @@ class Percache:
         self._step_ws = None
         self._lookup_ws = None
         self._topk_ws = None
+        self._captured_ws = {}   # workspaces that a graph has the address of
         self._draft_ws = {}
         self._draft_bytes = {}
 
@@ -506,11 +507,14 @@ class Percache:
 
     # ------------------------------------------------------------------ drafted tokens, eviction inside a slot
     def _draft_workspace(self, nbytes: int, stream):
-        """Each stream's own: one that is outgrown goes back to the memory of the stream it was made on, where nothing else has used it."""
+        """Each stream's own: one that is outgrown goes back to the memory of the stream it was made on, where nothing else has used it, unless a captured
+        call has it."""
         import torch
         ws = self._draft_ws.get(stream)
         if ws is None or ws.numel() < nbytes + 256:
             ws = self._draft_ws[stream] = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        if torch._C._cuda_isCurrentStreamCapturing():
+            self._captured_ws[ws.data_ptr()] = ws
         return (ws.data_ptr() + 255) // 256 * 256
 
     def _draft_need(self, batch, t_draft, max_chunks) -> int:

@@ -197,6 +197,37 @@ def test_lists_longer_than_a_launchs_arguments():
     pc.close()
 
 
+def test_a_captured_calls_workspace_stays_when_it_is_outgrown():
+    """Warm-up and capture on one stream, then a larger call there: what takes the memory that it gives back is not written by a replay."""
+    pc, g, kv = make(57, 4, 2, 64, 64, "bf16", [64] * 4, max_pos=1024)
+    q, k, v = packed(g, 4, 2, 64, 600)
+    out = torch.zeros((600, 256), dtype=torch.bfloat16, device=DEV)
+    small, large = ([0, 300], [0, 600])
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    qs, ks, vs = (x[:, :300].contiguous() for x in (q, k, v))
+
+    def call():
+        pc.percache_attention_packed(0, qs, ks, vs, small, attn_out=out[:300], n_splits=3)
+    with torch.cuda.stream(stream):
+        call()
+    torch.cuda.synchronize()
+    want, size = out.clone(), pc._draft_ws[stream.cuda_stream].numel()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call()
+    with torch.cuda.stream(stream):
+        pc.percache_attention_packed(0, q, k, v, large)
+        assert pc._draft_ws[stream.cuda_stream].numel() > size
+        others = [torch.full((size,), 7, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all((x == 7).all() for x in others)
+    pc.close()
+
+
 def test_a_list_too_long_for_a_captured_call_is_refused():
     """... without harm to the capture: what else is captured runs."""
     pc, g, kv = make(56, 4, 2, 64, 64, "bf16", [64] * 4, max_pos=1024)
