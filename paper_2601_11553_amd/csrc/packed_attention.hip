@@ -110,6 +110,10 @@ __device__ __forceinline__ float taint(unsigned two, float acc) {
 // a memory instruction that reads it.)
 template <bool ONCE>   // ONCE: read by this workgroup only, not kept in the caches
 __device__ __forceinline__ void to_lds(const char *src, unsigned off, unsigned to) {
+  // (all lanes' alike, which a compiler that optimises less does not see)
+  const unsigned long at = (unsigned long)src;
+  src = (const char *)((unsigned long)(unsigned)__builtin_amdgcn_readfirstlane((int)(at >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)at));
+  to = __builtin_amdgcn_readfirstlane((int)to);
   if (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(to), "v"(off), "s"(src) : "memory");
   else asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(src) : "memory");
 }
