@@ -3,10 +3,11 @@
 //
 // What bounds it: the logits, read once.  beam_rows_kernel: a workgroup has a row or a stretch of it, every lane a share of it, of which it keeps the running
 // maximum, the sum of exponentials and the round that the maximum came in -- per logit a maximum, a difference, a product, an exponential and a sum,
-// and no list.  64 groups of four lanes have k best tokens at or above the k-th best of their maxima; the lanes that reach it read their logits again
-// (a sixteenth of the stretch for 16 tokens, from cache), and what reaches it, a few more than k as a rule, is put in order by counting.
-// 512 rows of 131072 bf16 logits: 33 us, of which the stream of 134 MB takes some 25 and the rest is the start and what comes behind a stretch's last logit.
-// beam_pick_kernel: a request's stretches meet (8 us for 64 requests of 8 x 2 x 16 candidates); scores are formed and compared in 64 bits, so that
+// and no list.  64 groups of four lanes have k best tokens at or above the k-th best of their maxima; the lanes that reach it read the round of their maximum
+// again (those whose second best round reaches it too all of theirs), and what reaches it, a few more than k as a rule, is put in order by counting.
+// 512 rows of 131072 bf16 logits: 29.5 us, of which the stream of 134 MB takes 24 (19 without the exponentials) and what comes behind a stretch's last logit
+// 5: the bound 1.3, the second look 2.5, order and the way out (with all of a lane's logits read again 7).
+// beam_pick_kernel: a request's stretches meet (5.5 us for 64 requests of 8 x 2 x 16 candidates); scores are formed and compared in 64 bits, so that
 // candidates of different beams that lie next to each other come in their right order.
 #include "percache_internal.hpp"
 
@@ -35,10 +36,22 @@ __device__ __forceinline__ u64 key_of(float x, unsigned token) { return ((u64)or
 template <int CTRL>
 __device__ __forceinline__ float moved(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true)); }
 template <int CTRL>
-__device__ __forceinline__ double moved(double x) {
-  const u64 u = (u64)__double_as_longlong(x);
+__device__ __forceinline__ u64 moved(u64 u) {
   const unsigned lo = __builtin_amdgcn_update_dpp(0, (unsigned)u, CTRL, 0xf, 0xf, true), hi = __builtin_amdgcn_update_dpp(0, (unsigned)(u >> 32), CTRL, 0xf, 0xf, true);
-  return __longlong_as_double((long long)(((u64)hi << 32) | lo));
+  return ((u64)hi << 32) | lo;
+}
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {
+  return __longlong_as_double((long long)moved<CTRL>((u64)__double_as_longlong(x)));
+}
+template <int CTRL>
+__device__ __forceinline__ int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xf, 0xf, true); }
+// over 4 or 8 neighbouring lanes
+template <int N>
+__device__ __forceinline__ int sum_of(int x) {
+  x += moved<0xB1>(x);
+  x += moved<0x4E>(x);
+  return N == 8 ? x + moved<0x141>(x) : x;
 }
 template <class X, class Op>
 __device__ __forceinline__ X over_lanes(X x, Op op) {
@@ -65,7 +78,7 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict__ logits, long row_stride, int vocab, int n_stretch, int best, Stretch *__restrict__ st_out,
                                                             u64 *__restrict__ list_out) {
   constexpr int PER = 16 / (int)sizeof(T), NV = 4, EACH = NV * PER, ROUND = NV * 64;   // logits of a lane and round; vectors of a wavefront and round
-  __shared__ u64 least_of[kThreads], found[kFound];
+  __shared__ u64 found[kFound];
   __shared__ uint16_t again[kThreads];
   __shared__ float tops[kWaves];
   __shared__ double sums[kWaves];
@@ -90,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
     for (int j = 0; j < NV; ++j) raw[j] = *(const vec_at *)(x + (long)min(v + j * 64 + lane, v1 - 1) * PER);
   };
 
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, second = -INFINITY, l = 0.f;   // second: the largest in any round but m's
   int when = 0;   // first vector of the round that m came in
   const float tail = has_tail ? (float)x[tail0 + lane] : -INFINITY;
   auto take = [&](const u32x4_ (&raw)[NV], int v, auto whole_c) __attribute__((always_inline)) {
@@ -111,6 +124,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
     }
     l = (m == -INFINITY ? l : l * exp_below(m - ref)) + (s0 + s1);   // (a sum that is NaN stays)
     when = top > m ? v : when;
+    second = fmaxf(second, fminf(m, top));
     m = mn;
   };
   if (v0 < v1) {
@@ -134,21 +148,24 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
     if (tail > m) least = key_of(tail, (unsigned)(tail0 + lane));
     m = mn;
   }
-  least_of[tid] = least;
+  // the best token of every group of four neighbouring lanes is not below:
+  u64 group = least;
+  u64 other = moved<0xB1>(group);
+  group = other > group ? other : group;
+  other = moved<0x4E>(group);
+  group = other > group ? other : group;
+  if ((lane & 3) == 0) found[tid >> 2] = group;
   if (tid == 0) {
     n_found = 0;
     bound = ~0ull;
   }
   __syncthreads();
-  if (wave == 0) {
-    u64 own = 0;
+  {   // (a group's lanes count a quarter of the others each)
+    int above = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) own = least_of[w * 64 + lane] > own ? least_of[w * 64 + lane] : own;
-    found[lane] = own;
-    int rank = 0;
-#pragma unroll 16
-    for (int j = 0; j < 64; ++j) rank += found[j] > own;
-    if (rank < best) atomicMin(&bound, own ? own : 1ull);   // (fewer than `best` groups with a token: every one of theirs reaches it)
+    for (int j = 0; j < 16; ++j) above += found[j * 4 + (lane & 3)] > group;
+    above = sum_of<4>(above);
+    if ((lane & 3) == 0 && above < best) atomicMin(&bound, group ? group : 1ull);   // (fewer than `best` groups with a token: every one of theirs reaches it)
   }
   __syncthreads();
   const u64 reach = bound;
@@ -158,65 +175,92 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(const T *__restrict
   };
   const u64 tail_key = tail > -INFINITY ? key_of(tail, (unsigned)(tail0 + lane)) : 0ull;
   if (tail_key >= reach) put(tail_key);
-  // this wavefront's lanes that are read again, vector by vector
-  const u64 mask = __builtin_amdgcn_ballot_w64(most >= reach);
-  if (most >= reach) again[wave * 64 + __popcll(mask & ((1ull << lane) - 1))] = (uint16_t)lane;
-  __builtin_amdgcn_wave_barrier();
-  const int each = (v1 - v0 + 63) / 64, items = __popcll(mask) * each;
-  auto reread = [&](int item0, auto use) __attribute__((always_inline)) {   // two of them
-    u32x4_ raw[2];
-    int v[2];
+  // What reaches it is in lanes whose best token does, as a rule in that one's round alone: such a lane reads the round again.
+  const float from = reach > 1ull ? from_ordered((unsigned)(reach >> 32)) : -INFINITY;
+  const int each = (v1 - v0 + 63) / 64;
+  const bool hit = most >= reach, whole = hit && (second >= from || each <= NV);
+  auto look = [&](const u32x4_ &raw, int at, auto use) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+      const float y = value(raw, e);
+      if (at < v1 && y >= from && y > -INFINITY) use(key_of(y, (unsigned)(at * PER + e)));
+    }
+  };
+  // the others' vectors, all of them, are dealt out to the wavefront's lanes (and where there is one round: few lanes' are)
+  auto enlist = [&](bool mine) __attribute__((always_inline)) {
+    const u64 mask = __builtin_amdgcn_ballot_w64(mine);
+    __builtin_amdgcn_wave_barrier();
+    if (mine) again[wave * 64 + __popcll(mask & ((1ull << lane) - 1))] = (uint16_t)lane;
+    __builtin_amdgcn_wave_barrier();
+    return __popcll(mask) * each;
+  };
+  u32x4_ round[NV], more[2];
+  int more_at[2];
+  auto ask = [&](int item, int items) __attribute__((always_inline)) {   // two of them
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int item = item0 + 64 * j, i = item / each;
-      v[j] = item < items ? v0 + again[wave * 64 + i] + (item - i * each) * 64 : v1;
-      raw[j] = *(const vec_at *)(x + (long)min(v[j], v1 - 1) * PER);
+      const int i = (item + 64 * j) / each;
+      more_at[j] = item + 64 * j < items ? v0 + again[wave * 64 + i] + (item + 64 * j - i * each) * 64 : v1;
+      more[j] = *(const vec_at *)(x + (long)min(more_at[j], v1 - 1) * PER);
     }
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int e = 0; e < PER; ++e) {
-        const float y = value(raw[j], e);
-        if (v[j] < v1 && y > -INFINITY) use(key_of(y, (unsigned)(v[j] * PER + e)));
-      }
   };
-  for (int item = lane; item < items; item += 128)
-    reread(item, [&](u64 key) __attribute__((always_inline)) { if (key >= reach) put(key); });
-  // the wavefront's maximum and sum
+  if (hit && !whole) load(round, when);
+  const int rest = enlist(whole);
+  if (lane < rest) ask(lane, rest);
+  // meanwhile the wavefront's maximum and sum
   const float top = wave_max(m);
   const double sum = wave_sum(m == -INFINITY ? (l == l ? 0.0 : (double)NAN) : (double)l * (double)exp_below(m - top));
   if (lane == 0) {
     tops[wave] = top;
     sums[wave] = sum;
   }
+  auto put_if = [&](u64 key) __attribute__((always_inline)) { if (key >= reach) put(key); };
+  if (hit && !whole)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) look(round[j], when + j * 64 + lane, put_if);
+  for (int item = lane; item < rest; item += 128) {
+    if (item != lane) ask(item, rest);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) look(more[j], more_at[j], put_if);
+  }
   __syncthreads();
-  if (tid == kThreads - 1) {
+  if (wave == kWaves - 1) {
     float t = tops[0];
+#pragma unroll
     for (int w = 1; w < kWaves; ++w) t = fmaxf(t, tops[w]);
-    double s = 0.0;
-    for (int w = 0; w < kWaves; ++w) s += tops[w] == -INFINITY ? (sums[w] == sums[w] ? 0.0 : sums[w]) : sums[w] * exp((double)tops[w] - (double)t);
-    st_out[blockIdx.x] = Stretch{s, t, 0};
+    const float mine = tops[lane & (kWaves - 1)];
+    const double part = sums[lane & (kWaves - 1)];
+    double all = mine == -INFINITY ? (part == part ? 0.0 : part) : part * (double)exp_below(mine - t);
+    all += moved<0xB1>(all);
+    all += moved<0x4E>(all);
+    if (lane == 0) st_out[blockIdx.x] = Stretch{all, t, 0};
   }
   const int count = n_found;
   u64 *out = list_out + (size_t)blockIdx.x * best;
   if (count <= kFound) {
-    for (int f = tid; f < count; f += kThreads) {
+    for (int f = tid >> 2; f < count; f += kThreads / 4) {   // (four lanes a token)
       const u64 key = found[f];
-      int rank = 0;
-      for (int o = 0; o < count; ++o) rank += found[o] > key;
-      if (rank < best) out[rank] = key;
+      int above = 0;
+#pragma unroll 4
+      for (int o = lane & 3; o < count; o += 4) above += found[o] > key;
+      above = sum_of<4>(above);
+      if ((lane & 3) == 0 && above < best) out[above] = key;
     }
     for (int r = count + tid; r < best; r += kThreads) out[r] = 0;
     return;
   }
   // (the best ones of a stretch lie in few lanes: one after the other)
+  const int items = enlist(hit);
   u64 before = ~0ull;
   for (int r = 0; r < best; ++r) {
     if (tid == 0) next_best = 0;
     __syncthreads();
     u64 own = tail_key < before ? tail_key : 0ull;
-    for (int item = lane; item < items; item += 128)
-      reread(item, [&](u64 key) __attribute__((always_inline)) { own = key < before && key > own ? key : own; });
+    for (int item = lane; item < items; item += 128) {
+      ask(item, items);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) look(more[j], more_at[j], [&](u64 key) __attribute__((always_inline)) { own = key < before && key > own ? key : own; });
+    }
     atomicMax(&next_best, own);
     __syncthreads();
     before = next_best;
@@ -285,12 +329,13 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(const Stretch *
     if (total[j]) atomicMax(&groups[(5 * list + 13 * (c - list * best)) & 63], total[j]);
   }
   __syncthreads();
-  if (wave == 0) {
-    const u64 top = groups[lane];
-    int rank = 0;
-#pragma unroll 16
-    for (int j = 0; j < 64; ++j) rank += groups[j] > top;
-    if (rank < best) atomicMin(&bound, top ? top : 1ull);
+  {   // (eight lanes a group)
+    const u64 top = groups[tid >> 3];
+    int above = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) above += groups[j * 8 + (tid & 7)] > top;
+    above = sum_of<8>(above);
+    if ((tid & 7) == 0 && above < best) atomicMin(&bound, top ? top : 1ull);
   }
   __syncthreads();
   const u64 reach = bound;
@@ -304,12 +349,14 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(const Stretch *
     }
   __syncthreads();
   const int count = n_few;
-  for (int f = tid; f < count; f += kPickThreads) {
+  for (int f = tid >> 3; f < count; f += kPickThreads / 8) {   // (eight lanes a candidate)
     const u64 t = few[f];
     const int c = few_at[f];
     int rank = 0;
-    for (int o = 0; o < count; ++o) rank += few[o] > t || (few[o] == t && (int)few_at[o] < c);
-    if (rank >= best) continue;
+#pragma unroll 4
+    for (int o = tid & 7; o < count; o += 8) rank += few[o] > t || (few[o] == t && (int)few_at[o] < c);
+    rank = sum_of<8>(rank);
+    if ((tid & 7) || rank >= best) continue;
     const size_t to = (size_t)b * best + rank;
     const int beam = c / (n_stretch * best);
     parent[to] = beam;
@@ -323,7 +370,7 @@ __global__ __launch_bounds__(kPickThreads) void beam_pick_kernel(const Stretch *
   }
 }
 
-// Stretches a row is cut into: four workgroups a CU (512 rows of 131072: 35.8, 33.6, 34.7 us at two, four, eight), none shorter than 2048 logits, and no more
+// Stretches a row is cut into: four workgroups a CU (512 rows of 131072 logits: 29.6, 29.5, 31.2 us at two, four, eight; 64 rows 9.6, 8.6, 9.4), none shorter than 2048 logits, and no more
 // candidates of a request than beam_pick_kernel holds.
 int stretches_for(int n_cu, long rows, int beams, int vocab, int best) {
   long s = (4L * n_cu + rows - 1) / rows;

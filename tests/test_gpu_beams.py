@@ -89,6 +89,26 @@ def test_rows_at_a_distance_and_at_odd_places(pc, dtype):
         check(pc, wide[:, :, lo:lo + n], s, min(4, n))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_of_many_rounds(pc, dtype):
+    """So many rows that each is cut into few stretches and a lane has logits from several rounds: its best ones in one of them, in all, alike or nowhere."""
+    x, s = drawn(12, 48, 8, 50000, dtype)
+    x[1] = torch.sort(x[1], -1)[0]
+    for first, step in ((5, 1024), (7, 2048)):
+        n = x[2, :, first::step].shape[1]
+        x[2, :, first::step] = (20 + 0.25 * torch.arange(n, device=DEV) * (1 if first == 5 else -1)).to(dtype)
+        x[3, :, first::step] = 18
+    x[4, :, :] = -float("inf")
+    x[4, 3, ::4099] = 1.0
+    x[5] = -3.0
+    x[6, :, :20000] = -float("inf")
+    x[7, :, 256:] = x[7, :, 256:].clamp_(max=6)
+    x[7, :, :256] = torch.linspace(9, 10, 256, device=DEV).to(dtype)
+    s[1:8] = 0.0
+    s[1:8, 1:] = -5.0 * torch.arange(1, 8, device=DEV)
+    check(pc, x, s, 16)
+
+
 def test_large_and_small_logits(pc):
     x, s = drawn(9, 2, 2, 5000, torch.float32)
     check(pc, x * 40, s, 8)
