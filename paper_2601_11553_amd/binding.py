@@ -211,6 +211,7 @@ class Percache:
         self._topk_ws = None
         self._captured_ws = {}   # workspaces that a graph has the address of
         self._draft_ws = {}
+        self._all_chunks = {}    # lists of equal numbers of chunks, and their addresses
         self._draft_bytes = {}
 
     # ------------------------------------------------------------------ helpers
@@ -542,7 +543,10 @@ class Percache:
             if ids.size != batch * max_chunks:
                 raise ValueError(f"slot_ids: {ids.size} entries for {batch} queries")
         ul, ul_p = _i32_list(used_len, (batch, max_chunks))
-        nc, nc_p = _i32_list(n_chunks if n_chunks is not None else np.full(batch, max_chunks, np.int32), (batch,))
+        if n_chunks is None:
+            nc, nc_p = self._all_chunks.get((batch, max_chunks)) or self._all_chunks.setdefault((batch, max_chunks), _i32_list(np.full(batch, max_chunks, np.int32)))
+        else:
+            nc, nc_p = _i32_list(n_chunks, (batch,))
         return (ids, ul, nc), ids_p, ul_p, nc_p, max_chunks
 
     @staticmethod
@@ -737,7 +741,7 @@ class Percache:
         else:
             self._want("attn_out", attn_out, (n, Hq * D), bf16)
         if lse_out is True:
-            lse_out = torch.empty((Hq, n), dtype=torch.float32, device=self.device)
+            lse_out = q.new_empty((Hq, n), dtype=torch.float32)
         else:
             self._want("lse_out", lse_out, (Hq, n), torch.float32)
         stream = self._raw_stream()
@@ -770,7 +774,7 @@ class Percache:
             raise ValueError(f"logits: rows at an even distance are wanted, got strides {logits.stride()}")
         self._want("scores", scores, (batch, beams), torch.float32)
         score = scores.new_empty((batch, best))
-        parent, token = (torch.empty((batch, best), dtype=torch.int32, device=self.device) for _ in range(2))
+        parent, token = scores.new_empty((batch, best), dtype=torch.int32), scores.new_empty((batch, best), dtype=torch.int32)
         stream = self._raw_stream()
         key = ("beams", batch, beams, vocab, best)
         need = self._draft_bytes.get(key)

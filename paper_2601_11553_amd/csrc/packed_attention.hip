@@ -1019,9 +1019,9 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     }
     return blocks;
   };
-  // Partitions: blocks that take longer than a limit, one for each kind, are cut evenly.  A launch is dealt out longest first to the CUs, of which every kv head
-  // gets its share; that is played through for limits from the longest block's time down (while there are few workgroups a CU: many even out by themselves),
-  // and a limit that promises 3 % is taken.  Nothing is faster than its keys come from memory; a merge is a launch and the partial rows.  us at 1, 2, 3, 4
+  // Partitions: blocks that take longer than a limit, one for each kind, are cut evenly, or all are cut by shares.  A launch is dealt out longest first to the
+  // CUs, of which every kv head gets its share; that is played through (while there are few workgroups a CU: many even out by themselves), and what
+  // promises 3 % more is taken.  Nothing is faster than its keys come from memory; a merge is a launch and the partial rows.  us at 1, 2, 3, 4
   // partitions, measured: 72 wide blocks of 60 tiles 95, 64, 53, 60; head size 64, 152 of 36 to 60 tiles 84, 80, 70; 144 narrow ones of 52 tiles 53, 62, 53,
   // 59, 32 of them 48, 32, 24, 22, 200 wide ones of 50 to 60 tiles beside the 144 134 (cut evenly into 712 workgroups 151).
   auto parts_of = [&](const Block &x, const float (&limit)[2]) {
@@ -1032,9 +1032,9 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   float mb = 0.f;
   for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
   std::vector<float> costs, free_at;
+  std::vector<std::pair<float, int>> runs;   // so many workgroups of this cost
   std::vector<int> ends;
-  auto play = [&]() {   // us of workgroups of these costs
-    std::sort(costs.begin(), costs.end(), std::greater<float>());
+  auto play = [&]() {   // us of workgroups of these costs, longest first
     float end = costs[0];
     if ((int)costs.size() <= cus) return end;
     free_at.assign(costs.begin(), costs.begin() + cus);   // (a heap, the CU that is free first at its head)
@@ -1047,48 +1047,21 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     }
     return end;
   };
+  auto merge_us = [&](float rows) { return rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f; };
   auto settle = [&](std::vector<Block> &blocks) {   // chooses the partitions; us
-    float longest[2] = {0.f, 0.f};
-    bool any = false, open = true;   // whether a block can be cut; whether finer limits can still be better: their workgroups' time only grows
+    float longest[2] = {0.f, 0.f}, whole = 0.f;
+    bool any = false;   // whether a block can be cut
     for (const Block &x : blocks) {
       longest[x.kind] = std::max(longest[x.kind], cost_of(x, x.tiles));
+      whole += cost_of(x, x.tiles);
       any |= x.tiles >= (x.kind == kWide ? 12 : 8);
     }
-    float best = 1e30f, best_limit[2] = {longest[kWide], longest[kNarrow]};
-    const float top = std::max(longest[kWide], longest[kNarrow]);
-    const bool both = longest[kWide] > 0.f && longest[kNarrow] > 0.f;
-    for (float cut = 1.f; open && cut <= (any ? (float)kMaxPackedSplits : 1.f); cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
-      for (float cut2 = 1.f; cut2 <= (any && both ? 2.f : 1.f); cut2 *= 2.f) {
-        const float wide = kStart + (top - kStart) / cut, limit[2] = {wide, std::min(wide, kStart + (longest[kNarrow] - kStart) / cut2)};
-        float rows = 0.f, sum = 0.f;
-        costs.clear();
-        for (const Block &x : blocks) {
-          const int n = parts_of(x, limit);
-          const float each = kStart + tile_us(x) * (float)x.tiles / (float)n;
-          costs.insert(costs.end(), n, each);
-          sum += each * (float)n;
-          if (n > 1) rows += (float)(n * x.rows);
-        }
-        const float more = rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f;
-        if (std::max(sum / (float)cus, mb * kPerMb) + more >= 0.97f * best) {
-          open = cut2 > 1.f && open;
-          continue;
-        }
-        const float us = std::max(play(), mb * kPerMb) + more;
-        if (us < 0.97f * best) {
-          best = us;
-          best_limit[kWide] = limit[kWide];
-          best_limit[kNarrow] = limit[kNarrow];
-        }
-      }
-    for (Block &x : blocks) x.n = parts_of(x, best_limit);
     // The blocks' keys laid end to end and cut where a CU's share ends, the share a little longer from try to try until it is enough: partitions are as long as
     // a share or what is left of one on either side of a block's end, and the launch puts the latter together again, longest with shortest (the 200 wide blocks
     // alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64 and 8-bit chunks 67, 59; with the 144 narrow ones 131 uncut, 138).
-    float sum = 0.f;
-    for (const Block &x : blocks) sum += cost_of(x, x.tiles);
+    float by_share = 1e30f;
     int tries = any && (long)blocks.size() <= 4L * cus ? 8 : 0;
-    for (float share = std::max(sum / (float)cus + kStart, 2.f * kStart); tries > 0; share *= 1.05f, --tries) {
+    for (float share = std::max(whole / (float)cus + kStart, 2.f * kStart); tries > 0; share *= 1.05f, --tries) {
       ends.clear();
       costs.clear();
       int bins = 1;
@@ -1113,14 +1086,47 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
         if (n > 1) rows += (float)(n * x.rows);
       }
       if (bins > cus) continue;
-      const float us = std::max(play(), mb * kPerMb) + (rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f);
-      if (us < 0.97f * best) {
-        best = us;
-        for (Block &x : blocks) x.n = 0;
-      }
+      std::sort(costs.begin(), costs.end(), std::greater<float>());
+      by_share = std::max(play(), mb * kPerMb) + merge_us(rows);
       break;
     }
-    return best;
+    // Cut evenly, for limits from the longest block's time down.  (Taken where it promises what the shares do, within 3 %.)
+    float best = by_share * 1.06f, best_limit[2] = {longest[kWide], longest[kNarrow]};
+    bool evenly = false, open = true;   // open: whether finer limits can still be better: their workgroups' time only grows
+    const float top = std::max(longest[kWide], longest[kNarrow]);
+    const bool both = longest[kWide] > 0.f && longest[kNarrow] > 0.f;
+    for (float cut = 1.f; open && cut <= (any ? (float)kMaxPackedSplits : 1.f); cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
+      for (float cut2 = 1.f; cut2 <= (any && both ? 2.f : 1.f); cut2 *= 2.f) {
+        const float wide = kStart + (top - kStart) / cut, limit[2] = {wide, std::min(wide, kStart + (longest[kNarrow] - kStart) / cut2)};
+        float rows = 0.f, sum = 0.f, end = 0.f;
+        runs.clear();
+        for (const Block &x : blocks) {
+          const int n = parts_of(x, limit);
+          const float each = kStart + tile_us(x) * (float)x.tiles / (float)n;
+          runs.push_back({each, n});
+          sum += each * (float)n;
+          end = std::max(end, each);
+          if (n > 1) rows += (float)(n * x.rows);
+        }
+        const float more = merge_us(rows);
+        if (std::max(sum / (float)cus, mb * kPerMb) + more >= 0.97f * best) {
+          open = cut2 > 1.f && open;
+          continue;
+        }
+        if (end + more >= 0.97f * best) continue;
+        std::sort(runs.begin(), runs.end(), std::greater<std::pair<float, int>>());
+        costs.clear();
+        for (const auto &r : runs) costs.insert(costs.end(), r.second, r.first);
+        const float us = std::max(play(), mb * kPerMb) + more;
+        if (us < 0.97f * best) {
+          evenly = true;
+          best = us;
+          best_limit[kWide] = limit[kWide];
+          best_limit[kNarrow] = limit[kNarrow];
+        }
+      }
+    for (Block &x : blocks) x.n = evenly ? parts_of(x, best_limit) : 0;
+    return evenly ? best : by_share;
   };
   // Blocks of 256 rows; where few of them would find the chip half empty, 32 rows each may be the faster ones (few keys: more workgroups, less of a walk each)
   // or not (many keys: eight times as many are walked).
