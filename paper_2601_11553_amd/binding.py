@@ -690,9 +690,8 @@ class Percache:
         if qkv.dim() != 2 or qkv.dtype != bf16 or qkv.shape[1] != F or not qkv.is_cuda or qkv.stride(1) != 1:
             raise ValueError(f"qkv: a {bf16} tensor [N, {F}] on the GPU with dense rows is wanted, got {qkv.dtype} {tuple(qkv.shape)} strides {qkv.stride()}")
         n = qkv.shape[0]
-        if pos.dim() == 1:
-            pos = pos[None]
-        self._want("pos", pos, (pos.shape[0], n), torch.int32)
+        n_axes = pos.shape[0] if pos.dim() == 2 else 1
+        self._want("pos", pos, (n_axes, n) if pos.dim() == 2 else (n,), torch.int32)
         axis_p = None
         if axis is not None:
             if type(axis) is not np.ndarray or axis.dtype != np.uint8 or not axis.flags.c_contiguous:
@@ -716,7 +715,7 @@ class Percache:
         else:
             self._want("v_out", v_out, (Hkv, n, D), bf16)
         # (a single row has no stride of its own)
-        self._check(self.lib.percache_qkv_norm_rope(self.ctx, qkv.data_ptr(), qkv.stride(0) if n > 1 else F, n, pos.data_ptr(), pos.shape[0], axis_p, _ptr(qkv_bias),
+        self._check(self.lib.percache_qkv_norm_rope(self.ctx, qkv.data_ptr(), qkv.stride(0) if n > 1 else F, n, pos.data_ptr(), n_axes, axis_p, _ptr(qkv_bias),
                                                     _ptr(q_norm), _ptr(k_norm), eps, q_out.data_ptr(), k_out.data_ptr(), v_out.data_ptr(), self._raw_stream()))
         return q_out, k_out, v_out
 

@@ -1226,7 +1226,7 @@ pc_status percache_attention_packed(percache_ctx *ctx, int32_t layer, const void
   for (int s = 0; s < n_seq; ++s)
     if (start_host[s + 1] < start_host[s]) return pc::fail(ctx, PC_EINVAL, "start[%d]=%d lies before start[%d]=%d", s + 1, start_host[s + 1], s, start_host[s]);
   if (start_host[n_seq] > n_rows) return pc::fail(ctx, PC_EINVAL, "start[%d]=%d lies behind the last of %d rows", n_seq, start_host[n_seq], n_rows);
-  if (c.n_q_heads / c.n_kv_heads > 65535) return pc::fail(ctx, PC_ESHAPE, "more than 65535 query heads a kv head");
+  if (c.n_q_heads / c.n_kv_heads > 32767) return pc::fail(ctx, PC_ESHAPE, "more than 32767 query heads a kv head");   // (Args::per_group)
   // (stacked rows of a request, and partial rows, are counted in 32 bits)
   if ((long)n_rows * c.n_q_heads >= (1L << 31)) return pc::fail(ctx, PC_ESHAPE, "%d rows of %d heads are 2^31 or more", n_rows, c.n_q_heads);
   const int cap = max_splits(c, ctx->n_cu, n_seq, n_rows);

@@ -428,6 +428,18 @@ void refusals() {
   expect(percache_qkv_norm_rope(x.ctx, x.arena, 512, INT32_MAX, ints, 1, nullptr, nullptr, nullptr, nullptr, 0.f, x.arena, x.arena, x.arena, nullptr) == PC_ESHAPE, "refusals: rows of a projection");
 }
 
+// A block's rows are told apart by the upper half of a product in place of a division by the heads a kv head.
+void rows_of_heads() {
+  for (uint64_t G = 1; G <= 32767; ++G) {
+    const uint64_t per = (uint32_t)((0xffffffffull + G) / G);
+    bool ok = true;
+    for (uint64_t at : {(uint64_t)1, G - 1, G, 2 * G - 1, 2 * G, (uint64_t)255, (uint64_t)256, G + 254})
+      for (uint64_t x : {at - 1, at, at + 1})
+        if (x < G + 256) ok &= (G == 1 ? x : x * per >> 32) == x / G;
+    expect(ok, "rows: heads of a block");
+  }
+}
+
 // workspaces of the selection: never smaller than what its launches write
 void selection_sizes() {
   Context x(2, 1, 64, 1, 0, 64);
@@ -446,6 +458,7 @@ int main() {
   packed_calls();
   fork_calls();
   refusals();
+  rows_of_heads();
   selection_sizes();
   expect(seen_merges && seen_long && seen_short && seen_kind[0] && seen_kind[1] && seen_rings && seen_store[0] && seen_store[1] && seen_uneven, "calls of every kind");
   std::printf(bad ? "packed driver: %d FAILED checks\n" : "packed driver: ok\n", bad);
