@@ -1024,109 +1024,134 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   // promises 3 % more is taken.  Nothing is faster than its keys come from memory; a merge is a launch and the partial rows.  us at 1, 2, 3, 4
   // partitions, measured: 72 wide blocks of 60 tiles 95, 64, 53, 60; head size 64, 152 of 36 to 60 tiles 84, 80, 70; 144 narrow ones of 52 tiles 53, 62, 53,
   // 59, 32 of them 48, 32, 24, 22, 200 wide ones of 50 to 60 tiles beside the 144 134 (cut evenly into 712 workgroups 151).
-  auto parts_of = [&](const Block &x, const float (&limit)[2]) {
-    const int least = x.kind == kWide ? 6 : 4;   // tiles of a partition
-    return std::max(1, std::min({(int)(tile_us(x) * (float)x.tiles / std::max(limit[x.kind] - kStart, 1.f) + 0.99f), x.tiles / least, kMaxPackedSplits}));
-  };
+  auto least_of = [](int kind) { return kind == kWide ? 6 : 4; };   // tiles of a partition
   const int cus = std::max(1, ctx->n_cu / c.n_kv_heads);
   float mb = 0.f;
   for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
-  std::vector<float> costs, free_at;
-  std::vector<std::pair<float, int>> runs;   // so many workgroups of this cost
+  typedef std::vector<std::pair<float, int>> Runs;   // so many workgroups of this cost; so many CUs that are free at this time
+  Runs runs, free_at;
+  std::vector<float> costs;
   std::vector<int> ends;
-  auto play = [&]() {   // us of workgroups of these costs, longest first
-    float end = costs[0];
-    if ((int)costs.size() <= cus) return end;
-    free_at.assign(costs.begin(), costs.begin() + cus);   // (a heap, the CU that is free first at its head)
-    std::make_heap(free_at.begin(), free_at.end(), std::greater<float>());
-    for (size_t i = cus; i < costs.size(); ++i) {
-      std::pop_heap(free_at.begin(), free_at.end(), std::greater<float>());
-      free_at.back() += costs[i];
-      end = std::max(end, free_at.back());
-      std::push_heap(free_at.begin(), free_at.end(), std::greater<float>());
-    }
-    return end;
+  auto play = [&]() {   // us of the runs, longest first
+    std::sort(runs.begin(), runs.end(), std::greater<std::pair<float, int>>());
+    free_at.assign(1, {0.f, cus});   // (the CUs that are free first at its end)
+    for (auto [cost, count] : runs)
+      while (count > 0) {
+        const auto [at, n] = free_at.back();
+        const int m = std::min(n, count);
+        count -= m;
+        if (m == n) free_at.pop_back();
+        else free_at.back().second -= m;
+        auto to = free_at.end();
+        while (to != free_at.begin() && (to - 1)->first < at + cost) --to;
+        if (to != free_at.begin() && (to - 1)->first == at + cost) (to - 1)->second += m;
+        else free_at.insert(to, {at + cost, m});
+      }
+    return free_at.front().first;
   };
   auto merge_us = [&](float rows) { return rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f; };
+  struct Group { int kind, tiles, count; float tile, rows; };   // blocks that take equally long
+  std::vector<Group> groups;
   auto settle = [&](std::vector<Block> &blocks) {   // chooses the partitions; us
-    float longest[2] = {0.f, 0.f}, whole = 0.f;
-    bool any = false;   // whether a block can be cut
+    int most = 0;
+    for (const Block &x : blocks) most = std::max(most, x.tiles);
+    groups.assign(3 * (size_t)(most + 1), Group{});   // (wide; 17 to 32 rows; fewer)
     for (const Block &x : blocks) {
-      longest[x.kind] = std::max(longest[x.kind], cost_of(x, x.tiles));
-      whole += cost_of(x, x.tiles);
-      any |= x.tiles >= (x.kind == kWide ? 12 : 8);
+      Group &g = groups[(x.kind == kWide ? 0 : x.rows > 16 ? 1 : 2) * (size_t)(most + 1) + x.tiles];
+      g = {x.kind, x.tiles, g.count + 1, tile_us(x), g.rows + (float)x.rows};
     }
-    // The blocks' keys laid end to end and cut where a CU's share ends, the share a little longer from try to try until it is enough: partitions are as long as
-    // a share or what is left of one on either side of a block's end, and the launch puts the latter together again, longest with shortest (the 200 wide blocks
-    // alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64 and 8-bit chunks 67, 59; with the 144 narrow ones 131 uncut, 138).
-    float by_share = 1e30f;
-    int tries = any && (long)blocks.size() <= 4L * cus ? 8 : 0;
-    for (float share = std::max(whole / (float)cus + kStart, 2.f * kStart); tries > 0; share *= 1.05f, --tries) {
-      ends.clear();
-      costs.clear();
-      int bins = 1;
-      float left = share, rows = 0.f;
-      for (const Block &x : blocks) {
-        const int least = x.kind == kWide ? 6 : 4;
-        int n = 0;
-        for (int t = 0; t < x.tiles; ++n) {
-          int can = (int)((left - kStart) / tile_us(x));
-          if (can < std::min(least, x.tiles - t)) {
-            ++bins;
-            left = share;
-            can = std::max(least, (int)((left - kStart) / tile_us(x)));
-          }
-          if (can < x.tiles - t && x.tiles - t - can < least) can = x.tiles - t < 2 * least ? x.tiles - t : x.tiles - t - least;
-          can = std::min(can, x.tiles - t);
-          t += can;
-          left -= cost_of(x, can);
-          costs.push_back(cost_of(x, can));
-          ends.push_back(t);
-        }
-        if (n > 1) rows += (float)(n * x.rows);
-      }
-      if (bins > cus) continue;
-      std::sort(costs.begin(), costs.end(), std::greater<float>());
-      by_share = std::max(play(), mb * kPerMb) + merge_us(rows);
-      break;
+    groups.erase(std::remove_if(groups.begin(), groups.end(), [](const Group &g) { return g.count == 0; }), groups.end());
+    float longest[2] = {0.f, 0.f}, whole = 0.f;
+    for (const Group &g : groups) {
+      const float us = kStart + g.tile * (float)g.tiles;
+      longest[g.kind] = std::max(longest[g.kind], us);
+      whole += us * (float)g.count;
     }
-    // Cut evenly, for limits from the longest block's time down.  (Taken where it promises what the shares do, within 3 %.)
-    float best = by_share * 1.06f, best_limit[2] = {longest[kWide], longest[kNarrow]};
-    bool evenly = false, open = true;   // open: whether finer limits can still be better: their workgroups' time only grows
+    auto parts_of = [&](int kind, float tile, int tiles, const float (&limit)[2]) {
+      return std::max(1, std::min({(int)(tile * (float)tiles / std::max(limit[kind] - kStart, 1.f) + 0.99f), tiles / least_of(kind), kMaxPackedSplits}));
+    };
+    // Cut evenly, for limits from the longest block's time down.
+    float best = 1e30f, best_limit[2] = {longest[kWide], longest[kNarrow]};
+    bool open = true;   // whether finer limits can still be better: their workgroups' time only grows, and there are finer ones
     const float top = std::max(longest[kWide], longest[kNarrow]);
     const bool both = longest[kWide] > 0.f && longest[kNarrow] > 0.f;
-    for (float cut = 1.f; open && cut <= (any ? (float)kMaxPackedSplits : 1.f); cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f)   // (the longest block in so many)
-      for (float cut2 = 1.f; cut2 <= (any && both ? 2.f : 1.f); cut2 *= 2.f) {
+    for (float cut = 1.f; open && cut <= (float)kMaxPackedSplits; cut += cut < 6.f ? 1.f : cut < 16.f ? 2.f : 8.f) {   // (the longest block in so many)
+      open = false;
+      for (float cut2 = 1.f; cut2 <= (both ? 2.f : 1.f); cut2 *= 2.f) {
         const float wide = kStart + (top - kStart) / cut, limit[2] = {wide, std::min(wide, kStart + (longest[kNarrow] - kStart) / cut2)};
         float rows = 0.f, sum = 0.f, end = 0.f;
+        int number = 0;
+        bool finest = true;
         runs.clear();
-        for (const Block &x : blocks) {
-          const int n = parts_of(x, limit);
-          const float each = kStart + tile_us(x) * (float)x.tiles / (float)n;
-          runs.push_back({each, n});
-          sum += each * (float)n;
+        for (const Group &g : groups) {
+          const int n = parts_of(g.kind, g.tile, g.tiles, limit);
+          const float each = kStart + g.tile * (float)g.tiles / (float)n;
+          runs.push_back({each, n * g.count});
+          number += n * g.count;
+          sum += each * (float)(n * g.count);
           end = std::max(end, each);
-          if (n > 1) rows += (float)(n * x.rows);
+          finest &= n == std::max(1, std::min(g.tiles / least_of(g.kind), kMaxPackedSplits));
+          if (n > 1) rows += (float)n * g.rows;
         }
         const float more = merge_us(rows);
-        if (std::max(sum / (float)cus, mb * kPerMb) + more >= 0.97f * best) {
-          open = cut2 > 1.f && open;
-          continue;
-        }
+        if (std::max(sum / (float)cus, mb * kPerMb) + more >= 0.97f * best) continue;
+        open |= !finest;
         if (end + more >= 0.97f * best) continue;
-        std::sort(runs.begin(), runs.end(), std::greater<std::pair<float, int>>());
-        costs.clear();
-        for (const auto &r : runs) costs.insert(costs.end(), r.second, r.first);
-        const float us = std::max(play(), mb * kPerMb) + more;
+        if (number > cus) end = play();
+        const float us = std::max(end, mb * kPerMb) + more;
         if (us < 0.97f * best) {
-          evenly = true;
           best = us;
           best_limit[kWide] = limit[kWide];
           best_limit[kNarrow] = limit[kNarrow];
         }
       }
-    for (Block &x : blocks) x.n = evenly ? parts_of(x, best_limit) : 0;
-    return evenly ? best : by_share;
+    }
+    for (Block &x : blocks) x.n = parts_of(x.kind, tile_us(x), x.tiles, best_limit);
+    // The blocks' keys laid end to end and cut where a CU's share ends, the share a little longer from try to try until it is enough: partitions are as long as
+    // a share or what is left of one on either side of a block's end, and the launch puts the latter together again, longest with shortest (the 200 wide blocks
+    // alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64 and 8-bit chunks 67, 59; with the 144 narrow ones 131 uncut, 138).
+    int tries = (long)blocks.size() <= 4L * cus ? 8 : 0;
+    for (float share = std::max(whole / (float)cus + kStart, 2.f * kStart); tries > 0 && std::max(share, mb * kPerMb) + 3.f < 0.97f * best; share *= 1.05f, --tries) {
+      ends.clear();
+      costs.clear();
+      int bins = 1;
+      float left = share, rows = 0.f;
+      for (const Block &x : blocks) {
+        const int least = least_of(x.kind);
+        const float tile = tile_us(x);
+        int n = 0;
+        for (int t = 0; t < x.tiles; ++n) {
+          int can = (int)((left - kStart) / tile);
+          if (can < std::min(least, x.tiles - t)) {
+            ++bins;
+            left = share;
+            can = std::max(least, (int)((left - kStart) / tile));
+          }
+          if (can < x.tiles - t && x.tiles - t - can < least) can = x.tiles - t < 2 * least ? x.tiles - t : x.tiles - t - least;
+          can = std::min(can, x.tiles - t);
+          t += can;
+          const float us = kStart + tile * (float)can;
+          left -= us;
+          costs.push_back(us);
+          ends.push_back(t);
+        }
+        if (n > 1) rows += (float)(n * x.rows);
+        if (bins > cus) break;
+      }
+      if (bins > cus) continue;
+      std::sort(costs.begin(), costs.end());
+      runs.clear();
+      for (float us : costs)
+        if (!runs.empty() && runs.back().first == us) ++runs.back().second;
+        else runs.push_back({us, 1});
+      const float us = std::max(play(), mb * kPerMb) + merge_us(rows);
+      if (us < 0.97f * best) {
+        best = us;
+        for (Block &x : blocks) x.n = 0;
+      }
+      break;
+    }
+    return best;
   };
   // Blocks of 256 rows; where few of them would find the chip half empty, 32 rows each may be the faster ones (few keys: more workgroups, less of a walk each)
   // or not (many keys: eight times as many are walked).
