@@ -94,7 +94,7 @@ def load_library() -> ctypes.CDLL:
         "percache_kv_put": (_i32, [_vp, _i32, _i32, _vp, _vp, _i32, _vp]),
         "percache_kv_put_batch": (_i32, [_vp, _i32, _pi32, _i32, _vp, _vp, _i32, _vp]),
         "percache_kv_get": (_i32, [_vp, _i32, _i32, _vp, _vp, _pi32, _vp]),
-        "percache_kv_get_batch": (_i32, [_vp, _i32, _pi32, _i32, _vp, _vp, _i32, _vp]),
+        "percache_kv_get_batch": (_i32, [_vp, _i32, _vp, _i32, _vp, _vp, _i32, _vp]),
         "percache_kv_evict": (_i32, [_vp, _i32, _i32]),
         "percache_kv_len": (_i32, [_vp, _i32, _i32]),
         "percache_prefill_workspace_bytes": (_sz, [_vp, _i32, _i32, _i32]),
@@ -381,12 +381,12 @@ class Percache:
     def percache_kv_get_batch(self, layer: int, slots, n_tokens: int, k_out=None, v_out=None):
         """The first n_tokens tokens of every slot named, as [n, Hkv, n_tokens, D] tensors (one launch)."""
         import torch
-        arr, p = _host_i32(slots)
+        arr, p = _i32_list(slots)
         shape = (len(arr), self.cfg.n_kv_heads, n_tokens, self.cfg.head_dim)
         if k_out is None:
             k_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-            v_out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
-        self._check(self.lib.percache_kv_get_batch(self.ctx, layer, p, len(arr), _ptr(k_out), _ptr(v_out), n_tokens, _stream()))
+            v_out = k_out.new_empty(shape)
+        self._check(self.lib.percache_kv_get_batch(self.ctx, layer, p, len(arr), _ptr(k_out), _ptr(v_out), n_tokens, self._raw_stream()))
         return k_out, v_out
 
     def percache_kv_slice(self, layer: int, k, v, bounds, slots):
