@@ -984,13 +984,9 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   const percache_config &c = ctx->cfg;
   const int G = c.n_q_heads / c.n_kv_heads;
   struct Block { int seq, r_first, rows, kind, tiles, n; };   // n: partitions (0: they end where `ends` says)
-  // us of a workgroup's start and end, and of a tile (most of the chip at work: the clock falls; alone 1.45 at head size 128), us of a MB from memory
-  constexpr float kStart = 6.f, kPerMb = 1.f / 5.4f;
-  const bool d128 = c.head_dim == 128;
-  auto tile_us = [&](const Block &b) { return b.kind == kWide ? (d128 ? 1.85f : 1.28f) : b.rows > 16 ? (d128 ? 0.88f : 0.52f) : d128 ? 0.72f : 0.45f; };
-  auto cost_of = [&](const Block &b, int tiles) { return kStart + tile_us(b) * (float)tiles; };
   std::vector<int32_t> ents, first_ent(n_seq + 1), tiles_before;   // entries with keys; cached tiles before each
   std::vector<int> cached(n_seq);
+  long tiles8 = 0, all_tiles = 0;
   for (int s = 0; s < n_seq; ++s) {
     first_ent[s] = (int)ents.size() / 2;
     int tiles = 0;
@@ -1002,10 +998,25 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
         ents.push_back(used);
         tiles_before.push_back(tiles);
         tiles += (used + TK - 1) / TK;
+        if (ctx->is8(slot)) tiles8 += (used + TK - 1) / TK;
       }
+    all_tiles += tiles + (start[s + 1] - start[s] + TK - 1) / TK;
     cached[s] = tiles;
   }
   first_ent[n_seq] = (int)ents.size() / 2;
+  // us of a workgroup's start and end, of a MB from memory and of a tile of more than 128 rows, of more than 32, 16, fewer (most of the chip at work: the clock
+  // falls; alone 1.37 and 1.11 of the first two at head size 128, 1.02 and 0.78 at 64), of 8-bit tiles 2.4, 1.57, ..
+  constexpr float kStart = 6.f, kStartLow = 4.f, kPerMb = 1.f / 5.4f;
+  constexpr float kTile[2][2][4] = {{{1.28f, 0.97f, 0.52f, 0.45f}, {1.55f, 1.07f, 0.60f, 0.52f}}, {{1.85f, 1.54f, 0.88f, 0.72f}, {2.40f, 1.57f, 0.76f, 0.65f}}};
+  float tile_of[4];
+  for (int i = 0; i < 4; ++i) {
+    const auto &t = kTile[c.head_dim == 128];
+    tile_of[i] = t[0][i] + (t[1][i] - t[0][i]) * (float)tiles8 / (float)std::max(all_tiles, 1L);
+  }
+  auto class_of = [](const Block &b) { return b.kind == kWide ? b.rows <= kWideRows / 2 : b.rows > 16 ? 2 : 3; };
+  auto start_us = [&](const Block &b) { return class_of(b) == 1 ? kStartLow : kStart; };
+  auto tile_us = [&](const Block &b) { return tile_of[class_of(b)]; };
+  auto cost_of = [&](const Block &b, int tiles) { return start_us(b) + tile_us(b) * (float)tiles; };
   auto cut = [&](int height) {   // blocks of so many rows, the last of a request narrow where 32 rows are left
     std::vector<Block> blocks;
     for (int s = 0; s < n_seq; ++s) {
@@ -1049,21 +1060,21 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
       }
     return free_at.front().first;
   };
-  auto merge_us = [&](float rows) { return rows > 0.f ? 3.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f; };
-  struct Group { int kind, tiles, count; float tile, rows; };   // blocks that take equally long
+  auto merge_us = [&](float rows) { return rows > 0.f ? 4.5f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f; };
+  struct Group { int kind, tiles, count; float start, tile, rows; };   // blocks that take equally long
   std::vector<Group> groups;
   auto settle = [&](std::vector<Block> &blocks) {   // chooses the partitions; us
     int most = 0;
     for (const Block &x : blocks) most = std::max(most, x.tiles);
-    groups.assign(3 * (size_t)(most + 1), Group{});   // (wide; 17 to 32 rows; fewer)
+    groups.assign(4 * (size_t)(most + 1), Group{});   // (more than 128 rows; more than 32; more than 16; fewer)
     for (const Block &x : blocks) {
-      Group &g = groups[(x.kind == kWide ? 0 : x.rows > 16 ? 1 : 2) * (size_t)(most + 1) + x.tiles];
-      g = {x.kind, x.tiles, g.count + 1, tile_us(x), g.rows + (float)x.rows};
+      Group &g = groups[class_of(x) * (size_t)(most + 1) + x.tiles];
+      g = {x.kind, x.tiles, g.count + 1, start_us(x), tile_us(x), g.rows + (float)x.rows};
     }
     groups.erase(std::remove_if(groups.begin(), groups.end(), [](const Group &g) { return g.count == 0; }), groups.end());
     float longest[2] = {0.f, 0.f}, whole = 0.f;
     for (const Group &g : groups) {
-      const float us = kStart + g.tile * (float)g.tiles;
+      const float us = g.start + g.tile * (float)g.tiles;
       longest[g.kind] = std::max(longest[g.kind], us);
       whole += us * (float)g.count;
     }
@@ -1085,7 +1096,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
         runs.clear();
         for (const Group &g : groups) {
           const int n = parts_of(g.kind, g.tile, g.tiles, limit);
-          const float each = kStart + g.tile * (float)g.tiles / (float)n;
+          const float each = g.start + g.tile * (float)g.tiles / (float)n;
           runs.push_back({each, n * g.count});
           number += n * g.count;
           sum += each * (float)(n * g.count);
@@ -1111,26 +1122,26 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     // a share or what is left of one on either side of a block's end, and the launch puts the latter together again, longest with shortest (the 200 wide blocks
     // alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64 and 8-bit chunks 67, 59; with the 144 narrow ones 131 uncut, 138).
     int tries = (long)blocks.size() <= 4L * cus ? 8 : 0;
-    for (float share = std::max(whole / (float)cus + kStart, 2.f * kStart); tries > 0 && std::max(share, mb * kPerMb) + 3.f < 0.97f * best; share *= 1.05f, --tries) {
+    for (float share = std::max(whole / (float)cus + kStart, 2.f * kStart); tries > 0 && std::max(share, mb * kPerMb) + merge_us(1.f) < 0.97f * best; share *= 1.05f, --tries) {
       ends.clear();
       costs.clear();
       int bins = 1;
       float left = share, rows = 0.f;
       for (const Block &x : blocks) {
         const int least = least_of(x.kind);
-        const float tile = tile_us(x);
+        const float start = start_us(x), tile = tile_us(x);
         int n = 0;
         for (int t = 0; t < x.tiles; ++n) {
-          int can = (int)((left - kStart) / tile);
+          int can = (int)((left - start) / tile);
           if (can < std::min(least, x.tiles - t)) {
             ++bins;
             left = share;
-            can = std::max(least, (int)((left - kStart) / tile));
+            can = std::max(least, (int)((left - start) / tile));
           }
           if (can < x.tiles - t && x.tiles - t - can < least) can = x.tiles - t < 2 * least ? x.tiles - t : x.tiles - t - least;
           can = std::min(can, x.tiles - t);
           t += can;
-          const float us = kStart + tile * (float)can;
+          const float us = start + tile * (float)can;
           left -= us;
           costs.push_back(us);
           ends.push_back(t);
@@ -1153,17 +1164,26 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     }
     return best;
   };
-  // Blocks of 256 rows; where few of them would find the chip half empty, 32 rows each may be the faster ones (few keys: more workgroups, less of a walk each)
-  // or not (many keys: eight times as many are walked).
+  // Blocks of 256 rows; where few of them would find the chip half empty, 128 or 32 rows each may be the faster ones (few keys: more workgroups, less of a start
+  // and a walk each) or not (many keys: two and eight times as many are walked).  A walk of 20 tiles at head size 128: 8 blocks of 256 rows 37.5 us, 16 of
+  // 128 30; 64 and 128 39, 32; 128 and 256 42.3, 36.8.
   std::vector<Block> blocks = cut(kWideRows);
   const bool choose = n_splits <= 0 && (long)blocks.size() <= 8L * cus;
-  const float by_wide = choose ? settle(blocks) : 0.f;
-  if ((long)blocks.size() * 2 <= cus) {
-    std::vector<Block> low = cut(kNarrowRows);
-    const std::vector<int> of_wide = ends;
-    if ((long)low.size() <= 2L * cus && (!choose || settle(low) < by_wide)) blocks = std::move(low);
-    else ends = of_wide;
-  }
+  float best = choose ? settle(blocks) : 0.f;
+  std::vector<int> best_ends = ends;
+  auto lower = [&](int height, long most) {
+    std::vector<Block> low = cut(height);
+    if ((long)low.size() > most) return;
+    const float us = choose ? settle(low) : -1.f;
+    if (us >= best) return;
+    best = us;
+    best_ends = ends;
+    blocks = std::move(low);
+  };
+  const long tall = (long)blocks.size();
+  if (choose && tall * 2 <= cus) lower(kWideRows / 2, 2L * cus);
+  if (tall * 2 <= cus) lower(kNarrowRows, 2L * cus);
+  ends = std::move(best_ends);
   if (n_splits > 0)
     for (Block &x : blocks) x.n = std::min(n_splits, x.tiles);
   struct Unit { int block, begin, end; float cost; int part; };
