@@ -1035,7 +1035,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   // promises 3 % more is taken.  Nothing is faster than its keys come from memory; a merge is a launch and the partial rows.  us at 1, 2, 3, 4
   // partitions, measured: 72 wide blocks of 60 tiles 95, 64, 53, 60; head size 64, 152 of 36 to 60 tiles 84, 80, 70; 144 narrow ones of 52 tiles 53, 62, 53,
   // 59, 32 of them 48, 32, 24, 22, 200 wide ones of 50 to 60 tiles beside the 144 134 (cut evenly into 712 workgroups 151).
-  auto least_of = [](int kind) { return kind == kWide ? 6 : 4; };   // tiles of a partition
+  auto least_of = [&](const Block &b) { return class_of(b) == 0 ? 6 : 4; };   // tiles of a partition
   const int cus = std::max(1, ctx->n_cu / c.n_kv_heads);
   float mb = 0.f;
   for (int s = 0; s < n_seq; ++s) mb += (float)cached[s] * (float)(TK * c.head_dim * 4 * c.n_kv_heads) * 1e-6f;
@@ -1060,8 +1060,8 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
       }
     return free_at.front().first;
   };
-  auto merge_us = [&](float rows) { return rows > 0.f ? 4.5f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f; };
-  struct Group { int kind, tiles, count; float start, tile, rows; };   // blocks that take equally long
+  auto merge_us = [&](float rows) { return rows > 0.f ? 5.f + rows * (float)(c.n_kv_heads * c.head_dim) * 1e-6f : 0.f; };
+  struct Group { int kind, tiles, count, least; float start, tile, rows; };   // blocks that take equally long
   std::vector<Group> groups;
   auto settle = [&](std::vector<Block> &blocks) {   // chooses the partitions; us
     int most = 0;
@@ -1069,7 +1069,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     groups.assign(4 * (size_t)(most + 1), Group{});   // (more than 128 rows; more than 32; more than 16; fewer)
     for (const Block &x : blocks) {
       Group &g = groups[class_of(x) * (size_t)(most + 1) + x.tiles];
-      g = {x.kind, x.tiles, g.count + 1, start_us(x), tile_us(x), g.rows + (float)x.rows};
+      g = {x.kind, x.tiles, g.count + 1, least_of(x), start_us(x), tile_us(x), g.rows + (float)x.rows};
     }
     groups.erase(std::remove_if(groups.begin(), groups.end(), [](const Group &g) { return g.count == 0; }), groups.end());
     float longest[2] = {0.f, 0.f}, whole = 0.f;
@@ -1078,8 +1078,8 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
       longest[g.kind] = std::max(longest[g.kind], us);
       whole += us * (float)g.count;
     }
-    auto parts_of = [&](int kind, float tile, int tiles, const float (&limit)[2]) {
-      return std::max(1, std::min({(int)(tile * (float)tiles / std::max(limit[kind] - kStart, 1.f) + 0.99f), tiles / least_of(kind), kMaxPackedSplits}));
+    auto parts_of = [&](int kind, int least, float start, float tile, int tiles, const float (&limit)[2]) {
+      return std::max(1, std::min({(int)(tile * (float)tiles / std::max(limit[kind] - start, 1.f) + 0.99f), tiles / least, kMaxPackedSplits}));
     };
     // Cut evenly, for limits from the longest block's time down.
     float best = 1e30f, best_limit[2] = {longest[kWide], longest[kNarrow]};
@@ -1095,13 +1095,13 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
         bool finest = true;
         runs.clear();
         for (const Group &g : groups) {
-          const int n = parts_of(g.kind, g.tile, g.tiles, limit);
+          const int n = parts_of(g.kind, g.least, g.start, g.tile, g.tiles, limit);
           const float each = g.start + g.tile * (float)g.tiles / (float)n;
           runs.push_back({each, n * g.count});
           number += n * g.count;
           sum += each * (float)(n * g.count);
           end = std::max(end, each);
-          finest &= n == std::max(1, std::min(g.tiles / least_of(g.kind), kMaxPackedSplits));
+          finest &= n == std::max(1, std::min(g.tiles / g.least, kMaxPackedSplits));
           if (n > 1) rows += (float)n * g.rows;
         }
         const float more = merge_us(rows);
@@ -1117,7 +1117,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
         }
       }
     }
-    for (Block &x : blocks) x.n = parts_of(x.kind, tile_us(x), x.tiles, best_limit);
+    for (Block &x : blocks) x.n = parts_of(x.kind, least_of(x), start_us(x), tile_us(x), x.tiles, best_limit);
     // The blocks' keys laid end to end and cut where a CU's share ends, the share a little longer from try to try until it is enough: partitions are as long as
     // a share or what is left of one on either side of a block's end, and the launch puts the latter together again, longest with shortest (the 200 wide blocks
     // alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64 and 8-bit chunks 67, 59; with the 144 narrow ones 131 uncut, 138).
@@ -1128,7 +1128,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
       int bins = 1;
       float left = share, rows = 0.f;
       for (const Block &x : blocks) {
-        const int least = least_of(x.kind);
+        const int least = least_of(x);
         const float start = start_us(x), tile = tile_us(x);
         int n = 0;
         for (int t = 0; t < x.tiles; ++n) {
