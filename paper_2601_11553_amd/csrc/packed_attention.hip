@@ -15,7 +15,7 @@
 //
 // What bounds it: prompts the matrix products and, at their rate, the power (32 heads over 8, ten prompts of 574 to 6964 tokens: 895 us, 1.04 PFLOP/s of the
 // scores that count; a tile of 256 rows takes 3350 cycles, 2048 of them products, at 1.5 GHz with all CUs on such data); single tokens the key stream (32 tokens over 6100 cached
-// keys each, 700 MB: 120 us, 5.8 TB/s); short calls the launch (5 prompts of 11 to 71 tokens: 8.4 us).  256 rows a block: fewer would read every tile
+// keys each, 700 MB: 120 us, 5.8 TB/s); short calls the launch (5 prompts of 11 to 71 tokens: 7.8 us).  256 rows a block: fewer would read every tile
 // from LDS and memory more often, a wavefront's 32 are what its registers hold beside the scores of 64 keys.
 #include <algorithm>
 #include <exception>
