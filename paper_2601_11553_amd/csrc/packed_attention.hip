@@ -1081,6 +1081,17 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     auto parts_of = [&](int kind, int least, float start, float tile, int tiles, const float (&limit)[2]) {
       return std::max(1, std::min({(int)(tile * (float)tiles / std::max(limit[kind] - start, 1.f) + 0.99f), tiles / least, kMaxPackedSplits}));
     };
+    if (n_splits > 0) {   // the partitions asked for
+      float rows = 0.f;
+      runs.clear();
+      for (const Group &g : groups) {
+        const int n = std::min(n_splits, g.tiles);
+        runs.push_back({g.start + g.tile * (float)g.tiles / (float)n, n * g.count});
+        if (n > 1) rows += (float)n * g.rows;
+      }
+      for (Block &x : blocks) x.n = std::min(n_splits, x.tiles);
+      return std::max(play(), mb * kPerMb) + merge_us(rows);
+    }
     // Cut evenly, for limits from the longest block's time down.
     float best = 1e30f, best_limit[2] = {longest[kWide], longest[kNarrow]};
     bool open = true;   // whether finer limits can still be better: their workgroups' time only grows, and there are finer ones
@@ -1165,27 +1176,24 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     return best;
   };
   // Blocks of 256 rows; where few of them would find the chip half empty, 128 or 32 rows each may be the faster ones (few keys: more workgroups, less of a start
-  // and a walk each) or not (many keys: two and eight times as many are walked).  A walk of 20 tiles at head size 128: 8 blocks of 256 rows 37.5 us, 16 of
-  // 128 30; 64 and 128 39, 32; 128 and 256 42.3, 36.8.
+  // and a walk each) or not (many keys: two and eight times as many are walked), whether the partitions are asked for or chosen.  A walk of 20 tiles at
+  // head size 128: 8 blocks of 256 rows 37.5 us, 16 of 128 30; 64 and 128 39, 32; 128 and 256 42.3, 36.8.
   std::vector<Block> blocks = cut(kWideRows);
-  const bool choose = n_splits <= 0 && (long)blocks.size() <= 8L * cus;
-  float best = choose ? settle(blocks) : 0.f;
+  float best = n_splits > 0 || (long)blocks.size() <= 8L * cus ? settle(blocks) : 0.f;   // (more blocks than that even out uncut)
   std::vector<int> best_ends = ends;
   auto lower = [&](int height, long most) {
     std::vector<Block> low = cut(height);
     if ((long)low.size() > most) return;
-    const float us = choose ? settle(low) : -1.f;
+    const float us = settle(low);
     if (us >= best) return;
     best = us;
     best_ends = ends;
     blocks = std::move(low);
   };
   const long tall = (long)blocks.size();
-  if (choose && tall * 2 <= cus) lower(kWideRows / 2, 2L * cus);
+  if (tall * 2 <= cus) lower(kWideRows / 2, 2L * cus);
   if (tall * 2 <= cus) lower(kNarrowRows, 2L * cus);
   ends = std::move(best_ends);
-  if (n_splits > 0)
-    for (Block &x : blocks) x.n = std::min(n_splits, x.tiles);
   struct Unit { int block, begin, end; float cost; int part; };
   std::vector<Unit> units;
   long part_rows = 0, more = ws.most_items - (long)blocks.size();

@@ -1,0 +1,34 @@
+"""Packed calls whose blocks are tall: shapes shared by the GPU tests of the attention and by the CPU test that says which kind of work each of them plans.
+
+A shape is (heads, kv heads, head size, rows of every request, used lengths of every request's chunks or None, capacity).  A request's rows are cut into blocks
+of 256 stacked rows (row = token * heads a kv head + head), the last one shorter, of at most 32 where that is what is left; where the 256s fill less than half of the
+CUs of a kv head, into 128s or 32s instead.  So the 256s stay where there are few kv heads' CUs for many rows."""
+import numpy as np
+
+# many kv heads: short requests fill their CUs
+TALL = {
+    "32over32x64": (32, 32, 64, [300, 1, 257, 513, 40], [[100, 64, 3], [1, 0, 64], [128, 128, 65], [63, 0, 0], [127, 1, 2]], 128),
+    "32over32x128": (32, 32, 128, [290, 2, 260, 511], [[70, 64], [128, 5], [127, 0], [3, 65]], 128),
+    "32over8x128": (32, 8, 128, [300, 700, 411], [[190, 64], [65, 1], [192, 130]], 192),
+    "14over2x64": (14, 2, 64, [900, 1, 700, 810], [[200, 64], [0, 256], [255, 1], [65, 130]], 256),
+    "24over8x128_nothing_cached": (24, 8, 128, [513, 350, 640, 31], None, 64),
+    "16over16x64_many_chunks": (16, 16, 64, [600, 1000, 513], [[7] * 70, [64, 1] * 35, [40] * 70], 64),
+    "32over8x128_many_chunks": (32, 8, 128, [500, 450, 200], [[64, 5] * 33, [1] * 66, [50, 64] * 33], 64),
+}
+# few requests: blocks of 128 rows
+MIDDLE = {
+    "6over2x128": (6, 2, 128, [600], [[511, 300]], 512),
+    "8over1x64": (8, 1, 64, [700, 430], [[500, 511, 130], [512, 3, 60]], 512),
+    "8over2x128": (8, 2, 128, [513, 300], [[512, 400], [63, 512]], 512),
+}
+
+
+def slots_of(shape):
+    """Tokens of every slot, the slots of every request's chunks (or None) and how many of their tokens count."""
+    _, _, _, T, used, C = shape
+    n_c = len(used[0]) if used else 0
+    tokens = [C if s % 3 else max(1, C - 7) for s in range(max(2, len(T) * n_c))]
+    if not n_c:
+        return tokens, None, None
+    ids = np.random.default_rng(len(tokens)).permutation(len(T) * n_c).reshape(len(T), n_c)
+    return tokens, ids, np.minimum(np.array(used, np.int32), np.array(tokens, np.int32)[ids])

@@ -1,0 +1,63 @@
+// What calls of given shapes plan: the stand-in runtime of packed_driver.cpp, the calls from standard input, one a line:
+//   Hq Hkv D n_slots n_slots_8bit capacity  tokens of every slot  n_splits n_requests chunks  rows of every request  slots, used lengths of its chunks
+// and for each call a line "call STATUS ITEMS MERGES LISTS_IN_ARGUMENTS" and its items, a line each:
+//   rows kind cached_tiles fresh_tiles partial entries bf16 8-bit    (partial: 1 for one of several partitions; bf16, 8-bit: whether it walks such chunks)
+// Built and run by tests/test_packed_shapes.py.
+#define main main_of_packed_driver
+#include "packed_driver.cpp"
+#undef main
+
+#include <iostream>
+
+namespace {
+void one_call(int Hq, int Hkv, int D, int n_slots, int n8, int C) {
+  auto read = [](int n) {
+    std::vector<int32_t> v(n);
+    for (int32_t &x : v) std::cin >> x;
+    return v;
+  };
+  Context x(Hq, Hkv, D, n_slots, n8, C);
+  const std::vector<int32_t> tokens = read(n_slots);
+  for (int s = 0; s < n_slots; ++s)
+    if (tokens[s]) x.put(0, s, tokens[s]);
+  const std::vector<int32_t> head = read(3), T = read(head[1]);
+  const int n_splits = head[0], B = head[1], chunks = head[2];
+  std::vector<int32_t> start(B + 1, 0), n_chunks(B, chunks), ids, used;
+  for (int b = 0; b < B; ++b) {
+    start[b + 1] = start[b] + T[b];
+    for (int j = 0; j < chunks; ++j) {
+      const auto e = read(2);
+      ids.push_back(e[0]);
+      used.push_back(e[1]);
+    }
+  }
+  const size_t bytes = percache_packed_workspace_bytes(x.ctx, B, start[B], chunks);
+  void *ws = aligned(bytes);
+  packed.clear();
+  const pc_status st = percache_attention_packed(x.ctx, 0, x.arena, x.arena, x.arena, start[B], start.data(), B, ids.data(), used.data(), n_chunks.data(), chunks,
+                                                 std::min(n_splits, percache_packed_max_splits(x.ctx, B, start[B])), x.arena, nullptr, ws, bytes, nullptr);
+  const int n_items = packed.empty() ? 0 : packed[0].a.merges_at / kItemWords;
+  std::printf("call %d %d %d %d\n", (int)st, n_items, packed.size() == 2 ? (int)packed[1].grid.x : 0, packed.empty() || packed[0].in_args);
+  for (int i = 0; i < n_items; ++i) {
+    const Packed &p = packed[0];
+    Item it;
+    memcpy(&it, p.words.data() + (size_t)i * kItemWords, sizeof it);
+    int entries = 0, formats[2] = {0, 0};
+    for (int tiles = -it.tile0; it.n_cached && tiles < it.n_cached; ++entries) {
+      const int32_t *e = p.words.data() + p.a.ents_at + 2 * (it.ent + entries);
+      formats[e[0] >= n_slots - n8] = 1;
+      tiles += (e[1] + 63) / 64;
+    }
+    std::printf("%d %d %d %d %d %d %d %d\n", it.rows(), it.kind(), it.n_cached, it.f1 - it.f0, it.part >= 0, entries, formats[0], formats[1]);
+  }
+  std::free(ws);
+}
+}  // namespace
+
+int main(int argc, char **argv) {
+  const std::string what = argc > 1 ? argv[1] : "";
+  int Hq, Hkv, D, n_slots, n8, C;
+  while (what == "calls" && std::cin >> Hq >> Hkv >> D >> n_slots >> n8 >> C) one_call(Hq, Hkv, D, n_slots, n8, C);
+  std::printf(bad ? "shapes driver: %d FAILED checks\n" : "shapes driver: ok\n", bad);
+  return bad ? 1 : 0;
+}

@@ -1,0 +1,88 @@
+"""What calls on packed rows plan, on the CPU (tests/sanitize/packed_shapes_driver.cpp: the library's host code, sanitizers on, over a stand-in runtime):
+which blocks, partitions and formats the shapes of the GPU tests reach, so that no later rule empties these tests unseen; limits of launches and workspaces."""
+import os
+import re
+import shutil
+import subprocess
+from collections import Counter, namedtuple
+from concurrent.futures import ThreadPoolExecutor
+
+import pytest
+
+from packed_shapes import MIDDLE, TALL, slots_of
+from test_sanitizers import ENV, ROOT, SAN, _clean, _run
+
+pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"), reason="no hipcc")
+Item = namedtuple("Item", "rows kind cached fresh partial entries bf16 eight")
+FORMATS = {"bf16": 0, "8bit": 1, "mixed": 2}
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    from paper_2601_11553_amd.build import CSRC, FLAGS, HIPCC, SOURCES
+    at = tmp_path_factory.mktemp("shapes")
+    flags = [f for f in FLAGS if f != "-O3"] + [*SAN, "-fno-gpu-sanitize", "--cuda-host-only", "-Wno-division-by-zero"]
+
+    def compile_one(src):
+        obj = str(at / (os.path.splitext(os.path.basename(src))[0] + ".o"))
+        _run([HIPCC, *flags, "-x", "hip", "-c", src, "-o", obj])
+        return obj
+
+    sources = [os.path.join(CSRC, s) for s in SOURCES] + [os.path.join(ROOT, "tests", "sanitize", "packed_shapes_driver.cpp")]
+    with ThreadPoolExecutor(max_workers=4) as ex:
+        objs = list(ex.map(compile_one, sources))
+    # (no device code: its place in the registration stays empty)
+    names = subprocess.run(["nm", "-u", *objs], capture_output=True, text=True, check=True).stdout
+    empty = [f"-Wl,--defsym={n}=0" for n in sorted(set(re.findall(r"__hip_fatbin_\w+", names)))]
+    exe = str(at / "shapes_driver")
+    clang = os.path.join(os.path.dirname(os.path.realpath(HIPCC)), "..", "lib", "llvm", "bin", "clang++")
+    _run([clang, "-no-pie", *SAN, *objs, *empty, "-o", exe])
+
+    def run(what, lines=()):
+        r = subprocess.run([exe, what], env=ENV, capture_output=True, text=True, input="\n".join(lines))
+        _clean(r)
+        assert r.returncode == 0 and "shapes driver: ok" in r.stdout, r.stdout[-3000:]
+        return r.stdout
+    return run
+
+
+def line(shape, formats, n_splits):
+    Hq, Hkv, D, T, _, C = shape
+    tokens, ids, used = slots_of(shape)
+    n = len(tokens)
+    words = [Hq, Hkv, D, n, {"bf16": 0, "8bit": n, "mixed": n // 2}[formats], C, *tokens, n_splits, len(T), 0 if ids is None else ids.shape[1], *T]
+    if ids is not None:
+        words += [int(x) for pair in zip(ids.ravel(), used.ravel()) for x in pair]
+    return " ".join(map(str, words))
+
+
+def plans(driver, calls):
+    """The items of every (shape, formats, n_splits)."""
+    out = []
+    for text in driver("calls", [line(*c) for c in calls]).splitlines():
+        if text.startswith("call"):
+            assert text.split()[1] == "0", text
+            out.append([])
+        elif text[0].isdigit():
+            out[-1].append(Item(*map(int, text.split())))
+    assert len(out) == len(calls) and all(out)
+    return out
+
+
+def classes(items):
+    """How many items of more than 128 rows, of more than 32, of more than 16 and of fewer there are, whole and in partitions."""
+    return Counter(("tall" if i.rows > 128 else "middle" if i.kind == 0 else "low" if i.rows > 16 else "few", bool(i.partial)) for i in items)
+
+
+def test_blocks_where_partitions_are_asked_for(driver):
+    """The height of the blocks goes by the time that each promises there too: one partition gives what the library's own choice gives where that is uncut, and
+    many keys that are cut into several are not walked by blocks of 32 rows."""
+    short = {"8over2x128": (8, 2, 128, [128, 64, 96], None, 64), "6over2x64": (6, 2, 64, [120, 100], [[0], [1]], 64)}
+    uncut = [(s, f, n) for s in [*short.values(), *(TALL[x] for x in ("32over32x64", "32over32x128", "32over8x128", "24over8x128_nothing_cached"))]
+             for f in ("bf16", "mixed") for n in (0, 1)]
+    got = plans(driver, uncut)
+    for i in range(0, len(got), 2):
+        assert not any(x.partial for x in got[i]) and got[i] == got[i + 1], uncut[i]
+    assert all(classes(x)["middle", False] for x in got[:8])
+    for c, items in zip(many := [(s, f, n) for s in MIDDLE.values() for f in ("bf16", "8bit", "mixed") for n in (3, 7)], plans(driver, many)):
+        assert classes(items)["low", True] == 0 and (classes(items)["middle", True] or classes(items)["tall", True]), c
