@@ -159,14 +159,15 @@ extern "C" pc_status percache_qkv_norm_rope(percache_ctx *ctx, const void *qkv_d
   // A head for every group of lanes while that fills the chip; then several; past what the last-level cache holds, loads and stores that are not kept (48 heads
   // of 128, 4000 rows 20.4 us kept, 21.6 not; 8000 rows 40.0, 38.9; 16384 rows 84.6, 75.2 and with four heads a group 78: 5.4 TB/s, what a copy of 200 MB reaches).
   const long groups = (long)n_rows * heads;
-  if (groups >= 1L << 31) return pc::fail(ctx, PC_ESHAPE, "%d rows of %d heads are 2^31 or more", n_rows, heads);   // (a grid has fewer than 2^32 threads)
-#define PC_NR(DD, HH, OO)                                                                                                   \
-  hipLaunchKernelGGL((norm_rope_kernel<DD, HH, OO>), dim3((unsigned)(((long)n_rows * ((heads + HH - 1) / HH) * lanes + 255) / 256)), dim3(256), 0, s, a)
-#define PC_NR_D(DD)                                                                     \
-  do {                                                                                  \
-    if (groups * lanes <= 64L * 16 * ctx->n_cu) PC_NR(DD, 1, false);                    \
-    else if (groups * c.head_dim * 4 <= 160L << 20) PC_NR(DD, 4, false);                \
-    else PC_NR(DD, 2, true);                                                            \
+  const int each = groups * lanes <= 64L * 16 * ctx->n_cu ? 1 : groups * c.head_dim * 4 <= 160L << 20 ? 4 : 2;
+  const long blocks = ((long)n_rows * ((heads + each - 1) / each) * lanes + 255) / 256;
+  if (blocks >= 1L << 24) return pc::fail(ctx, PC_ESHAPE, "%d rows of %d heads are 2^24 workgroups or more", n_rows, heads);   // (a grid has fewer than 2^32 threads)
+#define PC_NR(DD, HH, OO) hipLaunchKernelGGL((norm_rope_kernel<DD, HH, OO>), dim3((unsigned)blocks), dim3(256), 0, s, a)
+#define PC_NR_D(DD)                          \
+  do {                                       \
+    if (each == 1) PC_NR(DD, 1, false);      \
+    else if (each == 4) PC_NR(DD, 4, false); \
+    else PC_NR(DD, 2, true);                 \
   } while (0)
   if (c.head_dim == 128) PC_NR_D(128); else PC_NR_D(64);
 #undef PC_NR_D

@@ -10,6 +10,20 @@
 #include <iostream>
 
 namespace {
+// Rows of a projection: as many as a launch of fewer than 2^32 threads holds, and one more.
+void rows_of_a_launch() {
+  struct Heads { int q, kv, D, threads; };   // threads a row, two heads a group of D / 16 lanes
+  for (const Heads &h : {Heads{3, 3, 128, 40}, Heads{4, 2, 128, 32}, Heads{14, 2, 64, 36}, Heads{4, 2, 64, 16}}) {
+    Context x(h.q, h.kv, h.D, 1, 0, 64);
+    const long most = (((1L << 24) - 1) * 256) / h.threads;   // (2^24 workgroups of 256 are 2^32 threads)
+    auto rows = [&](long n) {
+      return percache_qkv_norm_rope(x.ctx, x.arena, (h.q + 2 * h.kv) * h.D, (int32_t)n, (int32_t *)x.arena, 1, nullptr, nullptr, nullptr, nullptr, 0.f, x.arena, x.arena, x.arena, nullptr);
+    };
+    expect(rows(std::min<long>(most, INT32_MAX)) == PC_OK, "rows: what a launch holds");
+    if (most < INT32_MAX) expect(rows(most + 1) == PC_ESHAPE && rows(std::min<long>(2 * most, INT32_MAX)) == PC_ESHAPE, "rows: more than a launch holds");
+  }
+}
+
 void one_call(int Hq, int Hkv, int D, int n_slots, int n8, int C) {
   auto read = [](int n) {
     std::vector<int32_t> v(n);
@@ -56,6 +70,7 @@ void one_call(int Hq, int Hkv, int D, int n_slots, int n8, int C) {
 
 int main(int argc, char **argv) {
   const std::string what = argc > 1 ? argv[1] : "";
+  if (what == "rows") rows_of_a_launch();
   int Hq, Hkv, D, n_slots, n8, C;
   while (what == "calls" && std::cin >> Hq >> Hkv >> D >> n_slots >> n8 >> C) one_call(Hq, Hkv, D, n_slots, n8, C);
   std::printf(bad ? "shapes driver: %d FAILED checks\n" : "shapes driver: ok\n", bad);

@@ -86,3 +86,7 @@ def test_blocks_where_partitions_are_asked_for(driver):
     assert all(classes(x)["middle", False] for x in got[:8])
     for c, items in zip(many := [(s, f, n) for s in MIDDLE.values() for f in ("bf16", "8bit", "mixed") for n in (3, 7)], plans(driver, many)):
         assert classes(items)["low", True] == 0 and (classes(items)["middle", True] or classes(items)["tall", True]), c
+
+
+def test_rows_of_a_projection_that_a_launch_holds(driver):
+    driver("rows")
