@@ -951,9 +951,12 @@ struct PackedWs {
   size_t total;
 };
 long most_blocks(const percache_config &c, int n_seq, int n_rows) { return (long)(c.n_q_heads / c.n_kv_heads) * n_rows / kNarrowRows + n_seq; }
-long most_part_rows(const percache_config &c, int n_cu, int n_rows) {   // of one kv head
-  const long rows = (long)(c.n_q_heads / c.n_kv_heads) * n_rows;
-  return std::max(rows, std::min(rows * kMaxPackedSplits, 2L * n_cu * kWideRows / c.n_kv_heads));
+// Partial rows of one kv head.  As many as there are rows, at least two partitions of 256 rows a CU: the longest cut by shares.  No more than kMostCut blocks of 256
+// rows a CU have, since more blocks than that are not cut; a larger call asks for as much as that one, so that a workspace is enough for smaller calls too.
+constexpr int kMostCut = 8;
+long most_part_rows(const percache_config &c, int n_cu, int n_rows) {
+  const long rows = (long)(c.n_q_heads / c.n_kv_heads) * n_rows, cut = (long)kMostCut * std::max(1, n_cu / c.n_kv_heads) * kWideRows;
+  return std::max(std::min(rows, cut), std::min(rows * kMaxPackedSplits, 2L * n_cu * kWideRows / c.n_kv_heads));
 }
 PackedWs carve(const percache_config &c, int n_cu, void *base, int n_seq, int n_rows, int max_chunks) {
   PackedWs w;
@@ -1179,7 +1182,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   // and a walk each) or not (many keys: two and eight times as many are walked), whether the partitions are asked for or chosen.  A walk of 20 tiles at
   // head size 128: 8 blocks of 256 rows 37.5 us, 16 of 128 30; 64 and 128 39, 32; 128 and 256 42.3, 36.8.
   std::vector<Block> blocks = cut(kWideRows);
-  float best = n_splits > 0 || (long)blocks.size() <= 8L * cus ? settle(blocks) : 0.f;   // (more blocks than that even out uncut)
+  float best = n_splits > 0 || (long)blocks.size() <= (long)kMostCut * cus ? settle(blocks) : 0.f;   // (more blocks than that even out uncut)
   std::vector<int> best_ends = ends;
   auto lower = [&](int height, long most) {
     std::vector<Block> low = cut(height);

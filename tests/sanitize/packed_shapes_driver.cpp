@@ -24,6 +24,24 @@ void rows_of_a_launch() {
   }
 }
 
+// Workspaces: what is enough for a call is enough for every smaller one, and partial rows are kept for no more blocks than are ever cut.
+void packed_sizes() {
+  for (const auto &h : {std::array<int, 3>{32, 8, 128}, {2, 1, 128}, {14, 2, 64}, {16, 16, 64}}) {
+    Context x(h[0], h[1], h[2], 1, 0, 64);
+    const int G = h[0] / h[1];
+    size_t before = 0;
+    long rows_before = 0;
+    for (long n = 1; n < 9000000; n += 1 + n / 3) {
+      const size_t bytes = percache_packed_workspace_bytes(x.ctx, 3, (int32_t)n, 2);
+      expect(bytes >= before, "sizes: smaller calls");
+      if (rows_before * G / 256 > 8L * 256 / h[1])   // (8 blocks a CU and more: every further row only lengthens the lists)
+        expect(bytes - before <= (size_t)((n - rows_before) * G / kNarrowRows + 1) * (kItemWords + kMergeWords) * 4 + 3 * 256, "sizes: rows that are never cut");
+      before = bytes;
+      rows_before = n;
+    }
+  }
+}
+
 void one_call(int Hq, int Hkv, int D, int n_slots, int n8, int C) {
   auto read = [](int n) {
     std::vector<int32_t> v(n);
@@ -71,6 +89,7 @@ void one_call(int Hq, int Hkv, int D, int n_slots, int n8, int C) {
 int main(int argc, char **argv) {
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "rows") rows_of_a_launch();
+  if (what == "sizes") packed_sizes();
   int Hq, Hkv, D, n_slots, n8, C;
   while (what == "calls" && std::cin >> Hq >> Hkv >> D >> n_slots >> n8 >> C) one_call(Hq, Hkv, D, n_slots, n8, C);
   std::printf(bad ? "shapes driver: %d FAILED checks\n" : "shapes driver: ok\n", bad);

@@ -90,3 +90,7 @@ def test_blocks_where_partitions_are_asked_for(driver):
 
 def test_rows_of_a_projection_that_a_launch_holds(driver):
     driver("rows")
+
+
+def test_workspaces_grow_with_the_call_and_no_further_than_what_is_cut(driver):
+    driver("sizes")
