@@ -181,6 +181,7 @@ def _i32_list(a, shape=None):
 
 class Percache:
     """One context = one arena (a torch uint8 CUDA tensor) + host bookkeeping.  Methods mirror the C calls."""
+    kept_shapes = 256   # sizes of workspaces, and lists of equal chunk counts, that are kept from call to call
 
     def __init__(self, *, n_layers=1, hidden=1024, n_q_heads=16, n_kv_heads=8, head_dim=128, n_slots=16,
                  slot_capacity=512, max_pos=4096, rope_theta=10000.0, bank_capacity=0, emb_dim=0, kv_fp8=False,
@@ -518,11 +519,17 @@ class Percache:
             self._captured_ws[ws.data_ptr()] = ws
         return (ws.data_ptr() + 255) // 256 * 256
 
+    def _keep_size(self, key, n: int) -> int:
+        """A server's calls have ever new shapes: when as many sizes as kept_shapes are there, they are forgotten."""
+        if len(self._draft_bytes) >= self.kept_shapes:
+            self._draft_bytes.clear()
+        self._draft_bytes[key] = n
+        return n
+
     def _draft_need(self, batch, t_draft, max_chunks) -> int:
         key = (batch, t_draft, max_chunks)
-        if key not in self._draft_bytes:
-            self._draft_bytes[key] = self.lib.percache_draft_workspace_bytes(self.ctx, *key)
-        return self._draft_bytes[key]
+        need = self._draft_bytes.get(key)
+        return self._keep_size(key, self.lib.percache_draft_workspace_bytes(self.ctx, *key)) if need is None else need
 
     def _raw_stream(self):
         import torch
@@ -544,7 +551,12 @@ class Percache:
                 raise ValueError(f"slot_ids: {ids.size} entries for {batch} queries")
         ul, ul_p = _i32_list(used_len, (batch, max_chunks))
         if n_chunks is None:
-            nc, nc_p = self._all_chunks.get((batch, max_chunks)) or self._all_chunks.setdefault((batch, max_chunks), _i32_list(np.full(batch, max_chunks, np.int32)))
+            all_of_them = self._all_chunks.get((batch, max_chunks))
+            if all_of_them is None:
+                if len(self._all_chunks) >= self.kept_shapes:
+                    self._all_chunks.clear()
+                all_of_them = self._all_chunks[batch, max_chunks] = _i32_list(np.full(batch, max_chunks, np.int32))
+            nc, nc_p = all_of_them
         else:
             nc, nc_p = _i32_list(n_chunks, (batch,))
         return (ids, ul, nc), ids_p, ul_p, nc_p, max_chunks
@@ -747,7 +759,7 @@ class Percache:
         key = ("packed", n_seq, n, max_chunks)
         need = self._draft_bytes.get(key)
         if need is None:
-            need = self._draft_bytes[key] = self.lib.percache_packed_workspace_bytes(self.ctx, n_seq, n, max_chunks)
+            need = self._keep_size(key, self.lib.percache_packed_workspace_bytes(self.ctx, n_seq, n, max_chunks))
         st = self.lib.percache_attention_packed(self.ctx, layer, q.data_ptr(), k.data_ptr(), v.data_ptr(), n, start_p, n_seq, ids_p, ul_p, nc_p, max_chunks, n_splits,
                                                 attn_out.data_ptr(), _ptr(lse_out), self._draft_workspace(need, stream), need, stream)
         self._check(st)
@@ -778,7 +790,7 @@ class Percache:
         key = ("beams", batch, beams, vocab, best)
         need = self._draft_bytes.get(key)
         if need is None:
-            need = self._draft_bytes[key] = self.lib.percache_beam_select_workspace_bytes(self.ctx, batch, beams, vocab, best)
+            need = self._keep_size(key, self.lib.percache_beam_select_workspace_bytes(self.ctx, batch, beams, vocab, best))
         st = self.lib.percache_beam_select(self.ctx, logits.data_ptr(), int(logits.dtype == torch.float32), stride, scores.data_ptr(), batch, beams, vocab, best,
                                            parent.data_ptr(), token.data_ptr(), score.data_ptr(), self._draft_workspace(need, stream), need, stream)
         self._check(st)
