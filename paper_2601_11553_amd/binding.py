@@ -210,7 +210,6 @@ class Percache:
         self._step_ws = None
         self._lookup_ws = None
         self._topk_ws = None
-        self._captured_ws = {}   # workspaces that a graph has the address of
         self._draft_ws = {}
         self._all_chunks = {}    # lists of equal numbers of chunks, and their addresses
         self._draft_bytes = {}
@@ -509,14 +508,16 @@ class Percache:
 
     # ------------------------------------------------------------------ drafted tokens, eviction inside a slot
     def _draft_workspace(self, nbytes: int, stream):
-        """Each stream's own: one that is outgrown goes back to the memory of the stream it was made on, where nothing else has used it, unless a captured
-        call has it."""
+        """Each stream's own: one that is outgrown goes back to the memory of the stream it was made on, where nothing else has used it.  A captured call has one
+        of its graph's memory, as the tensors have that are made in a capture: graphs share theirs neither with each other nor with eager calls, and it goes with the
+        graph.  (What is captured behind the call may take it over: the address is all that is kept of it here.)"""
         import torch
-        ws = self._draft_ws.get(stream)
-        if ws is None or ws.numel() < nbytes + 256:
-            ws = self._draft_ws[stream] = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         if torch._C._cuda_isCurrentStreamCapturing():
-            self._captured_ws[ws.data_ptr()] = ws
+            ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
+        else:
+            ws = self._draft_ws.get(stream)
+            if ws is None or ws.numel() < nbytes + 256:
+                ws = self._draft_ws[stream] = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.device)
         return (ws.data_ptr() + 255) // 256 * 256
 
     def _keep_size(self, key, n: int) -> int:

@@ -1,4 +1,6 @@
 """What the binding keeps from call to call, without a device: its calls reach a stand-in for the library that does nothing."""
+import weakref
+
 import numpy as np
 import pytest
 import torch
@@ -18,7 +20,7 @@ def pc(monkeypatch):
     pc = Percache.__new__(Percache)
     pc.lib, pc.ctx, pc.device = Library(), None, torch.device("cpu")
     pc.cfg = Config(1, 256, 4, 2, 64, 8, 64, 1000, 1e4, 0, 0, 0, 0)
-    pc._draft_ws, pc._draft_bytes, pc._all_chunks, pc._captured_ws = {}, {}, {}, {}
+    pc._draft_ws, pc._draft_bytes, pc._all_chunks = {}, {}, {}
     monkeypatch.setattr(pc, "_raw_stream", lambda: 5, raising=False)
     monkeypatch.setattr(pc, "_want", lambda *a: None, raising=False)
     monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: False)
@@ -40,3 +42,29 @@ def test_calls_on_packed_rows_keep_no_size_for_good(pc):
         pc.percache_attention_packed(0, x, x[:2], x[:2], [0, n])
         assert len(pc._draft_bytes) <= Percache.kept_shapes
     assert ("packed", 1, n, 0) in pc._draft_bytes
+
+
+def test_a_captured_calls_workspace_is_its_graphs(pc, monkeypatch):
+    """Neither the stream's own one, which eager calls and other graphs would write, nor kept behind the call."""
+    made, given, empty = [], [], torch.empty
+
+    def watched(n, **kw):
+        t = empty(n, **kw)
+        made.append((weakref.ref(t), t.data_ptr(), n))
+        return t
+    monkeypatch.setattr(torch, "empty", watched)
+    monkeypatch.setattr(Library, "percache_beam_select", lambda lib, ctx, *args: given.append(args[-3]) or 0, raising=False)
+    x, scores = torch.zeros((2, 3, 40)), torch.zeros((2, 3))
+    logits = type("OnTheGpu", (), dict(dim=lambda s: 3, dtype=torch.float32, is_cuda=True, stride=lambda s, i: x.stride(i), shape=x.shape, data_ptr=lambda s: 0))()
+    call = lambda: pc.percache_beam_select(logits, scores, 4)
+    inside = lambda at, ws: ws[1] <= at < ws[1] + ws[2]
+    call()
+    own = pc._draft_ws[5]
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: True)
+    for _ in range(2):
+        call()
+    monkeypatch.setattr(torch._C, "_cuda_isCurrentStreamCapturing", lambda: False)
+    call()
+    assert len(made) == 3 and len(given) == 4
+    assert inside(given[0], made[0]) and inside(given[1], made[1]) and inside(given[2], made[2]) and inside(given[3], made[0])
+    assert made[0][0]() is own and pc._draft_ws == {5: own} and made[1][0]() is None and made[2][0]() is None
