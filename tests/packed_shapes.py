@@ -32,3 +32,14 @@ def slots_of(shape):
         return tokens, None, None
     ids = np.random.default_rng(len(tokens)).permutation(len(T) * n_c).reshape(len(T), n_c)
     return tokens, ids, np.minimum(np.array(used, np.int32), np.array(tokens, np.int32)[ids])
+# calls of the GPU tests: (shape, formats of the chunks, partitions asked for)
+CALLS = [(name, f, n) for shapes, splits in ((TALL, (0, 1, 2, 3)), (MIDDLE, (0, 3, 7))) for name in shapes
+         for f in (("bf16", "8bit", "mixed") if shapes[name][4] else ("bf16",)) for n in splits]
+# requests whose later rows, or whose slots behind the used length, hold what is not finite
+RUBBISH = {
+    "32over8x128": (32, 8, 128, [300, 130, 600, 64], [[60], [1], [64], [33]], 64),
+    "32over32x64": (32, 32, 64, [300, 1, 257, 513], [[100], [64], [127], [1]], 128),
+    "14over2x64": (14, 2, 64, [1000, 700, 900], [[63], [0], [64]], 64),
+    "16over16x128": (16, 16, 128, [520, 300, 700, 265], [[17], [128], [66], [9]], 128),
+}
+RUBBISH_CALLS = [(name, f, n) for name in RUBBISH for f in ("bf16", "8bit", "mixed") for n in (0, 1, 3)]

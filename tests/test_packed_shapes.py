@@ -9,7 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 
-from packed_shapes import MIDDLE, TALL, slots_of
+from packed_shapes import CALLS, MIDDLE, RUBBISH, RUBBISH_CALLS, TALL, slots_of
 from test_sanitizers import ENV, ROOT, SAN, _clean, _run
 
 pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"), reason="no hipcc")
@@ -94,3 +94,36 @@ def test_rows_of_a_projection_that_a_launch_holds(driver):
 
 def test_workspaces_grow_with_the_call_and_no_further_than_what_is_cut(driver):
     driver("sizes")
+
+
+def test_what_the_gpu_tests_of_tall_blocks_plan(driver):
+    """Every form of the wide blocks is among them: both head sizes, chunks of either format and of both, whole and in partitions, lists of more than 64 entries."""
+    shapes = {**TALL, **MIDDLE}
+    seen = set()
+    for (name, f, n), items in zip(CALLS, plans(driver, [(shapes[name], f, n) for name, f, n in CALLS])):
+        c, cut = classes(items), {0: (False, True), 1: (False,)}.get(n, (True,))
+        if name in TALL:
+            assert any(c["tall", x] for x in cut), (name, f, n, c)
+        else:
+            assert c["middle", True] or c["tall", True], (name, f, n, c)
+        for i in items:
+            if i.kind == 0:
+                seen.add((shapes[name][2], i.rows > 128, bool(i.partial), "mixed" if i.bf16 and i.eight else "8bit" if i.eight else "bf16" if i.cached else "fresh", i.cached > 0 and i.fresh > 0))
+                if i.entries > 64 and i.rows > 128:
+                    seen.add((shapes[name][2], "long", "mixed" if i.eight and i.bf16 else "8bit" if i.eight else "bf16"))
+    for D in (64, 128):
+        for walk in ("bf16", "8bit", "mixed"):
+            assert (D, "long", walk) in seen
+            for partial in (False, True):
+                assert (D, True, partial, walk, True) in seen, (D, partial, walk)
+            assert {x for x in seen if x[:2] == (D, False) and x[3] == walk}, (D, walk)
+        assert (D, True, True, "fresh", False) in seen and {x for x in seen if x[:2] == (D, False) and x[2]}
+    assert (128, True, False, "fresh", False) in seen
+
+
+def test_what_the_gpu_tests_with_rubbish_plan(driver):
+    """Tall blocks, whole and in partitions, over a last tile that later rows and used lengths end."""
+    for (name, f, n), items in zip(RUBBISH_CALLS, plans(driver, [(RUBBISH[name], f, n) for name, f, n in RUBBISH_CALLS])):
+        c = classes(items)
+        assert c["tall", n > 1] or (n == 0 and c["tall", True]), (name, f, n, c)
+        assert any(i.rows > 128 and i.fresh and i.cached for i in items), (name, f, n)
