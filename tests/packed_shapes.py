@@ -43,3 +43,11 @@ RUBBISH = {
     "16over16x128": (16, 16, 128, [520, 300, 700, 265], [[17], [128], [66], [9]], 128),
 }
 RUBBISH_CALLS = [(name, f, n) for name in RUBBISH for f in ("bf16", "8bit", "mixed") for n in (0, 1, 3)]
+# rows of a projection: heads, kv heads, head size, rows, heads a group of lanes.  On both sides of where the groups take four heads (rows * heads * D / 16 = 1024 a CU) and
+# where they take two, past the caches (rows * heads * D * 4 bytes = 160 MiB); head counts that neither divides
+ROWS = [
+    (14, 2, 128, 1820, 1), (14, 2, 128, 1821, 4), (14, 2, 128, 18204, 4), (14, 2, 128, 18205, 2),
+    (3, 3, 128, 3640, 1), (3, 3, 128, 3641, 4), (3, 3, 128, 36408, 4), (3, 3, 128, 36409, 2),
+    (14, 2, 64, 3640, 1), (14, 2, 64, 3641, 4), (14, 2, 64, 36408, 4), (14, 2, 64, 36409, 2),
+    (6, 2, 64, 6553, 1), (6, 2, 64, 6554, 4), (6, 2, 64, 65536, 4), (6, 2, 64, 65537, 2),
+]

@@ -2,6 +2,7 @@
 //   Hq Hkv D n_slots n_slots_8bit capacity  tokens of every slot  n_splits n_requests chunks  rows of every request  slots, used lengths of its chunks
 // and for each call a line "call STATUS ITEMS MERGES LISTS_IN_ARGUMENTS" and its items, a line each:
 //   rows kind cached_tiles fresh_tiles partial entries bf16 8-bit    (partial: 1 for one of several partitions; bf16, 8-bit: whether it walks such chunks)
+// "rotations": Hq Hkv D rows, answered by the workgroups of the launch.
 // Built and run by tests/test_packed_shapes.py.
 #define main main_of_packed_driver
 #include "packed_driver.cpp"
@@ -90,7 +91,13 @@ int main(int argc, char **argv) {
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "rows") rows_of_a_launch();
   if (what == "sizes") packed_sizes();
-  int Hq, Hkv, D, n_slots, n8, C;
+  int Hq, Hkv, D, n_slots, n8, C, rows;
+  while (what == "rotations" && std::cin >> Hq >> Hkv >> D >> rows) {
+    Context x(Hq, Hkv, D, 1, 0, 64);
+    expect(percache_qkv_norm_rope(x.ctx, x.arena, (Hq + 2 * Hkv) * D, rows, (int32_t *)x.arena, 1, nullptr, nullptr, nullptr, nullptr, 0.f, x.arena, x.arena, x.arena, nullptr) == PC_OK,
+           "rotations: call");
+    std::printf("workgroups %u\n", pushed.grid.x);
+  }
   while (what == "calls" && std::cin >> Hq >> Hkv >> D >> n_slots >> n8 >> C) one_call(Hq, Hkv, D, n_slots, n8, C);
   std::printf(bad ? "shapes driver: %d FAILED checks\n" : "shapes driver: ok\n", bad);
   return bad ? 1 : 0;

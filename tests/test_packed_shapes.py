@@ -9,7 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 
-from packed_shapes import CALLS, MIDDLE, RUBBISH, RUBBISH_CALLS, TALL, slots_of
+from packed_shapes import CALLS, MIDDLE, RUBBISH, RUBBISH_CALLS, ROWS, TALL, slots_of
 from test_sanitizers import ENV, ROOT, SAN, _clean, _run
 
 pytestmark = pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"), reason="no hipcc")
@@ -127,3 +127,12 @@ def test_what_the_gpu_tests_with_rubbish_plan(driver):
         c = classes(items)
         assert c["tall", n > 1] or (n == 0 and c["tall", True]), (name, f, n, c)
         assert any(i.rows > 128 and i.fresh and i.cached for i in items), (name, f, n)
+
+
+def test_forms_of_the_rotation_that_the_gpu_tests_take(driver):
+    words = driver("rotations", [" ".join(map(str, c[:4])) for c in ROWS]).split()
+    for (Hq, Hkv, D, rows, each), got in zip(ROWS, words[1::2]):
+        workgroups = lambda n: (rows * -(-(Hq + 2 * Hkv) // n) * (D // 16) + 255) // 256
+        assert int(got) == workgroups(each) and all(workgroups(n) != workgroups(each) for n in {1, 2, 4} - {each}), (Hq, Hkv, D, rows)
+    assert {(c[2], c[4]) for c in ROWS} == {(d, n) for d in (64, 128) for n in (1, 2, 4)}
+    assert all(any((c[0] + 2 * c[1]) % n and c[4] == n for c in ROWS) for n in (2, 4))
