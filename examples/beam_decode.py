@@ -83,16 +83,19 @@ class BeamDecoder:
     def choose(self, logits):
         parent, token, self.scores = self.pc.percache_beam_select(logits, self.scores, self.beams)
         parent, token = parent.cpu().numpy(), token.cpu().numpy()
-        # every beam's slot becomes that of the beam it goes on from, all at once
-        src = np.take_along_axis(self.slots, parent, 1)
+        # every beam's slot becomes that of the beam it goes on from, all at once.  Where a request has fewer continuations than beams, the others do not exist: a score of
+        # -infinity keeps them from being gone on from, their tokens are -1, and their slots are copies of the first beam's, since a row that is computed needs one.
+        exists, parent_or_first = parent >= 0, np.maximum(parent, 0)
+        src = np.take_along_axis(self.slots, parent_or_first, 1)
         self.pc.percache_kv_fork(src.ravel(), self.slots.ravel())
-        self.tokens = np.concatenate([np.take_along_axis(self.tokens, parent[..., None], 1), token[..., None]], 2)
+        before = np.where(exists[..., None], np.take_along_axis(self.tokens, parent_or_first[..., None], 1), -1)
+        self.tokens = np.concatenate([before, token[..., None]], 2)
         self.parent, self.token = parent, token
 
     def step(self):
         """Every beam of every request by one token."""
         B, K = self.batch, self.beams
-        x = self.embed[torch.from_numpy(self.token.ravel().astype(np.int64)).to(self.embed.device)]
+        x = self.embed[torch.from_numpy(np.maximum(self.token, 0).ravel().astype(np.int64)).to(self.embed.device)]
         pos = np.repeat(self.position, K)
         self.position += 1
         ids = np.concatenate([np.tile(np.arange(self.chunks, dtype=np.int32), (B * K, 1)), self.slots.reshape(-1, 1)], 1)
