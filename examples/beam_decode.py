@@ -23,11 +23,11 @@ class BeamDecoder:
 
     def __init__(self, batch=4, beams=4, chunks=3, capacity=512, longest=200, vocab=5000, hidden=1024, heads=16, kv_heads=8, head_dim=128, seed=0, n_slots_8bit=0,
                  device="cuda:0"):
-        self.batch, self.beams, self.chunks, self.vocab, self.heads, self.kv_heads, self.D = batch, beams, chunks, vocab, heads, kv_heads, head_dim
+        self.batch, self.beams, self.chunks, self.capacity, self.vocab, self.heads, self.kv_heads, self.D = batch, beams, chunks, capacity, vocab, heads, kv_heads, head_dim
         self.rng = np.random.default_rng(seed)
         self.gen = torch.Generator(device=device).manual_seed(seed)
         self.pc = Percache(n_layers=1, hidden=hidden, n_q_heads=heads, n_kv_heads=kv_heads, head_dim=head_dim, n_slots=chunks + batch * beams, slot_capacity=capacity,
-                           max_pos=1 << 13, n_slots_8bit=n_slots_8bit, device=device)
+                           max_pos=max(1 << 13, (chunks + 1) * capacity + 64), n_slots_8bit=n_slots_8bit, device=device)
         self.embed = self._randn(vocab, hidden)
         self.wqkv = self._randn((heads + 2 * kv_heads) * head_dim, hidden) / hidden ** 0.5
         self.wo = self._randn(hidden, heads * head_dim) / (heads * head_dim) ** 0.5
@@ -43,8 +43,8 @@ class BeamDecoder:
         return torch.randn(shape, generator=self.gen, device=self.gen.device).to(torch.bfloat16)
 
     def prompt_positions(self, b):
-        """[3, length]: text, and now and then a picture in the middle of it."""
-        n, at, pos = int(self.lengths[b]), self.chunks * 512, []
+        """[3, length]: text, and now and then a picture in the middle of it, behind the chunks."""
+        n, at, pos = int(self.lengths[b]), self.chunks * self.capacity, []
         while len(pos) < n:
             if self.rng.random() < 0.5:
                 pos += [(at + i, at + i, at + i) for i in range(20)]

@@ -1,8 +1,9 @@
-"""The host side of examples/beam_decode.py: beams that do not exist."""
+"""The host side of examples/beam_decode.py: beams that do not exist, positions behind the chunks."""
 import os
 import sys
 
 import numpy as np
+import pytest
 import torch
 
 from oracle import packed_ref as ref
@@ -47,3 +48,11 @@ def test_fewer_continuations_than_beams():
     assert (d.parent[0] >= 0).all() and 3 not in d.parent[0] and (d.parent[1] == -1).all()
     assert all(t[0] == [1, 2, 0][p] for t, p in zip(d.tokens[0].tolist(), d.parent[0])) and (d.tokens[1] == -1).all()
     assert d.pc.copies[-1][0][4:] == [5] * 4
+
+
+@pytest.mark.parametrize("capacity", [64, 512, 4096])
+def test_prompts_start_behind_the_chunks(capacity):
+    d = decoder(1, 2, 3, 10)
+    d.capacity, d.lengths, d.position, d.rng = capacity, np.array([50]), np.zeros(1, np.int64), np.random.default_rng(1)
+    pos = d.prompt_positions(0)
+    assert pos.shape == (3, 50) and pos.min() == 3 * capacity and d.position[0] == pos.max() + 1 and pos.max() < 4 * capacity
