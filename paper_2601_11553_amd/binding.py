@@ -508,7 +508,7 @@ class Percache:
 
     # ------------------------------------------------------------------ drafted tokens, eviction inside a slot
     def _draft_workspace(self, nbytes: int, stream):
-        """Each stream's own: one that is outgrown goes back to the memory of the stream it was made on, where nothing else has used it.  A captured call has one
+        """Each stream's own, so calls may be in flight on several streams where none writes what another reads or writes.  One that is outgrown goes back to the memory of the stream it was made on, where nothing else has used it.  A captured call has one
         of its graph's memory, as the tensors have that are made in a capture: graphs share theirs neither with each other nor with eager calls, and it goes with the
         graph.  (What is captured behind the call may take it over: the address is all that is kept of it here.)"""
         import torch
@@ -734,7 +734,8 @@ class Percache:
 
     def percache_attention_packed(self, layer, q, k, v, start, slot_ids=None, used_len=None, n_chunks=None, n_splits: int = 0, attn_out=None, lse_out=None):
         """(attn_out [N, Hq * D], lse [Hq, N] or None) of packed rows q [Hq, N, D], k, v [Hkv, N, D]; start: the requests' first rows and the end of the
-        last one.  lse_out: a float32 tensor, True for a new one, None for none.  Rows of no request are left as they are (new tensors: unset)."""
+        last one.  lse_out: a float32 tensor, True for a new one, None for none.  Rows of no request are left as they are (new tensors: unset).
+        A captured call keeps its lists, chunks and lengths included; one whose lists are longer than a launch's arguments (980 words) is refused."""
         import torch
         bf16 = torch.bfloat16
         c = self.cfg

@@ -13,10 +13,14 @@
 // What a row does not see takes no part, whatever stands there: K by the mask on the scores; V behind the end of a chunk or a request by clearing the
 // operand; V of a later token of the same tile, where it is not finite, by computing the rows that it made NaN once more, key by key.
 //
-// What bounds it: prompts the matrix products and, at their rate, the power (32 heads over 8, ten prompts of 574 to 6964 tokens: 895 us, 1.04 PFLOP/s of the
-// scores that count; a tile of 256 rows takes 3350 cycles, 2048 of them products, at 1.5 GHz with all CUs on such data); single tokens the key stream (32 tokens over 6100 cached
-// keys each, 700 MB: 120 us, 5.8 TB/s); short calls the launch (5 prompts of 11 to 71 tokens: 7.8 us).  256 rows a block: fewer would read every tile
-// from LDS and memory more often, a wavefront's 32 are what its registers hold beside the scores of 64 keys.
+// What bounds it: prompts the matrix products and the exponentials, whose units overlap in part only.  Head size 128, 256 workgroups of 256 rows over 129 tiles, one a CU: 3620
+// cycles a tile on zeros and 3730 on random data, start and end among them, 2048 of them products (0.55 of the cycles); the clock falls from 2.45 to 1.98 GHz
+// on random data.  Ten prompts of 574 to 6964 tokens, 32 heads over 8: 890 us, 1.04 PFLOP/s of the scores that count, products in 0.48 of 1.87 M cycles at 2.1 GHz (767 us at 2.4 GHz on
+// zeros).  Head size 64 has half of the products and all of the exponentials: 14 heads over 2, the same prompts 246 us, 0.83 PFLOP/s, products in 0.33 of the cycles and
+// vector instructions in 0.49.  Single tokens: the key stream (32 tokens over 6100 cached keys each, 700 MB: 120 us, 5.8 TB/s).  Short calls: the launch (5 prompts of 11 to 71
+// tokens: 7.8 us).  256 rows a block: fewer would read every tile from LDS and memory more often, a wavefront's 32 are what its registers hold beside the scores of 64
+// keys.  With 8-bit tiles at head size 128 they hold them not quite: 9 registers are spilled, none of them on the usual way of the loop.  What reads them back there, the request
+// of a tile that ends early and the refresh of the reference exponent, waits for all tiles in flight.
 #include <algorithm>
 #include <exception>
 #include <cmath>
@@ -197,7 +201,7 @@ struct Walk {
 };
 
 // One row of an item once more, key by key, by one wavefront: what the row does not see is not touched.  Rows that need it are those of a tile in which a
-// later token's V is not finite.
+// later token's V is not finite.  Their probabilities stay in 32 bits, so they are not, to the last bit, what they are beside finite rows, and nearer to the exact ones.
 template <int D, bool KV8>
 __device__ __forceinline__ void redo_row(const Args &a, const Item &it, int gkv, int lane, int local, float &m_out, float &l_out, float (&o)[D / 64]) {
   constexpr int E = D / 64;
@@ -1007,8 +1011,9 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     cached[s] = tiles;
   }
   first_ent[n_seq] = (int)ents.size() / 2;
-  // us of a workgroup's start and end, of a MB from memory and of a tile of more than 128 rows, of more than 32, 16, fewer (most of the chip at work: the clock
-  // falls; alone 1.37 and 1.11 of the first two at head size 128, 1.02 and 0.78 at 64), of 8-bit tiles 2.4, 1.57, ..
+  // us of a workgroup's start and end, of a MB from memory and of a tile of more than 128 rows, of more than 32, 16, fewer (most of the chip at work on random data: the
+  // clock falls; with few workgroups 1.37 and 1.11 of the first two at head size 128, 1.02 and 0.78 at 64), of 8-bit tiles 2.4, 1.57, ..  8-bit tiles cost more because their codes are
+  // turned into bf16 ones between the wait for them and the barrier, where no product runs; at head size 64 by half of the threads.
   constexpr float kStart = 6.f, kStartLow = 4.f, kPerMb = 1.f / 5.4f;
   constexpr float kTile[2][2][4] = {{{1.28f, 0.97f, 0.52f, 0.45f}, {1.55f, 1.07f, 0.60f, 0.52f}}, {{1.85f, 1.54f, 0.88f, 0.72f}, {2.40f, 1.57f, 0.76f, 0.65f}}};
   float tile_of[4];
@@ -1036,8 +1041,9 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   // Partitions: blocks that take longer than a limit, one for each kind, are cut evenly, or all are cut by shares.  A launch is dealt out longest first to the
   // CUs, of which every kv head gets its share; that is played through (while there are few workgroups a CU: many even out by themselves), and what
   // promises 3 % more is taken.  Nothing is faster than its keys come from memory; a merge is a launch and the partial rows.  us at 1, 2, 3, 4
-  // partitions, measured: 72 wide blocks of 60 tiles 95, 64, 53, 60; head size 64, 152 of 36 to 60 tiles 84, 80, 70; 144 narrow ones of 52 tiles 53, 62, 53,
-  // 59, 32 of them 48, 32, 24, 22, 200 wide ones of 50 to 60 tiles beside the 144 134 (cut evenly into 712 workgroups 151).
+  // partitions, measured (workgroups of all kv heads): 72 wide blocks of 60 tiles at head size 128 95, 64, 53, 60; head size 64, 152 of 36 to 60 tiles (14 heads over 2, seven questions of 43 to
+  // 1142 rows behind 2.3k cached keys) 84, 80, 70; 144 narrow ones of 52 tiles (24 heads over 8, 18 single tokens over 3k keys) 53, 62, 53, 59, 32 of them 48, 32, 24, 22; 200 wide ones of 50 to 60
+  // tiles (six questions of 118 to 595 rows) beside the 144 134 (cut evenly into 712 workgroups 151).
   auto least_of = [&](const Block &b) { return class_of(b) == 0 ? 6 : 4; };   // tiles of a partition
   const int cus = std::max(1, ctx->n_cu / c.n_kv_heads);
   float mb = 0.f;
@@ -1134,7 +1140,7 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
     for (Block &x : blocks) x.n = parts_of(x.kind, least_of(x), start_us(x), tile_us(x), x.tiles, best_limit);
     // The blocks' keys laid end to end and cut where a CU's share ends, the share a little longer from try to try until it is enough: partitions are as long as
     // a share or what is left of one on either side of a block's end, and the launch puts the latter together again, longest with shortest (the 200 wide blocks
-    // alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64 and 8-bit chunks 67, 59; with the 144 narrow ones 131 uncut, 138).
+    // named above alone, kernel and merge: 131 us cut evenly, 115 so; the 152 of head size 64, half of the chunks 8-bit, 67, 59; the 200 and the 144 narrow ones 131 uncut, 138).
     int tries = (long)blocks.size() <= 4L * cus ? 8 : 0;
     for (float share = std::max(whole / (float)cus + kStart, 2.f * kStart); tries > 0 && std::max(share, mb * kPerMb) + merge_us(1.f) < 0.97f * best; share *= 1.05f, --tries) {
       ends.clear();
