@@ -1189,7 +1189,8 @@ void plan_items(const percache_ctx *ctx, const std::vector<int32_t> &table, int 
   };
   // Blocks of 256 rows; where few of them would find the chip half empty, 128 or 32 rows each may be the faster ones (few keys: more workgroups, less of a start
   // and a walk each) or not (many keys: two and eight times as many are walked), whether the partitions are asked for or chosen.  A walk of 20 tiles at
-  // head size 128: 8 blocks of 256 rows 37.5 us, 16 of 128 30; 64 and 128 39, 32; 128 and 256 42.3, 36.8.
+  // head size 128: 8 blocks of 256 rows 37.5 us, 16 of 128 30; 64 and 128 39, 32; 128 and 256 42.3, 36.8.  Seven partitions asked for, 8 heads over 1 of 64, 700 and 430 rows
+  // behind 1135 and 575 keys: 84 us a call in blocks of 32 rows, 31 as they are chosen; 8 over 2 of 128, 513 and 300 rows behind 905 and 575: 79, 33.
   std::vector<Block> blocks = cut(kWideRows);
   float best = n_splits > 0 || (long)blocks.size() <= (long)kMostCut * cus ? settle(blocks) : 0.f;   // (more blocks than that even out uncut)
   std::vector<int> best_ends = ends;
